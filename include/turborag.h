@@ -11,6 +11,8 @@
  *   Sec. 3.3         documents and query in one pass with the masks and position ids of inference
  *                                                     -> tr_sequence_plan, tr_sequence_prefill_attn
  *   Eq. 1            projections around the attention for the query tokens -> tr_linear
+ *   Sec. 3.4 step 7  the same cache in pages, its lengths and block tables on the GPU -> tr_page_map, tr_rotary_init,
+ *                                                       tr_paged_append, tr_paged_decode_attn
  *
  * Conventions (all entry points):
  *   - Tensors are token-major, contiguous: [rows, heads, head_dim], element type `tr_shape.dtype`
@@ -280,6 +282,108 @@ int tr_sequence_prefill_attn(const tr_shape* shape, const void* q, const void* k
 size_t tr_linear_workspace_size(int32_t M, int32_t n_out, const int32_t* n_features /*host*/, int32_t K);
 int tr_linear(const void* x, int32_t M, int32_t K, int32_t n_out, const void* const* w /*host*/, void* const* y /*host*/,
               const int32_t* n_features /*host*/, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- a cache in pages (Sec. 3.4 steps 5 and 7 for a server whose requests come, grow and go) --------------------------------
+ * The calls above want a request's cache as contiguous rows and its length on the host.  The four calls below keep the rows of
+ * all requests in one pool of pages instead and read every length, page id and position on the GPU, so that one captured graph
+ * serves whatever lengths its buffers hold when it is replayed.  Per step: tr_page_map (which pages and rows the new tokens
+ * get), tr_paged_append (their heads, normalised and rotated, into those rows), tr_paged_decode_attn.  Assembled document rows
+ * reach the pages through tr_paged_append as well (rotary of no channels: a copy; with the store's rows, the chunk's offset as
+ * every row's position id and no norm: the re-rotation of tr_kv_assemble).
+ *
+ * tr_pages: the pool.  Row i of page p of KV head h begins at element p * page_stride + i * row_stride + h * head_stride of k
+ * (and of v) and is head_dim contiguous elements; so [page, row, head, channel] and [page, head, row, channel] pools, and pools
+ * whose k and v are halves of one allocation, are all described by their strides.  k, v 16-byte aligned, strides multiples of 16
+ * bytes and at most 64 MiB for rows and heads; page_size a power of two, 8 .. 1024; n_pages * page_size below 2^31; k, v and
+ * dtype, n_kv_heads and head_dim have to fit the tr_shape of the call (else TR_ERR_SHAPE).
+ * A slot is the index page * page_size + row of a row in the pool.  A page id outside [0, n_pages) means "no page": rows of
+ * such a page are never read or written, and attention gives their keys no weight. */
+typedef struct tr_pages {
+    void* k;
+    void* v;
+    int64_t page_stride; /* elements */
+    int64_t row_stride;
+    int64_t head_stride;
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t dtype;    /* tr_dtype */
+    int32_t reserved; /* must be 0 */
+} tr_pages;
+
+/* Block tables, slots, position ids and lengths of a batch, from its lengths, on the GPU.  All arrays device int32.
+ * cached_lens, new_lens [n_req]: tokens a request holds and tokens it is about to get (negative: 0); first_pos [n_req] or NULL:
+ * position id of its first new token (NULL: cached_lens, the reordered scheme; composite positions pass their own).  With
+ * have = ceil(cached / page_size), need = ceil((cached + new) / page_size), request r takes need - have pages, in order of r,
+ * from the front of free_pages [n_free]:
+ *   block_table [n_req, max_blocks], in and out: entries [have, need) of row r receive its new pages, all others stay;
+ *   kv_lens [n_req] = cached + new;  cu_new [n_req + 1] = prefix sums of new;
+ *   slots, pos [n_slots]: slot and position id of every new token, request after request; behind the last: -1 and 0;
+ *   counts [2] = new tokens of the batch, pages it takes (the caller's free list goes on behind them).
+ * n_slots may be more than the batch has tokens (a launch of fixed size); tokens beyond it get none.  Where free_pages or
+ * max_blocks do not suffice, the page id is -1 (entries beyond max_blocks are not written), the tokens' slots are -1, and
+ * counts[1] still says how many pages were needed.  Sums are cut at 2^31 - 1.  n_req <= 4096 (else TR_ERR_UNSUPPORTED).
+ * No output may overlap an input or another output, block_table's own entries aside (TR_ERR_INVALID_ARG). */
+int tr_page_map(const int32_t* cached_lens, const int32_t* new_lens, const int32_t* first_pos /*or NULL*/, int32_t n_req,
+                int32_t page_size, const int32_t* free_pages, int32_t n_free, int32_t* block_table, int32_t max_blocks,
+                int32_t* kv_lens, int32_t* cu_new, int32_t* slots, int32_t* pos, int32_t n_slots, int32_t* counts, void* stream);
+
+/* Which channels of a head turn, and how far.  Pair m < rotary_dim / 2 is channels (2m, 2m+1) or (m, m + rotary_dim/2) of the
+ * head (layout); it is turned by position * freq[m] radians and multiplied by amplitude; channels from rotary_dim on pass
+ * through.  rotary_dim: a multiple of 16 up to head_dim, 0 for none; 0 <= freq[m] <= 1. */
+typedef enum { TR_SCALE_NONE = 0, TR_SCALE_LINEAR = 1, TR_SCALE_BASE = 2, TR_SCALE_PARTS = 3 } tr_rope_scaling;
+typedef struct tr_rotary {
+    int32_t layout; /* tr_rope_layout */
+    int32_t rotary_dim;
+    double amplitude;
+    double freq[64];
+} tr_rotary;
+
+/* Fills *out (host only) for theta_m = base^(-2m/rotary_dim), r = rotary_dim, and a context stretched by factor s >= 1:
+ *   TR_SCALE_NONE    freq = theta
+ *   TR_SCALE_LINEAR  freq = theta / s (position interpolation, arXiv 2306.15595)
+ *   TR_SCALE_BASE    theta of the base base * s^(r/(r-2)): the slowest pair is slowed by s, the fastest not at all
+ *   TR_SCALE_PARTS   freq = theta (c + (1 - c) / s), c = clamp((t - slow_turns) / (fast_turns - slow_turns), 0, 1), where t =
+ *                    original_len * theta / 2 pi is how often the pair turns in the trained context (arXiv 2309.00071)
+ * factor, original_len, slow_turns and fast_turns are read only where the method uses them.  amplitude is a factor on the
+ * turned channels (1, or what the method's authors give for their s).  Errors: TR_ERR_INVALID_ARG, TR_ERR_SHAPE. */
+int tr_rotary_init(int32_t layout, int32_t rotary_dim, double base, int32_t scaling, double factor, double original_len,
+                   double slow_turns, double fast_turns, double amplitude, tr_rotary* out /*host*/);
+
+/* One pass over the heads of n_tokens tokens: each query and key head x [head_dim] is normalised where its weight is given,
+ *   y = x / sqrt(mean(x^2) + eps) * weight,
+ * turned at the token's position id, and rounded once; queries go to q_out, keys and values (unchanged) to the row of the pool
+ * that the token's slot names.  Tokens whose slot is outside the pool (padding: -1) write no key and no value.
+ *   rotary: NULL: all channels, by the shape's own layout and base (then pos is required)
+ *   q, q_out: [n_tokens, n_q_heads, head_dim], both or neither; k, v: [n_tokens, n_kv_heads, head_dim], with pages and slots,
+ *   or none of the four.  q_stride, k_stride, v_stride: elements between the rows of two tokens (heads of a token lie together),
+ *   so that the three may be parts of one packed projection; q_out is contiguous, and may be q itself where q is.
+ *   q_norm, k_norm: device [head_dim] in the shape's type, NULL: that side is not normalised; eps > 0
+ *   pos: device int32 [n_tokens] (NULL with a rotary of no channels), slots: device int32 [n_tokens], -1 or pairwise different
+ *   (of two tokens with one slot either may be the one that is kept, in parts).
+ * The sum of squares, the angle (64 bits) and all products are fp32 or wider.  Pointers and strides 16-byte aligned, else
+ * TR_ERR_INVALID_ARG.  n_tokens == 0 is a no-op. */
+int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* q, int64_t q_stride, const void* k,
+                    int64_t k_stride, const void* v, int64_t v_stride, const void* q_norm, const void* k_norm, double eps,
+                    const int32_t* pos, const int32_t* slots, int32_t n_tokens, void* q_out, const tr_pages* pages, void* stream);
+
+/* Attention of one new token per request over its pages.  q [n_req, n_q_heads, head_dim]: queries ALREADY normalised and
+ * rotated (tr_paged_append's q_out; unlike tr_decode_attn the kernel turns nothing); row j of request r is row j % page_size of
+ * page block_table[r][j / page_size]; the request has kv_lens[r] rows (device int32; at most max_blocks * page_size are looked
+ * at, a negative length is 0), the last of them the new token itself.  It attends row j where
+ *   window == 0 or j >= kv_lens[r] - window or j < n_sink
+ * (a window of the last `window` rows, and the first n_sink rows that stay visible); scores are scaled by 1/sqrt(head_dim).
+ * out [n_req, n_q_heads, head_dim].  A request that sees no row (length 0, or no page behind any visible row) gets zeros.  Rows
+ * that are not visible are not read as values: what they hold (NaN included) does not matter.
+ * Scores, softmax, weights and the weighted sum are fp32, whatever the type.  Results do not depend on how long the table is.
+ * workspace: tr_paged_decode_attn_workspace_size() bytes, 256-byte aligned, else TR_ERR_WORKSPACE; it depends on the arguments
+ * of the query alone, not on the lengths; calls that may overlap need one each.  q, out and pages 16-byte aligned.
+ * n_req <= 65536 (else TR_ERR_UNSUPPORTED); n_req == 0 is a no-op. */
+size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size);
+int tr_paged_decode_attn(const tr_shape* shape, const void* q, const tr_pages* pages, const int32_t* block_table /*device*/,
+                         int32_t max_blocks, const int32_t* kv_lens /*device*/, int32_t n_req, int32_t window, int32_t n_sink,
+                         void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- launch-policy override for tests and sweeps -------------------------------------------------------------------------
  * Sets a process-wide override of one value of the launch policy; value 0 restores the default.  Names: "wg_rows"

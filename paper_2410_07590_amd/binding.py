@@ -19,6 +19,7 @@ TR_ERR_UNSUPPORTED, TR_ERR_HIP, TR_ERR_WORKSPACE, TR_ERR_NO_MEMORY = -5, -6, -7,
 TR_POS_COMPOSITE, TR_POS_REORDERED = 0, 1
 TR_F32, TR_BF16 = 0, 1
 TR_ROPE_INTERLEAVED, TR_ROPE_HALF = 0, 1
+TR_SCALE_NONE, TR_SCALE_LINEAR, TR_SCALE_BASE, TR_SCALE_PARTS = 0, 1, 2, 3
 
 EXPORTS = [
     "tr_last_error", "tr_store_create", "tr_store_destroy", "tr_plan",
@@ -30,6 +31,7 @@ EXPORTS = [
     "tr_chunk_prefill_attn_workspace_size", "tr_chunk_prefill_attn",
     "tr_sequence_plan", "tr_sequence_prefill_attn_workspace_size", "tr_sequence_prefill_attn",
     "tr_linear_workspace_size", "tr_linear", "tr_set_tuning",
+    "tr_page_map", "tr_rotary_init", "tr_paged_append", "tr_paged_decode_attn_workspace_size", "tr_paged_decode_attn",
     "tr_probe_mfma_loop_sink_bytes", "tr_probe_mfma_loop",
 ]
 
@@ -38,6 +40,16 @@ class tr_shape(C.Structure):
     _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("dtype", C.c_int32), ("rope_base", C.c_double), ("rope_layout", C.c_int32),
                 ("reserved", C.c_int32)]
+
+
+class tr_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("row_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class tr_rotary(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rotary_dim", C.c_int32), ("amplitude", C.c_double), ("freq", C.c_double * 64)]
 
 
 class TurboRagError(RuntimeError):
@@ -66,7 +78,7 @@ def lib():
         for name in ("tr_prefill_attn_workspace_size", "tr_prefill_attn_batched_workspace_size",
                      "tr_prefill_attn_gather_workspace_size", "tr_decode_attn_workspace_size",
                      "tr_chunk_prefill_attn_workspace_size", "tr_sequence_prefill_attn_workspace_size",
-                     "tr_linear_workspace_size", "tr_prefill_attn_static_scratch_bytes",
+                     "tr_linear_workspace_size", "tr_paged_decode_attn_workspace_size", "tr_prefill_attn_static_scratch_bytes",
                      "tr_probe_mfma_loop_sink_bytes"):
             getattr(L, name).restype = C.c_size_t
         _tr_host.bind({name: C.cast(getattr(L, name), C.c_void_p).value for name in EXPORTS}, TurboRagError,
@@ -288,6 +300,51 @@ def tr_linear(x, w, y, workspace=None, stream=None):
     that share x."""
     ws_, ys_ = (list(w), list(y)) if isinstance(w, (list, tuple)) else ([w], [y])
     _native().linear(x, ws_, ys_, workspace, stream)
+
+
+def make_pages(k_pages, v_pages):
+    """The pool behind two device tensors [n_pages, page_size, n_kv_heads, head_dim] of equal strides, last one 1: a pool that
+    keeps the rows of a head together ([page, head, row, channel]) is passed as its transpose(1, 2).  Keeps the tensors alive."""
+    assert k_pages.is_cuda and v_pages.is_cuda and k_pages.device == v_pages.device, "pages are device tensors"
+    assert k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.stride() == v_pages.stride() and k_pages.dtype == v_pages.dtype
+    assert k_pages.stride(3) == 1, "the channels of a row must be contiguous"
+    n, size, heads, d = k_pages.shape
+    assert max(n, size, heads) < 2 ** 31
+    p = tr_pages(k_pages.data_ptr(), v_pages.data_ptr(), *k_pages.stride()[:3], n, size, heads, d,
+                 {torch.float32: TR_F32, torch.bfloat16: TR_BF16}[k_pages.dtype], 0)
+    if n == 1:
+        p.page_stride = 0   # never applied
+    if heads == 1:
+        p.head_stride = 0
+    p.tensors = (k_pages, v_pages)
+    return p
+
+
+def tr_page_map(cached_lens, new_lens, first_pos, page_size, free_pages, block_table, kv_lens, cu_new, slots, pos, counts, stream=None):
+    """All tensors device int32.  first_pos: None for position ids that go on from cached_lens."""
+    _native().page_map(cached_lens, new_lens, first_pos, page_size, free_pages, block_table, kv_lens, cu_new, slots, pos, counts, stream)
+
+
+def tr_rotary_init(layout, rotary_dim, base, scaling=TR_SCALE_NONE, factor=1.0, original_len=0.0, slow_turns=1.0, fast_turns=32.0,
+                   amplitude=1.0):
+    r = tr_rotary()
+    _check(lib().tr_rotary_init(C.c_int32(layout), C.c_int32(rotary_dim), C.c_double(base), C.c_int32(scaling), C.c_double(factor),
+                                C.c_double(original_len), C.c_double(slow_turns), C.c_double(fast_turns), C.c_double(amplitude),
+                                C.byref(r)))
+    return r
+
+
+def tr_paged_append(shape, rotary, q, k, v, q_norm, k_norm, eps, pos, slots, q_out, pages, stream=None):
+    """q, k, v: [tokens, heads, head_dim], rows any (16-byte aligned) distance apart.  None where the C interface takes NULL."""
+    _native().paged_append(shape, rotary, q, k, v, q_norm, k_norm, eps, pos, slots, q_out, pages, stream)
+
+
+def tr_paged_decode_attn_workspace_size(shape, n_req, max_blocks, page_size):
+    return int(lib().tr_paged_decode_attn_workspace_size(C.byref(shape), C.c_int32(n_req), C.c_int32(max_blocks), C.c_int32(page_size)))
+
+
+def tr_paged_decode_attn(shape, q, pages, block_table, kv_lens, window, n_sink, out, workspace=None, stream=None):
+    _native().paged_decode_attn(shape, q, pages, block_table, kv_lens, window, n_sink, out, workspace, stream)
 
 
 def workspace(nbytes, device="cuda"):

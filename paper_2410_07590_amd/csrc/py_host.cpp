@@ -22,7 +22,8 @@ namespace {
 #define TR_CALLS(X)                                                                                                          \
     X(tr_last_error) X(tr_plan) X(tr_kv_assemble) X(tr_kv_assemble_raw) X(tr_kv_assemble_batched) X(tr_kv_append)            \
     X(tr_kv_assemble_append) X(tr_kv_append_batched) X(tr_prefill_attn) X(tr_prefill_attn_static) X(tr_prefill_attn_batched) \
-    X(tr_prefill_attn_gather) X(tr_decode_attn) X(tr_chunk_prefill_attn) X(tr_sequence_prefill_attn) X(tr_linear)
+    X(tr_prefill_attn_gather) X(tr_decode_attn) X(tr_chunk_prefill_attn) X(tr_sequence_prefill_attn) X(tr_linear)                \
+    X(tr_page_map) X(tr_paged_append) X(tr_paged_decode_attn)
 struct Api {
 #define X(name) decltype(&::name) name;
     TR_CALLS(X)
@@ -412,6 +413,152 @@ PyObject* linear(Args a) // x, [w], [y], workspace, stream
     return run([&] { return api.tr_linear(xp, (int32_t)M, (int32_t)K, (int32_t)n, w.data(), y.data(), f.data(), ws.p, ws.bytes, s); });
 }
 
+// ---- the paged cache: what a pointer does not say (types, sizes, devices) is checked here ------------------------------
+// The tensors of a call lie on one device; without a stream that is the current one, whose stream is used.
+class Place {
+public:
+    const at::Tensor& on(PyObject* o, bool contiguous = true)
+    {
+        const at::Tensor& t = tensor(o);
+        if (!t.is_cuda()) fail(PyExc_AssertionError, "a device tensor is expected");
+        if (contiguous && !t.is_contiguous()) fail(PyExc_AssertionError, "device tensors must be contiguous");
+        const int d = t.device().index();
+        if (device_ >= 0 && d != device_) fail(PyExc_AssertionError, "the tensors of a call lie on one device");
+        device_ = d;
+        return t;
+    }
+    int32_t* ints(PyObject* o, int64_t* n = nullptr)
+    {
+        const at::Tensor& t = on(o);
+        if (t.scalar_type() != at::kInt) fail(PyExc_AssertionError, "an int32 tensor is expected");
+        if (n) *n = t.numel();
+        return (int32_t*)t.data_ptr();
+    }
+    int32_t* ints_of(PyObject* o, int64_t n)
+    {
+        int64_t have;
+        int32_t* p = ints(o, &have);
+        if (have != n) fail(PyExc_AssertionError, "an index tensor has an unexpected size");
+        return p;
+    }
+    void* stream_of(PyObject* o)
+    {
+        if (o == Py_None && device_ >= 0) {
+            PyObject* d = PyObject_CallNoArgs(current_device);
+            if (!d) throw Failed();
+            const long now = PyLong_AsLong(d);
+            Py_DECREF(d);
+            if (now == -1 && PyErr_Occurred()) throw Failed();
+            if (now != device_) fail(PyExc_AssertionError, "the tensors lie on another device than the current one");
+        }
+        return stream(o);
+    }
+
+private:
+    int device_ = -1;
+};
+int32_t small(int64_t n)
+{
+    if (n > INT32_MAX) fail(PyExc_ValueError, "a tensor has 2^31 entries or more");
+    return (int32_t)n;
+}
+void has_type(const at::Tensor& t, const tr_shape& s)
+{
+    if (t.scalar_type() != (s.dtype == TR_F32 ? at::kFloat : at::kBFloat16)) fail(PyExc_AssertionError, "a tensor has another type than the shape");
+}
+tr_pages pool(PyObject* o)
+{
+    tr_pages p;
+    read_buffer(o, &p, sizeof p);
+    return p;
+}
+
+PyObject* page_map(Args a) // cached_lens, new_lens, first_pos, page_size, free_pages, block_table, kv_lens, cu_new, slots, pos, counts, stream
+{
+    Place at;
+    int64_t n, n_free, n_slots;
+    const int32_t *cached = at.ints(a[0], &n), *fresh = at.ints_of(a[1], n), *first = a[2] == Py_None ? nullptr : at.ints_of(a[2], n);
+    const int32_t page = int32(a[3]), *free_pages = at.ints(a[4], &n_free);
+    int32_t* table = at.ints(a[5]);
+    const at::Tensor& t = tensor(a[5]);
+    if (t.dim() != 2 || t.size(0) != n) fail(PyExc_AssertionError, "block_table is [requests, blocks]");
+    const int32_t blocks = small(t.size(1)), req = small(n), n_free_ = small(n_free);
+    int32_t *lens = at.ints_of(a[6], n), *cu = at.ints_of(a[7], n + 1), *slots = at.ints(a[8], &n_slots), *pos = at.ints_of(a[9], n_slots);
+    int32_t *counts = at.ints_of(a[10], 2), n_slots_ = small(n_slots);
+    void* s = at.stream_of(a[11]);
+    return run([&] { return api.tr_page_map(cached, fresh, first, req, page, free_pages, n_free_, table, blocks, lens, cu, slots, pos, n_slots_, counts, s); });
+}
+
+PyObject* paged_append(Args a) // shape, rotary, q, k, v, q_norm, k_norm, eps, pos, slots, q_out, pages, stream
+{
+    const tr_shape sh = shape(a[0]);
+    tr_rotary rot;
+    if (a[1] != Py_None) read_buffer(a[1], &rot, sizeof rot);
+    Place at;
+    int64_t n = -1;
+    struct Rows { void* p = nullptr; int64_t stride = 0; };
+    auto heads = [&](PyObject* o, int count) { // [tokens, heads, head_dim], the heads of a token side by side
+        Rows r;
+        if (o == Py_None) return r;
+        const at::Tensor& t = at.on(o, false);
+        has_type(t, sh);
+        if (t.dim() != 3 || t.size(1) != count || t.size(2) != sh.head_dim) fail(PyExc_AssertionError, "[tokens, heads, head_dim] is expected");
+        if (n >= 0 && t.size(0) != n) fail(PyExc_AssertionError, "tensors of different numbers of tokens");
+        n = t.size(0);
+        if (n > 0 && (t.stride(2) != 1 || (count > 1 && t.stride(1) != sh.head_dim))) fail(PyExc_AssertionError, "the heads of a token must be contiguous");
+        r.p = t.data_ptr();
+        r.stride = n > 1 ? t.stride(0) : (int64_t)count * sh.head_dim;
+        return r;
+    };
+    const Rows q = heads(a[2], sh.n_q_heads), k = heads(a[3], sh.n_kv_heads), v = heads(a[4], sh.n_kv_heads), out = heads(a[10], sh.n_q_heads);
+    if (n < 0) n = 0;
+    if (a[10] != Py_None && out.stride != (int64_t)sh.n_q_heads * sh.head_dim) fail(PyExc_AssertionError, "q_out must be contiguous");
+    auto weight = [&](PyObject* o) -> const void* {
+        if (o == Py_None) return nullptr;
+        const at::Tensor& t = at.on(o);
+        has_type(t, sh);
+        if (t.numel() != sh.head_dim) fail(PyExc_AssertionError, "a norm's weight has head_dim entries");
+        return t.data_ptr();
+    };
+    const void *qw = weight(a[5]), *kw = weight(a[6]);
+    const double eps = PyFloat_AsDouble(a[7]);
+    if (eps == -1.0 && PyErr_Occurred()) throw Failed();
+    const int32_t* pos = a[8] == Py_None ? nullptr : at.ints_of(a[8], n);
+    const int32_t* slots = a[9] == Py_None ? nullptr : at.ints_of(a[9], n);
+    tr_pages pg;
+    if (a[11] != Py_None) pg = pool(a[11]);
+    const int32_t tokens = small(n);
+    void* s = at.stream_of(a[12]);
+    return run([&] {
+        return api.tr_paged_append(&sh, a[1] == Py_None ? nullptr : &rot, q.p, q.stride, k.p, k.stride, v.p, v.stride, qw, kw, eps, pos, slots, tokens,
+                                   out.p, a[11] == Py_None ? nullptr : &pg, s);
+    });
+}
+
+PyObject* paged_decode(Args a) // shape, q, pages, block_table, kv_lens, window, n_sink, out, workspace, stream
+{
+    const tr_shape sh = shape(a[0]);
+    Place at;
+    const at::Tensor &q = at.on(a[1]), &out = at.on(a[7]);
+    has_type(q, sh);
+    has_type(out, sh);
+    const tr_pages pg = pool(a[2]);
+    int32_t* table = at.ints(a[3]);
+    const at::Tensor& t = tensor(a[3]);
+    int64_t n;
+    const int32_t* lens = at.ints(a[4], &n);
+    if (t.dim() != 2 || t.size(0) != n) fail(PyExc_AssertionError, "block_table is [requests, blocks]");
+    const int64_t row = (int64_t)sh.n_q_heads * sh.head_dim;
+    if (q.numel() != n * row || out.numel() != n * row) fail(PyExc_AssertionError, "q and out are [requests, heads, head_dim]");
+    const int32_t req = small(n), blocks = small(t.size(1)), window = int32(a[5]), sinks = int32(a[6]);
+    const void* qp = q.data_ptr();
+    void* op = out.data_ptr();
+    if (a[8] != Py_None) at.on(a[8]);
+    const Work w(a[8]);
+    void* s = at.stream_of(a[9]);
+    return run([&] { return api.tr_paged_decode_attn(&sh, qp, &pg, table, blocks, lens, req, window, sinks, op, w.p, w.bytes, s); });
+}
+
 // addresses: dict name -> address of the library's entry point; error: the exception class for a failed call
 PyObject* bind(PyObject*, PyObject* args)
 {
@@ -455,6 +602,9 @@ PyMethodDef methods[] = {
     ENTRY("chunk_prefill_attn", 11, chunk_prefill),
     ENTRY("sequence_prefill_attn", 11, sequence_prefill),
     ENTRY("linear", 5, linear),
+    ENTRY("page_map", 12, page_map),
+    ENTRY("paged_append", 13, paged_append),
+    ENTRY("paged_decode_attn", 10, paged_decode),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tr_host", "argument marshalling for binding.py", -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -64,26 +64,6 @@ extern "C" int tr_probe_mfma_loop(int32_t iters, int32_t random_operands, float*
 
 extern "C" size_t tr_probe_mfma_loop_sink_bytes(void) { return (size_t)TrChip::CUS * 512 * sizeof(float); }
 
-// No C++ exception may cross the C boundary: the entry points run inside these.
-template <class F> static int tr_guard_int(F&& f)
-{
-    try {
-        return f();
-    } catch (const std::bad_alloc&) {
-        return tr_fail(TR_ERR_NO_MEMORY, "out of host memory");
-    } catch (...) {
-        return tr_fail(TR_ERR_INVALID_ARG, "unexpected C++ exception");
-    }
-}
-template <class F> static size_t tr_guard_size(F&& f)
-{
-    try {
-        return f();
-    } catch (...) {
-        return 0;
-    }
-}
-
 int tr_check_shape(const tr_shape* s)
 {
     if (!s) return tr_fail(TR_ERR_INVALID_ARG, "shape is NULL");

@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <atomic>
+#include <new>
 #include <stdint.h>
 #include <stddef.h>
 #include <vector>
@@ -30,6 +31,26 @@ static inline int tr_raise_lds_limit(const void* kernel, int bytes, std::atomic<
         done->fetch_or(bit, std::memory_order_release);
     }
     return TR_OK;
+}
+
+// No C++ exception may cross the C boundary: the entry points run inside these.
+template <class F> static int tr_guard_int(F&& f)
+{
+    try {
+        return f();
+    } catch (const std::bad_alloc&) {
+        return tr_fail(TR_ERR_NO_MEMORY, "out of host memory");
+    } catch (...) {
+        return tr_fail(TR_ERR_INVALID_ARG, "unexpected C++ exception");
+    }
+}
+template <class F> static size_t tr_guard_size(F&& f)
+{
+    try {
+        return f();
+    } catch (...) {
+        return 0;
+    }
 }
 
 int tr_check_shape(const tr_shape* s);
@@ -362,3 +383,58 @@ extern "C" int tr_linear_direct_tile(int32_t M, int32_t N, int32_t K);
 int tr_launch_mfma_loop_probe(int iters, int random_operands, float* sink, hipStream_t s, double* flops);
 int tr_launch_linear(const void* x, int32_t n_out, const void* const* w, void* const* y, const int32_t* n_features, void* partial,
                      int32_t M, int32_t K, hipStream_t s);
+
+// ---- a cache in pages (tr_paged_api.hip, tr_paged.hip) ---------------------------------------------------------------------
+#define TR_MAX_MAP_REQ 4096 // what the prefix sums of tr_page_map have room for in LDS
+#define TR_MAP_TOKENS 1024  // slots per workgroup
+struct TrPageMapArgs {
+    const int32_t* cached;
+    const int32_t* fresh;
+    const int32_t* first_pos; // or NULL
+    const int32_t* free_pages;
+    int32_t* table;
+    int32_t* kv_lens;
+    int32_t* cu;
+    int32_t* slots;
+    int32_t* pos;
+    int32_t* counts;
+    int32_t n_req, n_free, max_blocks, n_slots, page_shift, pad_;
+};
+
+// The pool as the kernels address it: strides in bytes.
+struct TrPool {
+    char* k;
+    char* v;
+    int64_t page_stride, row_stride, head_stride;
+    int32_t n_pages, page_shift;
+};
+struct TrPagedAppendArgs {
+    const char* q;
+    const char* k;
+    const char* v;
+    char* q_out;
+    const void* q_norm;
+    const void* k_norm;
+    const int32_t* pos;
+    const int32_t* slots;
+    int64_t q_stride, k_stride, v_stride; // bytes
+    TrPool pool;
+    int32_t n_tokens;
+    int32_t n_q_heads, n_kv_heads; // 0 where the side is absent
+    int32_t rotary_dim;
+    float eps, amplitude;
+    double freq[64];
+};
+struct TrPagedDecodeArgs {
+    const void* q;
+    void* out;
+    const int32_t* table;
+    const int32_t* kv_lens;
+    TrPool pool;
+    int32_t n_req, max_blocks, window, n_sink;
+    int32_t n_q_heads, n_kv_heads, group;
+    float scale_log2e; // log2(e) / sqrt(head_dim)
+};
+int tr_launch_page_map(const TrPageMapArgs& a, hipStream_t s);
+int tr_launch_paged_append(const TrPagedAppendArgs& a, int dtype, int head_dim, int layout, hipStream_t s);
+int tr_launch_paged_decode(const TrPagedDecodeArgs& a, int dtype, int head_dim, hipStream_t s);

@@ -1,0 +1,262 @@
+// Host side of the paged cache: argument validation and launch geometry.  No kernels here.
+#include "tr_internal.h"
+
+#include <float.h>
+#include <math.h>
+#include <string.h>
+
+namespace {
+
+const int64_t INT_LIMIT = ((int64_t)1 << 31) - 1;
+
+int page_shift(int32_t page_size)
+{
+    if (page_size < 8 || page_size > 1024 || (page_size & (page_size - 1)) != 0) return -1;
+    return __builtin_ctz((unsigned)page_size);
+}
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Checks the pool against the shape and gives the form that the kernels address.
+int pool_of(const char* who, const tr_shape* sh, const tr_pages* p, TrPool* out)
+{
+    if (p->reserved != 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: reserved of tr_pages must be 0", who);
+    if (p->dtype != sh->dtype || p->n_kv_heads != sh->n_kv_heads || p->head_dim != sh->head_dim)
+        return tr_fail(TR_ERR_SHAPE, "%s: pages of type %d with %d heads of %d channels, the shape has type %d, %d heads, %d channels", who, p->dtype,
+                       p->n_kv_heads, p->head_dim, sh->dtype, sh->n_kv_heads, sh->head_dim);
+    const int shift = page_shift(p->page_size);
+    if (shift < 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: page_size %d is not a power of two from 8 to 1024", who, p->page_size);
+    if (p->n_pages < 1 || (int64_t)p->n_pages * p->page_size > INT_LIMIT) return tr_fail(TR_ERR_INVALID_ARG, "%s: n_pages %d", who, p->n_pages);
+    if (!p->k || !p->v) return tr_fail(TR_ERR_INVALID_ARG, "%s: k or v of the pages is NULL", who);
+    const int64_t e = tr_elem_bytes(sh), widest = (int64_t)64 << 20;
+    // a stride of a single page or head is never applied; the others have to keep rows apart
+    if (p->row_stride < sh->head_dim || (p->n_kv_heads > 1 && p->head_stride < sh->head_dim) || (p->n_pages > 1 && p->page_stride < sh->head_dim))
+        return tr_fail(TR_ERR_INVALID_ARG, "%s: strides of the pages are smaller than a head", who);
+    if (p->head_stride < 0 || p->page_stride < 0 || p->page_stride > INT64_MAX / 4 / p->n_pages / e)
+        return tr_fail(TR_ERR_INVALID_ARG, "%s: strides of the pages are out of range", who);
+    if (p->row_stride > widest / e || p->head_stride > widest / e)
+        return tr_fail(TR_ERR_UNSUPPORTED, "%s: rows or heads of the pages are more than 64 MiB apart", who);
+    if (!aligned16(p->k) || !aligned16(p->v) || p->page_stride * e % 16 || p->row_stride * e % 16 || p->head_stride * e % 16)
+        return tr_fail(TR_ERR_INVALID_ARG, "%s: pages and their strides must be 16-byte aligned", who);
+    out->k = (char*)p->k;
+    out->v = (char*)p->v;
+    out->page_stride = p->page_stride * e;
+    out->row_stride = p->row_stride * e;
+    out->head_stride = p->head_stride * e;
+    out->n_pages = p->n_pages;
+    out->page_shift = shift;
+    return TR_OK;
+}
+
+struct Span {
+    const void* p;
+    int64_t bytes;
+};
+bool overlap(const Span& a, const Span& b)
+{
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return a.bytes > 0 && b.bytes > 0 && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
+}
+Span ints(const int32_t* p, int64_t n) { return {p, p ? 4 * n : 0}; }
+// n rows of `row` bytes, a stride apart
+Span rows(const void* p, int64_t n, int64_t stride, int64_t row) { return {p, p ? (n - 1) * stride + row : 0}; }
+
+} // namespace
+
+extern "C" int tr_page_map(const int32_t* cached_lens, const int32_t* new_lens, const int32_t* first_pos, int32_t n_req, int32_t page_size,
+                           const int32_t* free_pages, int32_t n_free, int32_t* block_table, int32_t max_blocks, int32_t* kv_lens,
+                           int32_t* cu_new, int32_t* slots, int32_t* pos, int32_t n_slots, int32_t* counts, void* stream)
+{
+    return tr_guard_int([&]() -> int {
+    tr_clear_error();
+    if (n_req < 0 || n_free < 0 || max_blocks < 0 || n_slots < 0) return tr_fail(TR_ERR_INVALID_ARG, "tr_page_map: a count is negative");
+    if (n_req > TR_MAX_MAP_REQ) return tr_fail(TR_ERR_UNSUPPORTED, "tr_page_map: %d requests, at most %d", n_req, TR_MAX_MAP_REQ);
+    const int shift = page_shift(page_size);
+    if (shift < 0) return tr_fail(TR_ERR_INVALID_ARG, "tr_page_map: page_size %d is not a power of two from 8 to 1024", page_size);
+    if (!cu_new || !counts || (n_req > 0 && (!cached_lens || !new_lens || !kv_lens)) || (n_slots > 0 && (!slots || !pos)) ||
+        (n_free > 0 && !free_pages) || (n_req > 0 && max_blocks > 0 && !block_table))
+        return tr_fail(TR_ERR_INVALID_ARG, "tr_page_map: an array is NULL");
+    const Span in[] = {ints(cached_lens, n_req), ints(new_lens, n_req), ints(first_pos, n_req), ints(free_pages, n_free)};
+    const Span out[] = {ints(block_table, (int64_t)n_req * max_blocks), ints(kv_lens, n_req), ints(cu_new, (int64_t)n_req + 1),
+                        ints(slots, n_slots), ints(pos, n_slots), ints(counts, 2)};
+    for (int i = 0; i < 6; ++i) {
+        for (const Span& s : in)
+            if (overlap(out[i], s)) return tr_fail(TR_ERR_INVALID_ARG, "tr_page_map: an output overlaps an input");
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return tr_fail(TR_ERR_INVALID_ARG, "tr_page_map: two outputs overlap");
+    }
+    TrPageMapArgs a;
+    memset(&a, 0, sizeof a);
+    a.cached = cached_lens;
+    a.fresh = new_lens;
+    a.first_pos = first_pos;
+    a.free_pages = free_pages;
+    a.table = block_table;
+    a.kv_lens = kv_lens;
+    a.cu = cu_new;
+    a.slots = slots;
+    a.pos = pos;
+    a.counts = counts;
+    a.n_req = n_req;
+    a.n_free = n_free;
+    a.max_blocks = max_blocks;
+    a.n_slots = n_slots;
+    a.page_shift = shift;
+    return tr_launch_page_map(a, (hipStream_t)stream);
+    });
+}
+
+extern "C" int tr_rotary_init(int32_t layout, int32_t rotary_dim, double base, int32_t scaling, double factor, double original_len,
+                              double slow_turns, double fast_turns, double amplitude, tr_rotary* out)
+{
+    return tr_guard_int([&]() -> int {
+    tr_clear_error();
+    if (!out) return tr_fail(TR_ERR_INVALID_ARG, "tr_rotary_init: out is NULL");
+    if (layout != TR_ROPE_INTERLEAVED && layout != TR_ROPE_HALF) return tr_fail(TR_ERR_INVALID_ARG, "tr_rotary_init: layout %d", layout);
+    if (rotary_dim < 0 || rotary_dim > 128 || rotary_dim % 16) return tr_fail(TR_ERR_SHAPE, "tr_rotary_init: rotary_dim %d is not a multiple of 16 up to 128", rotary_dim);
+    if (!(base > 1.0) || !isfinite(base)) return tr_fail(TR_ERR_INVALID_ARG, "tr_rotary_init: base must be finite and > 1");
+    if (scaling < TR_SCALE_NONE || scaling > TR_SCALE_PARTS) return tr_fail(TR_ERR_INVALID_ARG, "tr_rotary_init: scaling %d", scaling);
+    if (scaling != TR_SCALE_NONE && (!(factor >= 1.0) || !isfinite(factor))) return tr_fail(TR_ERR_INVALID_ARG, "tr_rotary_init: factor must be finite and >= 1");
+    if (!isfinite((float)amplitude)) return tr_fail(TR_ERR_INVALID_ARG, "tr_rotary_init: amplitude must be finite");
+    if (scaling == TR_SCALE_PARTS && (!(original_len > 0.0) || !isfinite(original_len) || !(slow_turns < fast_turns) || !isfinite(slow_turns) || !isfinite(fast_turns)))
+        return tr_fail(TR_ERR_INVALID_ARG, "tr_rotary_init: original_len must be positive and slow_turns below fast_turns");
+    tr_rotary r;
+    memset(&r, 0, sizeof r);
+    r.layout = layout;
+    r.rotary_dim = rotary_dim;
+    r.amplitude = amplitude;
+    const double d = rotary_dim;
+    if (scaling == TR_SCALE_BASE && rotary_dim) base *= pow(factor, d / (d - 2.0));
+    if (!isfinite(base)) return tr_fail(TR_ERR_INVALID_ARG, "tr_rotary_init: the stretched base is not finite");
+    for (int m = 0; m < rotary_dim / 2; ++m) {
+        const double theta = pow(base, -2.0 * m / d);
+        double f = theta;
+        if (scaling == TR_SCALE_LINEAR) f = theta / factor;
+        if (scaling == TR_SCALE_PARTS) {
+            const double turns = original_len * theta / 6.283185307179586;
+            const double c = fmin(fmax((turns - slow_turns) / (fast_turns - slow_turns), 0.0), 1.0);
+            f = theta * (c + (1.0 - c) / factor);
+        }
+        r.freq[m] = f;
+    }
+    *out = r;
+    return TR_OK;
+    });
+}
+
+extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, const void* q_norm, const void* k_norm, double eps, const int32_t* pos,
+                               const int32_t* slots, int32_t n_tokens, void* q_out, const tr_pages* pages, void* stream)
+{
+    return tr_guard_int([&]() -> int {
+    tr_clear_error();
+    const char* const who = "tr_paged_append";
+    if (int rc = tr_check_shape(shape)) return rc;
+    if (n_tokens < 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: n_tokens < 0", who);
+    if ((q != nullptr) != (q_out != nullptr)) return tr_fail(TR_ERR_INVALID_ARG, "%s: q and q_out go together", who);
+    const int given = (k != nullptr) + (v != nullptr) + (slots != nullptr) + (pages != nullptr);
+    if (n_tokens > 0 && given != 0 && given != 4) return tr_fail(TR_ERR_INVALID_ARG, "%s: k, v, slots and pages go together", who);
+    if (!((float)eps >= FLT_MIN) || !isfinite((float)eps)) return tr_fail(TR_ERR_INVALID_ARG, "%s: eps must be finite and a positive normal fp32 value", who);
+    TrPagedAppendArgs a;
+    memset(&a, 0, sizeof a);
+    int layout = shape->rope_layout;
+    if (rotary) {
+        layout = rotary->layout;
+        if (layout != TR_ROPE_INTERLEAVED && layout != TR_ROPE_HALF) return tr_fail(TR_ERR_INVALID_ARG, "%s: layout %d of the rotary", who, layout);
+        a.rotary_dim = rotary->rotary_dim;
+        if (a.rotary_dim < 0 || a.rotary_dim > shape->head_dim || a.rotary_dim % 16)
+            return tr_fail(TR_ERR_SHAPE, "%s: rotary_dim %d is not a multiple of 16 up to head_dim", who, a.rotary_dim);
+        if (!isfinite((float)rotary->amplitude)) return tr_fail(TR_ERR_INVALID_ARG, "%s: amplitude must be finite", who);
+        a.amplitude = (float)rotary->amplitude;
+        for (int m = 0; m < a.rotary_dim / 2; ++m) {
+            if (!(rotary->freq[m] >= 0.0 && rotary->freq[m] <= 1.0)) return tr_fail(TR_ERR_INVALID_ARG, "%s: freq[%d] is outside [0, 1]", who, m);
+            a.freq[m] = rotary->freq[m];
+        }
+    } else {
+        a.rotary_dim = shape->head_dim;
+        a.amplitude = 1.0f;
+        tr_fill_theta(shape, a.freq);
+    }
+    const int64_t e = tr_elem_bytes(shape), q_row = (int64_t)shape->n_q_heads * shape->head_dim, kv_row = (int64_t)shape->n_kv_heads * shape->head_dim;
+    if (pages) {
+        if (int rc = pool_of(who, shape, pages, &a.pool)) return rc;
+    }
+    if (n_tokens == 0 || (!q && !k)) return TR_OK;
+    if (a.rotary_dim && !pos) return tr_fail(TR_ERR_INVALID_ARG, "%s: pos is NULL", who);
+    // tokens may share a row of the input (a stride of 0), they may not overlap in part
+    if ((q && (q_stride < 0 || q_stride > INT64_MAX / 8 / n_tokens)) || (k && (k_stride < 0 || k_stride > INT64_MAX / 8 / n_tokens || v_stride < 0 || v_stride > INT64_MAX / 8 / n_tokens)))
+        return tr_fail(TR_ERR_INVALID_ARG, "%s: a stride is out of range", who);
+    const Span qs = rows(q, n_tokens, q_stride * e, q_row * e), ks = rows(k, n_tokens, k_stride * e, kv_row * e), vs = rows(v, n_tokens, v_stride * e, kv_row * e);
+    const Span outs = rows(q_out, n_tokens, q_row * e, q_row * e);
+    if ((overlap(outs, qs) && !(q == q_out && (n_tokens == 1 || q_stride == q_row))) || overlap(outs, ks) || overlap(outs, vs))
+        return tr_fail(TR_ERR_INVALID_ARG, "%s: q_out overlaps an input (it may be a contiguous q itself)", who);
+    if (pages) {
+        const int64_t pool = (int64_t)(a.pool.n_pages - 1) * a.pool.page_stride + (pages->page_size - 1) * a.pool.row_stride +
+                             (pages->n_kv_heads - 1) * a.pool.head_stride + shape->head_dim * e;
+        for (const Span& s : {Span{pages->k, pool}, Span{pages->v, pool}})
+            if (overlap(s, qs) || overlap(s, ks) || overlap(s, vs) || overlap(s, outs))
+                return tr_fail(TR_ERR_INVALID_ARG, "%s: the pages overlap another tensor of the call", who);
+    }
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(q_norm) || !aligned16(k_norm) || (q && q_stride * e % 16) ||
+        (k && (k_stride * e % 16 || v_stride * e % 16)))
+        return tr_fail(TR_ERR_INVALID_ARG, "%s: tensors and their strides must be 16-byte aligned", who);
+    a.q = (const char*)q;
+    a.k = (const char*)k;
+    a.v = (const char*)v;
+    a.q_out = (char*)q_out;
+    a.q_norm = q_norm;
+    a.k_norm = k_norm;
+    a.pos = pos;
+    a.slots = slots;
+    a.q_stride = q_stride * e;
+    a.k_stride = k_stride * e;
+    a.v_stride = v_stride * e;
+    a.n_tokens = n_tokens;
+    a.n_q_heads = q ? shape->n_q_heads : 0;
+    a.n_kv_heads = k ? shape->n_kv_heads : 0;
+    a.eps = (float)eps;
+    return tr_launch_paged_append(a, shape->dtype, shape->head_dim, layout, (hipStream_t)stream);
+    });
+}
+
+extern "C" size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size)
+{
+    return tr_guard_size([&]() -> size_t {
+    tr_clear_error();
+    if (tr_check_shape(shape) || n_req < 1 || max_blocks < 1 || page_shift(page_size) < 0) return 0;
+    return 0;
+    });
+}
+
+extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const tr_pages* pages, const int32_t* block_table, int32_t max_blocks,
+                                    const int32_t* kv_lens, int32_t n_req, int32_t window, int32_t n_sink, void* out, void* workspace,
+                                    size_t workspace_bytes, void* stream)
+{
+    return tr_guard_int([&]() -> int {
+    tr_clear_error();
+    const char* const who = "tr_paged_decode_attn";
+    if (int rc = tr_check_shape(shape)) return rc;
+    if (n_req < 0 || max_blocks < 0 || window < 0 || n_sink < 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: a count is negative", who);
+    if (n_req > 65536) return tr_fail(TR_ERR_UNSUPPORTED, "%s: %d requests, at most 65536", who, n_req);
+    if (!pages) return tr_fail(TR_ERR_INVALID_ARG, "%s: pages is NULL", who);
+    TrPagedDecodeArgs a;
+    memset(&a, 0, sizeof a);
+    if (int rc = pool_of(who, shape, pages, &a.pool)) return rc;
+    if ((int64_t)max_blocks * pages->page_size > INT_LIMIT) return tr_fail(TR_ERR_INVALID_ARG, "%s: max_blocks %d", who, max_blocks);
+    if (n_req == 0) return TR_OK;
+    if (!q || !out || !kv_lens || (max_blocks > 0 && !block_table)) return tr_fail(TR_ERR_INVALID_ARG, "%s: an array is NULL", who);
+    if (!aligned16(q) || !aligned16(out)) return tr_fail(TR_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned", who);
+    a.q = q;
+    a.out = out;
+    a.table = block_table;
+    a.kv_lens = kv_lens;
+    a.n_req = n_req;
+    a.max_blocks = max_blocks;
+    a.window = window;
+    a.n_sink = n_sink;
+    a.n_q_heads = shape->n_q_heads;
+    a.n_kv_heads = shape->n_kv_heads;
+    a.group = shape->n_q_heads / shape->n_kv_heads;
+    a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)shape->head_dim));
+    return tr_launch_paged_decode(a, shape->dtype, shape->head_dim, (hipStream_t)stream);
+    });
+}
