@@ -20,23 +20,17 @@
 // Softmax works in the log2 domain with a lazily updated reference maximum: the accumulators are rescaled
 // only when the running maximum grew by more than 2^8, which is exact (softmax is invariant to the reference)
 // and keeps P <= 256.
+#include "tr_device.h"
 #include "tr_internal.h"
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-
-#define LDS_AS __attribute__((address_space(3)))
-#define GLB_AS __attribute__((address_space(1)))
 
 constexpr int KT = 64;               // keys per tile
 constexpr float RESCALE_SLACK = 8.f; // log2 units a tile maximum may exceed the reference before a rescale
@@ -55,19 +49,6 @@ template <int D> struct Geo {
     // V: 64-byte group q of row r sits at group q ^ vswz(r): 4 consecutive rows of one group cover all banks
     __device__ static __forceinline__ int vswz(int r) { return (r / (4 / GPR)) & (GPR - 1); }
 };
-
-// s_waitcnt immediate that waits for vmcnt <= n only (gfx9 encoding: vmcnt in bits 3:0 and 15:14)
-constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
-template <int N> __device__ __forceinline__ void wait_vm() { __builtin_amdgcn_s_waitcnt(vmcnt_imm(N)); }
-
-// Waits until this wave's LDS reads have delivered: what they read may be overwritten behind it.
-__device__ __forceinline__ void wait_lds()
-{
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0xC07F); // lgkmcnt(0)
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
 
 struct RowCtx {
     bool valid;

@@ -425,6 +425,11 @@ struct TrPagedAppendArgs {
     float eps, amplitude;
     double freq[64];
 };
+// Decode: each of TR_PAGED_WORKERS workgroups takes an equal share of the batch's steps, of at least TR_PAGED_MIN_STEPS.
+#define TR_PAGED_STEP_KEYS 128
+#define TR_PAGED_WORKERS 512
+#define TR_PAGED_MIN_STEPS 2
+static inline int tr_paged_tile_rows(int group) { return group <= 16 ? 16 : 32; }
 struct TrPagedDecodeArgs {
     const void* q;
     void* out;
@@ -434,7 +439,15 @@ struct TrPagedDecodeArgs {
     int32_t n_req, max_blocks, window, n_sink;
     int32_t n_q_heads, n_kv_heads, group;
     float scale_log2e; // log2(e) / sqrt(head_dim)
+    int32_t workers;   // shares; not the number of workgroups, which may be fewer where the table bounds the work
+    int32_t cut;       // items may be cut: a second launch joins their pieces
+    int32_t ws_rows;   // rows of a piece
+    int32_t pad_;
+    float* ws_o;       // [2 workers][ws_rows][head_dim] sums of a piece: 2 w of the item that worker w continues, 2 w + 1 of the one it begins
+    float* ws_ml;      // [2 workers][ws_rows][2] reference maximum (log2 domain) and denominator
+    int32_t* ws_items; // [items][2] worker that begins an item, number of its pieces
 };
 int tr_launch_page_map(const TrPageMapArgs& a, hipStream_t s);
 int tr_launch_paged_append(const TrPagedAppendArgs& a, int dtype, int head_dim, int layout, hipStream_t s);
-int tr_launch_paged_decode(const TrPagedDecodeArgs& a, int dtype, int head_dim, hipStream_t s);
+int tr_launch_paged_decode_f32(const TrPagedDecodeArgs& a, int head_dim, hipStream_t s);
+int tr_launch_paged_decode_bf16(const TrPagedDecodeArgs& a, int head_dim, int grid, hipStream_t s);

@@ -325,11 +325,10 @@ int tr_launch_paged_append(const TrPagedAppendArgs& a, int dtype, int head_dim, 
     return TR_OK;
 }
 
-int tr_launch_paged_decode(const TrPagedDecodeArgs& a, int dtype, int head_dim, hipStream_t s)
+int tr_launch_paged_decode_f32(const TrPagedDecodeArgs& a, int head_dim, hipStream_t s)
 {
     const dim3 grid(a.n_req * a.n_q_heads), block(256);
-    if (dtype == TR_BF16) head_dim == 128 ? paged_decode_kernel<TR_BF16, 128><<<grid, block, 0, s>>>(a) : paged_decode_kernel<TR_BF16, 64><<<grid, block, 0, s>>>(a);
-    else head_dim == 128 ? paged_decode_kernel<TR_F32, 128><<<grid, block, 0, s>>>(a) : paged_decode_kernel<TR_F32, 64><<<grid, block, 0, s>>>(a);
+    head_dim == 128 ? paged_decode_kernel<TR_F32, 128><<<grid, block, 0, s>>>(a) : paged_decode_kernel<TR_F32, 64><<<grid, block, 0, s>>>(a);
     TR_HIP(hipGetLastError());
     return TR_OK;
 }

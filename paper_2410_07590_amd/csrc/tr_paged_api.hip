@@ -4,6 +4,7 @@
 #include <float.h>
 #include <math.h>
 #include <string.h>
+#include <algorithm>
 
 namespace {
 
@@ -218,12 +219,36 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     });
 }
 
+namespace {
+// What the pieces of cut items need: sums and statistics of two pieces per worker, and who has pieces of which item.  None of it
+// depends on the lengths, which are not known here.
+struct DecodePlan {
+    int64_t items, bound; // items of the batch; most steps that they can have
+    int32_t ws_rows;
+    size_t ml_at, items_at, bytes;
+};
+DecodePlan decode_plan(const tr_shape* sh, int64_t n_req, int64_t keys)
+{
+    DecodePlan p;
+    const int group = sh->n_q_heads / sh->n_kv_heads, tile = tr_paged_tile_rows(group);
+    p.items = n_req * sh->n_kv_heads * ((group + tile - 1) / tile);
+    const int64_t steps = std::max<int64_t>((keys + TR_PAGED_STEP_KEYS - 1) / TR_PAGED_STEP_KEYS, 1);
+    p.bound = p.items * steps;
+    p.ws_rows = std::min(group, tile);
+    const bool none = sh->dtype == TR_F32 || steps == 1; // a step is never cut
+    p.ml_at = tr_align256(2ull * TR_PAGED_WORKERS * p.ws_rows * sh->head_dim * 4);
+    p.items_at = p.ml_at + tr_align256(2ull * TR_PAGED_WORKERS * p.ws_rows * 8);
+    p.bytes = none ? 0 : p.items_at + tr_align256((size_t)p.items * 8);
+    return p;
+}
+} // namespace
+
 extern "C" size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size)
 {
     return tr_guard_size([&]() -> size_t {
     tr_clear_error();
     if (tr_check_shape(shape) || n_req < 1 || max_blocks < 1 || page_shift(page_size) < 0) return 0;
-    return 0;
+    return decode_plan(shape, n_req, (int64_t)max_blocks * page_size).bytes;
     });
 }
 
@@ -241,7 +266,8 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     TrPagedDecodeArgs a;
     memset(&a, 0, sizeof a);
     if (int rc = pool_of(who, shape, pages, &a.pool)) return rc;
-    if ((int64_t)max_blocks * pages->page_size > INT_LIMIT) return tr_fail(TR_ERR_INVALID_ARG, "%s: max_blocks %d", who, max_blocks);
+    if ((int64_t)max_blocks * pages->page_size > ((int64_t)1 << 30)) return tr_fail(TR_ERR_INVALID_ARG, "%s: max_blocks %d", who, max_blocks);
+    if ((int64_t)n_req * shape->n_q_heads > TR_MAX_BLOCKS_256) return tr_fail(TR_ERR_UNSUPPORTED, "%s: more than 2^24 (request, head) pairs", who);
     if (n_req == 0) return TR_OK;
     if (!q || !out || !kv_lens || (max_blocks > 0 && !block_table)) return tr_fail(TR_ERR_INVALID_ARG, "%s: an array is NULL", who);
     if (!aligned16(q) || !aligned16(out)) return tr_fail(TR_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned", who);
@@ -257,6 +283,19 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     a.n_kv_heads = shape->n_kv_heads;
     a.group = shape->n_q_heads / shape->n_kv_heads;
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)shape->head_dim));
-    return tr_launch_paged_decode(a, shape->dtype, shape->head_dim, (hipStream_t)stream);
+    if (shape->dtype == TR_F32) return tr_launch_paged_decode_f32(a, shape->head_dim, (hipStream_t)stream);
+    const DecodePlan plan = decode_plan(shape, n_req, (int64_t)max_blocks * pages->page_size);
+    if (plan.bytes) {
+        if (!workspace || ((uintptr_t)workspace & 255)) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace missing or not 256-byte aligned", who);
+        if (workspace_bytes < plan.bytes) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace holds %zu bytes, %zu needed", who, workspace_bytes, plan.bytes);
+        a.ws_o = (float*)workspace;
+        a.ws_ml = (float*)((char*)workspace + plan.ml_at);
+        a.ws_items = (int32_t*)((char*)workspace + plan.items_at);
+    }
+    a.cut = plan.bytes != 0;
+    a.ws_rows = plan.ws_rows;
+    a.workers = TR_PAGED_WORKERS;
+    const int64_t workers = std::min<int64_t>((plan.bound + TR_PAGED_MIN_STEPS - 1) / TR_PAGED_MIN_STEPS, TR_PAGED_WORKERS);
+    return tr_launch_paged_decode_bf16(a, shape->head_dim, (int)workers, (hipStream_t)stream);
     });
 }

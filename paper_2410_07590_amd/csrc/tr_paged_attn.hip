@@ -1,0 +1,511 @@
+// bf16 decode attention over a paged cache: one new token per request, lengths and page ids known on the GPU only.
+//
+// Bound by the stream of keys and values (4 g flops per 4 bytes for g query heads to a KV head), so the design is about
+// keeping requests for memory on their way on every compute unit, whatever the lengths are:
+//
+// Work.  An item is a (request, KV head, block of at most 16 NT query heads).  Its visible keys are walked in steps of 128:
+// 32 for each of the four waves, which all hold the same queries and share the keys.  The host does not know the lengths, so the
+// launch is a fixed number of workers, each of which takes an equal share of all steps of the batch, in order of items: it works
+// out the batch's sum from kv_lens and finds its own range in it.  No share is longer than another by more than a step,
+// whatever the mix of lengths, and at most the first and the last item of a share are cut.  Pieces of cut items go to the
+// workspace and a second, small launch joins them.
+//
+// Products.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, keys and values as the A operands from LDS (V through
+// the transposing read), so that a lane owns one query column: its maximum and denominator are scalars, and its share of S^T
+// is, up to the order of the keys, its B operand of the second product.  The weights go into it as two bf16 parts, which
+// keeps 16 bits of them: the matrix unit is idle most of the time, and the result is as exact as fp32 weights would give.
+//
+// Data movement.  Each wave has room for one unit (32 rows) of K and of V and refills them as soon as their operands
+// are read, straight from memory to LDS, counted waits instead of barriers.  A page id is needed for every 8 rows at the most: a wave
+// keeps the ids of its next units in one register, a lane each, and takes them out as scalars.
+#include "tr_device.h"
+#include "tr_internal.h"
+
+#include <algorithm>
+
+namespace {
+
+constexpr int NW = 4, UNIT = 32, STEP = NW * UNIT; // waves, keys of a wave, keys of a step
+static_assert(STEP == TR_PAGED_STEP_KEYS, "");
+constexpr float SLACK = 8.0f;        // log2 units by which a score may exceed the reference before it moves
+constexpr float NOTHING = -3.0e38f;  // reference of a row that has seen no key
+constexpr int DMA_STREAM = 2;        // non-temporal: every key is read once
+constexpr int FLIGHT = 6;            // loads of 1 KB that a wave has on their way
+
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// a / b for numbers that nearly always fit 32 bits
+__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) { return ((a | b) >> 32) == 0 ? (uint64_t)((uint32_t)a / (uint32_t)b) : a / b; }
+
+// The keys of a request as units of 32: the first `su` hold the sinks, the others run from unit `lu` to the end.
+struct Walk {
+    int len, lo, sink, su, lu, units;
+    __device__ __forceinline__ int steps() const { return max((units + NW - 1) / NW, 1); } // at least one, which writes the result
+    __device__ __forceinline__ int unit(int i) const { return i < su ? i : i - su + lu; }
+    __device__ __forceinline__ uint32_t seen(int first_key) const // bit b: key first_key + b is visible
+    {
+        return low_bits(len - first_key) & (low_bits(sink - first_key) | ~low_bits(lo - first_key));
+    }
+};
+__device__ __forceinline__ Walk walk_of(const TrPagedDecodeArgs& a, int kv_len)
+{
+    Walk w;
+    w.len = min(max(kv_len, 0), a.max_blocks << a.pool.page_shift);
+    w.lo = a.window ? max(w.len - a.window, 0) : 0;
+    w.sink = min(a.n_sink, w.lo);
+    w.su = (w.sink + UNIT - 1) / UNIT;
+    w.lu = max(w.lo / UNIT, w.su);
+    w.units = w.su + max((w.len + UNIT - 1) / UNIT - w.lu, 0);
+    return w;
+}
+
+template <bool MAX> __device__ __forceinline__ float column_reduce(float x) // over the four lanes of a query column
+{
+    auto op = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+    uint32_t u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    u = __float_as_uint(x);
+    const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+
+// Where a wave's loads of a unit go and what its lanes add to them.  Load i fills rows RPI i .. of the unit, lane after lane;
+// K: 16-byte chunk c of row r sits at c ^ ksw(r), V: 32-byte group g of row r at g ^ vsw(r), so that the reads of operands
+// spread over all banks.
+template <int D> struct Rows {
+    static constexpr int CPR = D / 8, RPI = 64 / CPR, LPU = UNIT / RPI, BYTES = UNIT * D * 2;
+    __device__ static __forceinline__ int ksw(int r) { return (r / (16 / CPR)) & (CPR - 1); }
+    __device__ static __forceinline__ int vsw(int r) { return (r / (16 / CPR)) & (CPR / 2 - 1); }
+    __device__ static __forceinline__ int kchunk(int row, int lane) { return (lane % CPR) ^ ksw(row); }
+    __device__ static __forceinline__ int vchunk(int row, int lane) { return (((lane % CPR) >> 1) ^ vsw(row)) * 2 + (lane & 1); }
+};
+
+// One unit of a wave: its first key, which of its keys are seen, and where its page ids are among the wave's.
+struct UnitRef {
+    int key0, at;
+    uint32_t seen;
+};
+
+// What one wave accumulates: O^T (element e of block b is channel 16 b + 4 (lane / 16) + e of query column lane % 16), reference
+// maximum (log2 domain) and this lane's share of the denominator.
+template <int D, int NT> struct Acc {
+    f32x4 o[NT][D / 16];
+    float m[NT], l[NT];
+};
+
+// A wave's walk over its units of a piece.  A function of its own with restricted pointers, LDS by whole addresses: the
+// compiler otherwise takes the reads of LDS to depend on every load on its way to it.
+template <int D, int NT>
+__device__ __forceinline__ void walk_units(const char* __restrict__ k, const char* __restrict__ v, const int32_t* __restrict__ table, const TrPool& pool,
+                                           const Walk& w, const bf16x8 (&q)[NT][D / 32], int u0, int u1, float scale, int64_t head, uint32_t ring,
+                                           int wave, int lane, Acc<D, NT>& acc)
+{
+    using R = Rows<D>;
+    constexpr int LPU = R::LPU;
+    static_assert(FLIGHT <= 2 * LPU, "");
+    const int n_own = (u1 - u0 - wave + NW - 1) / NW;
+    if (n_own <= 0) return;
+    const int page = 1 << pool.page_shift;
+    const int sub_shift = min(pool.page_shift, 5), per_unit_shift = 5 - sub_shift; // rows of a page within a unit; pages of a unit
+    const int refill = 64 >> per_unit_shift;                                         // units whose ids a register holds
+    const int c16 = lane & 15, quad = lane >> 4;
+    const int row_bytes = (int)pool.row_stride;
+
+    auto fetch_ids = [&](int j0) {
+        const int j = j0 + (lane >> per_unit_shift), u = u0 + wave + NW * j;
+        const int key = w.unit(u) * UNIT + ((lane & ((1 << per_unit_shift) - 1)) << sub_shift);
+        int id = -1;
+        if (u < u1 && key < w.len) id = table[key >> pool.page_shift];
+        if ((uint32_t)id >= (uint32_t)pool.n_pages) id = -1;
+        asm volatile("" : "+v"(id)); // waited for here, once for many units, and not wherever an id is taken out
+        return id;
+    };
+    auto ref = [&](int j, uint64_t none) {
+        UnitRef u;
+        u.key0 = w.unit(u0 + wave + NW * j) * UNIT;
+        u.at = (j & (refill - 1)) << per_unit_shift;
+        u.seen = w.seen(u.key0);
+        uint32_t holes = (uint32_t)(none >> u.at) & low_bits(1 << per_unit_shift);
+        while (holes) { // pages that are none
+            const int s = __builtin_ctz(holes);
+            holes &= holes - 1;
+            u.seen &= ~(low_bits(1 << sub_shift) << (s << sub_shift));
+        }
+        return u;
+    };
+    // load i of a unit
+    const int r_in = lane / R::CPR;
+    auto load = [&](const char* base, const UnitRef& u, int ids, int i, uint32_t lds, bool is_v) {
+        const int row = i * R::RPI + r_in; // of the unit; says where the data lands
+        const int chunk = (is_v ? R::vchunk(row, lane) : R::kchunk(row, lane)) * 16;
+        const char* p;
+        if (u.seen == 0xffffffffu) { // the rows of a load lie in one page
+            const int id = __builtin_amdgcn_readlane(ids, u.at + ((i * R::RPI) >> sub_shift));
+            const char* at = base + (int64_t)id * pool.page_stride + (int64_t)((u.key0 + i * R::RPI) & (page - 1)) * pool.row_stride + head;
+            p = at + (uint32_t)(r_in * row_bytes + chunk);
+        } else { // rows that are not seen read one that is: what lies there may be anything
+            const int first = u.seen ? __builtin_ctz(u.seen) : 0;
+            const int src = (u.seen >> row) & 1 ? row : first;
+            const int id = max(__shfl(ids, u.at + (src >> sub_shift)), 0);
+            p = base + (int64_t)id * pool.page_stride + (int64_t)((u.key0 + src) & (page - 1)) * pool.row_stride + head + chunk;
+        }
+        __builtin_amdgcn_global_load_lds((const GLB_AS void*)p, (LDS_AS void*)(uintptr_t)(lds + i * 1024), 16, 0, DMA_STREAM);
+    };
+
+    const uint32_t kring = ring, vring = ring + R::BYTES;
+    int koff[D / 32], voff[D / 16];
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) koff[ks] = (int)kring + c16 * D * 2 + (((4 * ks + quad) ^ R::ksw(c16)) * 16);
+    const int vrow = 4 * quad + (c16 >> 2);
+#pragma unroll
+    for (int cb = 0; cb < D / 16; ++cb) voff[cb] = (int)vring + vrow * D * 2 + ((cb ^ R::vsw(vrow)) * 32) + (c16 & 3) * 8;
+    LDS_AS const char* lds = (LDS_AS const char*)(uintptr_t)0;
+
+    int ids = fetch_ids(0);
+    uint64_t none = __ballot(ids < 0);
+    UnitRef cur = ref(0, none);
+#pragma unroll
+    for (int i = 0; i < LPU; ++i) load(k, cur, ids, i, kring, false);
+#pragma unroll
+    for (int i = 0; i < LPU; ++i) load(v, cur, ids, i, vring, true);
+    for (int t = 0; t < n_own; ++t) {
+        const bool more = t + 1 < n_own;
+        UnitRef next = cur;
+        if (more) {
+            if (((t + 1) & (refill - 1)) == 0) {
+                ids = fetch_ids(t + 1);
+                none = __ballot(ids < 0);
+            }
+            next = ref(t + 1, none);
+        }
+        wait_vm<LPU>(); // K(t)
+        asm volatile("" ::: "memory");
+        f32x4 s[NT][2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) {
+                const bf16x8 a = *(LDS_AS const bf16x8*)(lds + koff[ks] + kb * 16 * D * 2);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    s[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[n][ks], ks == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[n][kb], 0, 0, 0);
+            }
+        }
+        wait_lds(); // the unit's keys are read
+        if (more) {
+#pragma unroll
+            for (int i = 0; i < LPU; ++i) {
+                if (i + LPU >= FLIGHT) wait_vm<FLIGHT - 1>();
+                load(k, next, ids, i, kring, false);
+            }
+        }
+        // element e of block kb is key 16 kb + 4 quad + e of the unit
+        if (cur.seen != 0xffffffffu) {
+            const uint32_t mine = cur.seen >> (4 * quad);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!(mine & (1u << (16 * kb + e)))) s[n][kb][e] = -INFINITY;
+        }
+        bf16x8 hi[NT], lo[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
+                              fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
+            top *= scale;
+            // the reference is exact wherever it is: it only has to stay near enough for the exponential's range
+            if (__any(top > acc.m[n] + SLACK)) {
+                const float to = fmaxf(acc.m[n], column_reduce<true>(top)), alpha = __builtin_amdgcn_exp2f(acc.m[n] - to);
+                acc.m[n] = to;
+                acc.l[n] *= alpha;
+#pragma unroll
+                for (int cb = 0; cb < D / 16; ++cb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc.o[n][cb][e] *= alpha;
+            }
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[n][i >> 2][i & 3], scale, -acc.m[n]));
+                sum += p;
+                hi[n][i] = (__bf16)p;
+                lo[n][i] = (__bf16)(p - (float)hi[n][i]);
+            }
+            acc.l[n] += sum;
+        }
+        if (more) wait_vm<LPU>(); // V(t)
+        else wait_vm<0>();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            if (cur.seen) {
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    const int cb = half * (D / 32) + c;
+                    LDS_AS const char* p0 = lds + voff[cb];
+                    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)p0);
+                    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(p0 + 16 * D * 2));
+                    const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, hi[n], acc.o[n][cb], 0, 0, 0);
+                        acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, lo[n], acc.o[n][cb], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        wait_lds(); // the unit's values are read
+        if (more) {
+#pragma unroll
+            for (int i = 0; i < LPU; ++i) {
+                if (i + LPU >= FLIGHT) wait_vm<FLIGHT - 1>();
+                load(v, next, ids, i, vring, true);
+            }
+        }
+        cur = next;
+    }
+}
+
+template <int D, int NT> constexpr int park_row_bytes() { return D * 4 + 16; }
+template <int D, int NT> constexpr int lds_bytes()
+{
+    const int ring = NW * 2 * Rows<D>::BYTES, park = NW * 16 * NT * park_row_bytes<D, NT>();
+    return (ring > park ? ring : park) + NW * 16 * NT * 8;
+}
+
+template <int D, int NT>
+__global__ __launch_bounds__(64 * NW, 2) void paged_decode_kernel(const TrPagedDecodeArgs a)
+{
+    constexpr int ROWS = 16 * NT, ROWB = park_row_bytes<D, NT>();
+    extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
+    LDS_AS char* smem = (LDS_AS char*)smem_raw;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c16 = lane & 15, quad = lane >> 4;
+    const int tiles = (a.group + ROWS - 1) / ROWS, per_req = a.n_kv_heads * tiles; // items of a request
+    const int worker = blockIdx.x;
+
+    // the batch's steps, and the request that this worker's share begins in
+    auto steps_of = [&](int r) { return r < a.n_req ? walk_of(a, a.kv_lens[r]).steps() : 0; };
+    uint64_t total = 0;
+    for (int r0 = 0; r0 < a.n_req; r0 += 64) {
+        int x = steps_of(r0 + lane);
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
+        total += (uint32_t)__builtin_amdgcn_readfirstlane(x);
+    }
+    total *= (uint32_t)per_req;
+    const uint64_t share = max((total + (uint32_t)(a.workers - 1)) / (uint32_t)a.workers, (uint64_t)TR_PAGED_MIN_STEPS);
+    const uint64_t begin = share * (uint32_t)worker;
+    if (begin >= total) return;
+    const uint64_t end = min(begin + share, total);
+    uint64_t left = end - begin;
+    const uint64_t step = quotient(begin, (uint64_t)per_req); // begin, in steps of all heads together
+    uint64_t before = 0;
+    int r = 0;
+    for (int r0 = 0; r0 < a.n_req; r0 += 64) {
+        int x = steps_of(r0 + lane);
+        const int own = x;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(x, o);
+            if (lane >= o) x += y;
+        }
+        const uint64_t here = __ballot(before + (uint32_t)x > step);
+        if (here) {
+            const int i = __builtin_ctzll(here);
+            r = r0 + i;
+            before += (uint32_t)(__builtin_amdgcn_readlane(x, i) - __builtin_amdgcn_readlane(own, i));
+            break;
+        }
+        before += (uint32_t)__builtin_amdgcn_readlane(x, 63);
+    }
+    r = __builtin_amdgcn_readfirstlane(r);
+    Walk w = walk_of(a, a.kv_lens[r]);
+    int steps = w.steps();
+    const uint64_t local = begin - before * (uint32_t)per_req;
+    int item = (int)quotient(local, (uint64_t)steps);
+    int step0 = (int)(local - (uint64_t)item * (uint32_t)steps);
+
+    while (true) {
+        const int n = (int)min((uint64_t)(steps - step0), left);
+        const int kvh = item / tiles, tile = item - kvh * tiles;
+        const int head0 = kvh * a.group + tile * ROWS, rows = min(a.group - tile * ROWS, ROWS);
+        bf16x8 q[NT][D / 32];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) {
+                bf16x8 x;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = (__bf16)0.0f;
+                if (16 * t + c16 < rows)
+                    x = *(const bf16x8*)((const __bf16*)a.q + ((int64_t)r * a.n_q_heads + head0 + 16 * t + c16) * D + 32 * ks + 8 * quad);
+                q[t][ks] = x;
+            }
+        Acc<D, NT> acc;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            acc.m[t] = NOTHING;
+            acc.l[t] = 0.0f;
+#pragma unroll
+            for (int cb = 0; cb < D / 16; ++cb) acc.o[t][cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        walk_units<D, NT>(a.pool.k, a.pool.v, a.table + (int64_t)r * a.max_blocks, a.pool, w, q, NW * step0, min(NW * (step0 + n), w.units),
+                          a.scale_log2e, kvh * a.pool.head_stride, (uint32_t)(uintptr_t)(smem + wave * 2 * Rows<D>::BYTES), wave, lane, acc);
+
+        // join the four waves' keys: every wave parks its sums where the rings were
+        __syncthreads();
+        LDS_AS char* park = smem + wave * ROWS * ROWB;
+        LDS_AS float* ml = (LDS_AS float*)(smem + lds_bytes<D, NT>() - NW * ROWS * 8);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const float l = column_reduce<false>(acc.l[t]);
+            if (16 * t + c16 < rows) {
+#pragma unroll
+                for (int cb = 0; cb < D / 16; ++cb) *(LDS_AS f32x4*)(park + (16 * t + c16) * ROWB + (16 * cb + 4 * quad) * 4) = acc.o[t][cb];
+                if (quad == 0) {
+                    ml[(wave * ROWS + 16 * t + c16) * 2] = acc.m[t];
+                    ml[(wave * ROWS + 16 * t + c16) * 2 + 1] = l;
+                }
+            }
+        }
+        __syncthreads();
+        const bool whole = step0 == 0 && n == steps;
+        constexpr int LPR = D / 8; // threads of a row, eight channels each
+        for (int row = tid / LPR; row < rows; row += 64 * NW / LPR) {
+            const int ch = tid % LPR * 8;
+            float mw[NW], M = NOTHING, L = 0.0f, o[8];
+#pragma unroll
+            for (int i = 0; i < NW; ++i) M = fmaxf(M, mw[i] = ml[(i * ROWS + row) * 2]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) {
+                const float f = __builtin_amdgcn_exp2f(mw[i] - M);
+                L = fmaf(f, ml[(i * ROWS + row) * 2 + 1], L);
+                const f32x4 x = *(LDS_AS const f32x4*)(smem + i * ROWS * ROWB + row * ROWB + ch * 4);
+                const f32x4 y = *(LDS_AS const f32x4*)(smem + i * ROWS * ROWB + row * ROWB + ch * 4 + 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[e], o[e]), o[4 + e] = fmaf(f, y[e], o[4 + e]);
+            }
+            if (whole) {
+                const float inv = L == 0.0f ? 0.0f : 1.0f / L; // a row without any weight is zero
+                bf16x8 y;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = (__bf16)(o[e] * inv);
+                *(bf16x8*)((__bf16*)a.out + ((int64_t)r * a.n_q_heads + head0 + row) * D + ch) = y;
+            } else {
+                const int64_t slot = (int64_t)(2 * worker + (step0 == 0)) * a.ws_rows + row; // a share cuts at most its first and its last item
+                *(f32x4*)(a.ws_o + slot * D + ch) = f32x4{o[0], o[1], o[2], o[3]};
+                *(f32x4*)(a.ws_o + slot * D + ch + 4) = f32x4{o[4], o[5], o[6], o[7]};
+                if (ch == 0) *(float2*)(a.ws_ml + slot * 2) = make_float2(M, L);
+            }
+        }
+        if (a.cut && step0 == 0 && tid == 0) { // who begins an item says who else has a piece of it
+            const int pieces = whole ? 1 : (int)(quotient(end - left + (uint32_t)steps - 1, share) - (uint32_t)worker) + 1;
+            *(int2*)(a.ws_items + 2 * ((int64_t)r * per_req + item)) = make_int2(worker, pieces);
+        }
+        left -= (uint32_t)n;
+        if (left == 0) break;
+        step0 = 0;
+        if (++item == per_req) {
+            item = 0;
+            if (++r == a.n_req) break; // not reached unless the lengths are written meanwhile
+            w = walk_of(a, a.kv_lens[r]);
+            steps = w.steps();
+        }
+        __syncthreads(); // the parked sums are read
+    }
+}
+
+// Joins the pieces of cut items: out = sum_p f_p O_p / sum_p f_p l_p with f_p = 2^(m_p - max m).  One workgroup per row of the
+// result; groups of D / 4 lanes take every GROUPS-th piece and are joined through LDS.
+template <int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs a, int rows_per_tile)
+{
+    constexpr int LPR = D / 4, GROUPS = 256 / LPR;
+    __shared__ f32x4 os[GROUPS][LPR];
+    __shared__ float2 mls[GROUPS];
+    const int tid = threadIdx.x, grp = tid / LPR, piece = tid % LPR;
+    const int r = blockIdx.x / a.n_q_heads, h = blockIdx.x - r * a.n_q_heads;
+    const int tiles = (a.group + rows_per_tile - 1) / rows_per_tile, kvh = h / a.group, in = h - kvh * a.group;
+    const int tile = in / rows_per_tile, row = in - tile * rows_per_tile;
+    const int2 item = *(const int2*)(a.ws_items + 2 * (((int64_t)r * a.n_kv_heads + kvh) * tiles + tile));
+    if (item.y <= 1) return;
+    float M = NOTHING, L = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int AHEAD = 4;
+    for (int p0 = grp; p0 < item.y; p0 += GROUPS * AHEAD) {
+        f32x4 x[AHEAD];
+        float2 ml[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int p = p0 + GROUPS * i;
+            const int64_t slot = (int64_t)(2 * (item.x + min(p, item.y - 1)) + (p == 0)) * a.ws_rows + row;
+            x[i] = *(const f32x4*)(a.ws_o + slot * D + 4 * piece);
+            ml[i] = *(const float2*)(a.ws_ml + slot * 2);
+            if (p >= item.y) ml[i] = make_float2(NOTHING, 0.0f), x[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, ml[i].x);
+        const float old = __builtin_amdgcn_exp2f(M - top);
+        L *= old;
+        o *= old;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const float f = __builtin_amdgcn_exp2f(ml[i].x - top);
+            L = fmaf(f, ml[i].y, L);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[i][e], o[e]);
+        }
+        M = top;
+    }
+    os[grp][piece] = o;
+    if (piece == 0) mls[grp] = make_float2(M, L);
+    __syncthreads();
+    if (grp != 0) return;
+    float top = NOTHING, total = 0.0f;
+    f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) top = fmaxf(top, mls[g].x);
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+        const float f = __builtin_amdgcn_exp2f(mls[g].x - top);
+        total = fmaf(f, mls[g].y, total);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = fmaf(f, os[g][piece][e], y[e]);
+    }
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    bf16x4 z;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = (__bf16)(y[e] * inv);
+    *(bf16x4*)((__bf16*)a.out + (int64_t)blockIdx.x * D + 4 * piece) = z;
+}
+
+template <int D, int NT> int launch_decode(const TrPagedDecodeArgs& a, int grid, hipStream_t s)
+{
+    static std::atomic<uint64_t> raised{0};
+    constexpr int lds = lds_bytes<D, NT>();
+    if (const int rc = tr_raise_lds_limit((const void*)paged_decode_kernel<D, NT>, lds, &raised)) return rc;
+    paged_decode_kernel<D, NT><<<dim3(grid), dim3(64 * NW), lds, s>>>(a);
+    TR_HIP(hipGetLastError());
+    if (a.cut) {
+        paged_join_kernel<D><<<dim3(a.n_req * a.n_q_heads), dim3(256), 0, s>>>(a, 16 * NT);
+        TR_HIP(hipGetLastError());
+    }
+    return TR_OK;
+}
+
+} // namespace
+
+int tr_launch_paged_decode_bf16(const TrPagedDecodeArgs& a, int head_dim, int grid, hipStream_t s)
+{
+    if (a.group <= 16) return head_dim == 128 ? launch_decode<128, 1>(a, grid, s) : launch_decode<64, 1>(a, grid, s);
+    return head_dim == 128 ? launch_decode<128, 2>(a, grid, s) : launch_decode<64, 2>(a, grid, s);
+}
