@@ -294,7 +294,7 @@ int tr_linear(const void* x, int32_t M, int32_t K, int32_t n_out, const void* co
  * tr_pages: the pool.  Row i of page p of KV head h begins at element p * page_stride + i * row_stride + h * head_stride of k
  * (and of v) and is head_dim contiguous elements; so [page, row, head, channel] and [page, head, row, channel] pools, and pools
  * whose k and v are halves of one allocation, are all described by their strides.  k, v 16-byte aligned, strides multiples of 16
- * bytes and at most 64 MiB for rows and heads; page_size a power of two, 8 .. 1024; n_pages * page_size below 2^31; k, v and
+ * bytes, at most 64 MiB for rows and heads and below 4 GiB for pages; page_size a power of two, 8 .. 1024; n_pages * page_size below 2^31; k, v and
  * dtype, n_kv_heads and head_dim have to fit the tr_shape of the call (else TR_ERR_SHAPE).
  * A slot is the index page * page_size + row of a row in the pool.  A page id outside [0, n_pages) means "no page": rows of
  * such a page are never read or written, and attention gives their keys no weight. */
@@ -379,7 +379,8 @@ int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* 
  * Scores, softmax, weights and the weighted sum are fp32, whatever the type.  Results do not depend on how long the table is.
  * workspace: tr_paged_decode_attn_workspace_size() bytes, 256-byte aligned, else TR_ERR_WORKSPACE; it depends on the arguments
  * of the query alone, not on the lengths; calls that may overlap need one each.  q, out and pages 16-byte aligned.
- * max_blocks * page_size <= 2^30; n_req <= 65536 and n_req * n_q_heads < 2^24 (else TR_ERR_UNSUPPORTED); n_req == 0 is a no-op. */
+ * max_blocks * page_size <= 2^30; n_req <= 65536, n_req * n_q_heads < 2^24 and
+ * n_req * n_kv_heads * max_blocks * page_size < 2^36 (else TR_ERR_UNSUPPORTED); n_req == 0 is a no-op. */
 size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size);
 int tr_paged_decode_attn(const tr_shape* shape, const void* q, const tr_pages* pages, const int32_t* block_table /*device*/,
                          int32_t max_blocks, const int32_t* kv_lens /*device*/, int32_t n_req, int32_t window, int32_t n_sink,

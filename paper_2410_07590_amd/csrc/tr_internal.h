@@ -428,7 +428,7 @@ struct TrPagedAppendArgs {
 // Decode: each of TR_PAGED_WORKERS workgroups takes an equal share of the batch's steps, of at least TR_PAGED_MIN_STEPS.
 #define TR_PAGED_STEP_KEYS 128
 #define TR_PAGED_WORKERS 512
-#define TR_PAGED_MIN_STEPS 2
+#define TR_PAGED_MIN_STEPS 1
 static inline int tr_paged_tile_rows(int group) { return group <= 16 ? 16 : 32; }
 struct TrPagedDecodeArgs {
     const void* q;

@@ -32,10 +32,10 @@ int pool_of(const char* who, const tr_shape* sh, const tr_pages* p, TrPool* out)
     // a stride of a single page or head is never applied; the others have to keep rows apart
     if (p->row_stride < sh->head_dim || (p->n_kv_heads > 1 && p->head_stride < sh->head_dim) || (p->n_pages > 1 && p->page_stride < sh->head_dim))
         return tr_fail(TR_ERR_INVALID_ARG, "%s: strides of the pages are smaller than a head", who);
-    if (p->head_stride < 0 || p->page_stride < 0 || p->page_stride > INT64_MAX / 4 / p->n_pages / e)
+    if (p->head_stride < 0 || p->page_stride < 0)
         return tr_fail(TR_ERR_INVALID_ARG, "%s: strides of the pages are out of range", who);
-    if (p->row_stride > widest / e || p->head_stride > widest / e)
-        return tr_fail(TR_ERR_UNSUPPORTED, "%s: rows or heads of the pages are more than 64 MiB apart", who);
+    if (p->row_stride > widest / e || p->head_stride > widest / e || p->page_stride > (widest * 64 - 1) / e)
+        return tr_fail(TR_ERR_UNSUPPORTED, "%s: rows or heads of the pages are more than 64 MiB apart, or pages 4 GiB", who);
     if (!aligned16(p->k) || !aligned16(p->v) || p->page_stride * e % 16 || p->row_stride * e % 16 || p->head_stride * e % 16)
         return tr_fail(TR_ERR_INVALID_ARG, "%s: pages and their strides must be 16-byte aligned", who);
     out->k = (char*)p->k;
@@ -285,6 +285,7 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)shape->head_dim));
     if (shape->dtype == TR_F32) return tr_launch_paged_decode_f32(a, shape->head_dim, (hipStream_t)stream);
     const DecodePlan plan = decode_plan(shape, n_req, (int64_t)max_blocks * pages->page_size);
+    if (plan.bound > INT_LIMIT) return tr_fail(TR_ERR_UNSUPPORTED, "%s: the table has room for 2^31 steps of 128 keys or more", who);
     if (plan.bytes) {
         if (!workspace || ((uintptr_t)workspace & 255)) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace missing or not 256-byte aligned", who);
         if (workspace_bytes < plan.bytes) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace holds %zu bytes, %zu needed", who, workspace_bytes, plan.bytes);

@@ -22,6 +22,7 @@
 #include "tr_internal.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
@@ -34,8 +35,19 @@ constexpr int FLIGHT = 6;            // loads of 1 KB that a wave has on their w
 
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// a / b for numbers that nearly always fit 32 bits
-__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) { return ((a | b) >> 32) == 0 ? (uint64_t)((uint32_t)a / (uint32_t)b) : a / b; }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Inclusive sums over the wave, on the vector unit's cross-lane path: within rows of 16 lanes, then across them.
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false); // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false); // last lane of a row to the next row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false); // lane 31 to the upper half
+    return x;
+}
 
 // The keys of a request as units of 32: the first `su` hold the sinks, the others run from unit `lu` to the end.
 struct Walk {
@@ -98,7 +110,7 @@ template <int D, int NT> struct Acc {
 // compiler otherwise takes the reads of LDS to depend on every load on its way to it.
 template <int D, int NT>
 __device__ __forceinline__ void walk_units(const char* __restrict__ k, const char* __restrict__ v, const int32_t* __restrict__ table, const TrPool& pool,
-                                           const Walk& w, const bf16x8 (&q)[NT][D / 32], int u0, int u1, float scale, int64_t head, uint32_t ring,
+                                           const Walk& w, const bf16x8 (&q)[NT][D / 32], int u0, int u1, float scale, uint32_t ring,
                                            int wave, int lane, Acc<D, NT>& acc)
 {
     using R = Rows<D>;
@@ -110,7 +122,6 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
     const int sub_shift = min(pool.page_shift, 5), per_unit_shift = 5 - sub_shift; // rows of a page within a unit; pages of a unit
     const int refill = 64 >> per_unit_shift;                                         // units whose ids a register holds
     const int c16 = lane & 15, quad = lane >> 4;
-    const int row_bytes = (int)pool.row_stride;
 
     auto fetch_ids = [&](int j0) {
         const int j = j0 + (lane >> per_unit_shift), u = u0 + wave + NW * j;
@@ -123,7 +134,7 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
     };
     auto ref = [&](int j, uint64_t none) {
         UnitRef u;
-        u.key0 = w.unit(u0 + wave + NW * j) * UNIT;
+        u.key0 = uniform(w.unit(u0 + wave + NW * j) * UNIT);
         u.at = (j & (refill - 1)) << per_unit_shift;
         u.seen = w.seen(u.key0);
         uint32_t holes = (uint32_t)(none >> u.at) & low_bits(1 << per_unit_shift);
@@ -132,26 +143,46 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             holes &= holes - 1;
             u.seen &= ~(low_bits(1 << sub_shift) << (s << sub_shift));
         }
+        u.seen = (uint32_t)uniform((int)u.seen);
         return u;
     };
-    // load i of a unit
+    // What a lane adds to the start of a unit's page for load i (i: its row within the page, where pages are shorter than units).
     const int r_in = lane / R::CPR;
-    auto load = [&](const char* base, const UnitRef& u, int ids, int i, uint32_t lds, bool is_v) {
-        const int row = i * R::RPI + r_in; // of the unit; says where the data lands
-        const int chunk = (is_v ? R::vchunk(row, lane) : R::kchunk(row, lane)) * 16;
-        const char* p;
+    const uint32_t row_bytes = (uint32_t)pool.row_stride, page_bytes = (uint32_t)pool.page_stride;
+    uint32_t dk[LPU], dv[LPU];
+#pragma unroll
+    for (int i = 0; i < LPU; ++i) {
+        const int row = i * R::RPI + r_in;
+        const uint32_t in = (uint32_t)(row & ((1 << sub_shift) - 1)) * row_bytes;
+        dk[i] = in + R::kchunk(row, lane) * 16;
+        dv[i] = in + R::vchunk(row, lane) * 16;
+    }
+    auto issue = [&](const char* base, const uint32_t (&d)[LPU], const UnitRef& u, int ids, uint32_t lds, bool is_v, auto later) {
+        constexpr bool LATER = decltype(later)::value; // not the first unit: no more than FLIGHT loads on their way
+        const char* const first_row = base + (uint64_t)(uint32_t)(u.key0 & (page - 1)) * row_bytes;
         if (u.seen == 0xffffffffu) { // the rows of a load lie in one page
-            const int id = __builtin_amdgcn_readlane(ids, u.at + ((i * R::RPI) >> sub_shift));
-            const char* at = base + (int64_t)id * pool.page_stride + (int64_t)((u.key0 + i * R::RPI) & (page - 1)) * pool.row_stride + head;
-            p = at + (uint32_t)(r_in * row_bytes + chunk);
+#pragma unroll
+            for (int i = 0; i < LPU; ++i) {
+                if (LATER && i + LPU >= FLIGHT) wait_vm<FLIGHT - 1>();
+                const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(ids, u.at + ((i * R::RPI) >> sub_shift));
+                __builtin_amdgcn_global_load_lds((const GLB_AS void*)(first_row + (uint64_t)id * page_bytes + d[i]), (LDS_AS void*)(uintptr_t)(lds + i * 1024), 16, 0,
+                                                 DMA_STREAM);
+            }
         } else { // rows that are not seen read one that is: what lies there may be anything
             const int first = u.seen ? __builtin_ctz(u.seen) : 0;
-            const int src = (u.seen >> row) & 1 ? row : first;
-            const int id = max(__shfl(ids, u.at + (src >> sub_shift)), 0);
-            p = base + (int64_t)id * pool.page_stride + (int64_t)((u.key0 + src) & (page - 1)) * pool.row_stride + head + chunk;
+#pragma unroll 1
+            for (int i = 0; i < LPU; ++i) {
+                if (LATER) wait_vm<FLIGHT - 1>();
+                const int row = i * R::RPI + r_in, src = (u.seen >> row) & 1 ? row : first;
+                const uint32_t id = (uint32_t)max(__shfl(ids, u.at + (src >> sub_shift)), 0);
+                const char* p = first_row + (uint64_t)id * page_bytes + (uint64_t)(uint32_t)(src & ((1 << sub_shift) - 1)) * row_bytes +
+                                (is_v ? R::vchunk(row, lane) : R::kchunk(row, lane)) * 16;
+                __builtin_amdgcn_global_load_lds((const GLB_AS void*)p, (LDS_AS void*)(uintptr_t)(uint32_t)uniform((int)(lds + i * 1024)), 16, 0, DMA_STREAM);
+            }
         }
-        __builtin_amdgcn_global_load_lds((const GLB_AS void*)p, (LDS_AS void*)(uintptr_t)(lds + i * 1024), 16, 0, DMA_STREAM);
     };
+    const std::false_type at_once;
+    const std::true_type in_turn;
 
     const uint32_t kring = ring, vring = ring + R::BYTES;
     int koff[D / 32], voff[D / 16];
@@ -165,10 +196,8 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
     int ids = fetch_ids(0);
     uint64_t none = __ballot(ids < 0);
     UnitRef cur = ref(0, none);
-#pragma unroll
-    for (int i = 0; i < LPU; ++i) load(k, cur, ids, i, kring, false);
-#pragma unroll
-    for (int i = 0; i < LPU; ++i) load(v, cur, ids, i, vring, true);
+    issue(k, dk, cur, ids, kring, false, at_once);
+    issue(v, dv, cur, ids, vring, true, at_once);
     for (int t = 0; t < n_own; ++t) {
         const bool more = t + 1 < n_own;
         UnitRef next = cur;
@@ -182,24 +211,20 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
         wait_vm<LPU>(); // K(t)
         asm volatile("" ::: "memory");
         f32x4 s[NT][2];
+        bf16x8 ka[2][D / 32];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) {
-                const bf16x8 a = *(LDS_AS const bf16x8*)(lds + koff[ks] + kb * 16 * D * 2);
+            for (int ks = 0; ks < D / 32; ++ks) ka[kb][ks] = *(LDS_AS const bf16x8*)(lds + koff[ks] + kb * 16 * D * 2);
+        wait_lds(); // the unit's keys are read
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
-                    s[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[n][ks], ks == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[n][kb], 0, 0, 0);
-            }
-        }
-        wait_lds(); // the unit's keys are read
-        if (more) {
-#pragma unroll
-            for (int i = 0; i < LPU; ++i) {
-                if (i + LPU >= FLIGHT) wait_vm<FLIGHT - 1>();
-                load(k, next, ids, i, kring, false);
-            }
-        }
+                    s[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[kb][ks], q[n][ks], ks == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[n][kb], 0, 0, 0);
+        if (more) issue(k, dk, next, ids, kring, false, in_turn);
         // element e of block kb is key 16 kb + 4 quad + e of the unit
         if (cur.seen != 0xffffffffu) {
             const uint32_t mine = cur.seen >> (4 * quad);
@@ -240,31 +265,23 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
         if (more) wait_vm<LPU>(); // V(t)
         else wait_vm<0>();
         asm volatile("" ::: "memory");
+        bf16x8 va[D / 16];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            if (cur.seen) {
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    const int cb = half * (D / 32) + c;
-                    LDS_AS const char* p0 = lds + voff[cb];
-                    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)p0);
-                    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(p0 + 16 * D * 2));
-                    const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, hi[n], acc.o[n][cb], 0, 0, 0);
-                        acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, lo[n], acc.o[n][cb], 0, 0, 0);
-                    }
-                }
-            }
+        for (int cb = 0; cb < D / 16; ++cb) {
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(lds + voff[cb]));
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(lds + voff[cb] + 16 * D * 2));
+            va[cb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
         }
         wait_lds(); // the unit's values are read
-        if (more) {
+        if (more) issue(v, dv, next, ids, vring, true, in_turn);
+        if (cur.seen) { // else: values that are nobody's, for weights of zero
 #pragma unroll
-            for (int i = 0; i < LPU; ++i) {
-                if (i + LPU >= FLIGHT) wait_vm<FLIGHT - 1>();
-                load(v, next, ids, i, vring, true);
-            }
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int cb = 0; cb < D / 16; ++cb) {
+                    acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], hi[n], acc.o[n][cb], 0, 0, 0);
+                    acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], lo[n], acc.o[n][cb], 0, 0, 0);
+                }
         }
         cur = next;
     }
@@ -289,50 +306,35 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_decode_kernel(const TrPagedD
     const int worker = blockIdx.x;
 
     // the batch's steps, and the request that this worker's share begins in
-    auto steps_of = [&](int r) { return r < a.n_req ? walk_of(a, a.kv_lens[r]).steps() : 0; };
-    uint64_t total = 0;
-    for (int r0 = 0; r0 < a.n_req; r0 += 64) {
-        int x = steps_of(r0 + lane);
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
-        total += (uint32_t)__builtin_amdgcn_readfirstlane(x);
-    }
-    total *= (uint32_t)per_req;
-    const uint64_t share = max((total + (uint32_t)(a.workers - 1)) / (uint32_t)a.workers, (uint64_t)TR_PAGED_MIN_STEPS);
-    const uint64_t begin = share * (uint32_t)worker;
+    auto len_of = [&](int r) { return r < a.n_req ? a.kv_lens[r] : 0; };
+    auto steps_of = [&](int r, int len) { return r < a.n_req ? walk_of(a, len).steps() : 0; };
+    int lens = len_of(lane), own = steps_of(lane, lens), sums = wave_scan(own); // of the 64 requests from r0 on
+    int total = __builtin_amdgcn_readlane(sums, 63);
+    for (int r0 = 64; r0 < a.n_req; r0 += 64) total += __builtin_amdgcn_readlane(wave_scan(steps_of(r0 + lane, len_of(r0 + lane))), 63);
+    total *= per_req;
+    const int share = max((total + a.workers - 1) / a.workers, TR_PAGED_MIN_STEPS);
+    const int begin = share * worker;
     if (begin >= total) return;
-    const uint64_t end = min(begin + share, total);
-    uint64_t left = end - begin;
-    const uint64_t step = quotient(begin, (uint64_t)per_req); // begin, in steps of all heads together
-    uint64_t before = 0;
-    int r = 0;
-    for (int r0 = 0; r0 < a.n_req; r0 += 64) {
-        int x = steps_of(r0 + lane);
-        const int own = x;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int y = __shfl_up(x, o);
-            if (lane >= o) x += y;
-        }
-        const uint64_t here = __ballot(before + (uint32_t)x > step);
-        if (here) {
-            const int i = __builtin_ctzll(here);
-            r = r0 + i;
-            before += (uint32_t)(__builtin_amdgcn_readlane(x, i) - __builtin_amdgcn_readlane(own, i));
-            break;
-        }
-        before += (uint32_t)__builtin_amdgcn_readlane(x, 63);
+    const int end = min(begin + share, total);
+    int left = end - begin;
+    const int step = begin / per_req; // in steps of all heads together
+    int before = 0, r0 = 0;
+    while (before + __builtin_amdgcn_readlane(sums, 63) <= step && r0 + 64 < a.n_req) {
+        before += __builtin_amdgcn_readlane(sums, 63);
+        r0 += 64;
+        lens = len_of(r0 + lane), own = steps_of(r0 + lane, lens), sums = wave_scan(own);
     }
-    r = __builtin_amdgcn_readfirstlane(r);
-    Walk w = walk_of(a, a.kv_lens[r]);
+    const int at = __builtin_ctzll(__ballot(before + sums > step));
+    int r = r0 + at;
+    before += __builtin_amdgcn_readlane(sums, at) - __builtin_amdgcn_readlane(own, at);
+    Walk w = walk_of(a, __builtin_amdgcn_readlane(lens, at));
     int steps = w.steps();
-    const uint64_t local = begin - before * (uint32_t)per_req;
-    int item = (int)quotient(local, (uint64_t)steps);
-    int step0 = (int)(local - (uint64_t)item * (uint32_t)steps);
+    const int local = begin - before * per_req;
+    int item = uniform(local / steps), step0 = local - item * steps;
 
     while (true) {
-        const int n = (int)min((uint64_t)(steps - step0), left);
-        const int kvh = item / tiles, tile = item - kvh * tiles;
+        const int n = min(steps - step0, left);
+        const int kvh = uniform(item / tiles), tile = item - kvh * tiles;
         const int head0 = kvh * a.group + tile * ROWS, rows = min(a.group - tile * ROWS, ROWS);
         bf16x8 q[NT][D / 32];
 #pragma unroll
@@ -354,8 +356,9 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_decode_kernel(const TrPagedD
 #pragma unroll
             for (int cb = 0; cb < D / 16; ++cb) acc.o[t][cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        walk_units<D, NT>(a.pool.k, a.pool.v, a.table + (int64_t)r * a.max_blocks, a.pool, w, q, NW * step0, min(NW * (step0 + n), w.units),
-                          a.scale_log2e, kvh * a.pool.head_stride, (uint32_t)(uintptr_t)(smem + wave * 2 * Rows<D>::BYTES), wave, lane, acc);
+        const int64_t head = kvh * a.pool.head_stride;
+        walk_units<D, NT>(a.pool.k + head, a.pool.v + head, a.table + (int64_t)r * a.max_blocks, a.pool, w, q, NW * step0, min(NW * (step0 + n), w.units),
+                          a.scale_log2e, (uint32_t)(uintptr_t)(smem + wave * 2 * Rows<D>::BYTES), wave, lane, acc);
 
         // join the four waves' keys: every wave parks its sums where the rings were
         __syncthreads();
@@ -406,16 +409,16 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_decode_kernel(const TrPagedD
             }
         }
         if (a.cut && step0 == 0 && tid == 0) { // who begins an item says who else has a piece of it
-            const int pieces = whole ? 1 : (int)(quotient(end - left + (uint32_t)steps - 1, share) - (uint32_t)worker) + 1;
+            const int pieces = whole ? 1 : (end - left + steps - 1) / share - worker + 1;
             *(int2*)(a.ws_items + 2 * ((int64_t)r * per_req + item)) = make_int2(worker, pieces);
         }
-        left -= (uint32_t)n;
+        left -= n;
         if (left == 0) break;
         step0 = 0;
         if (++item == per_req) {
             item = 0;
             if (++r == a.n_req) break; // not reached unless the lengths are written meanwhile
-            w = walk_of(a, a.kv_lens[r]);
+            w = walk_of(a, uniform(a.kv_lens[r]));
             steps = w.steps();
         }
         __syncthreads(); // the parked sums are read

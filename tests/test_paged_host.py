@@ -160,7 +160,8 @@ def rotary(**kw):
     (dict(pages=pages(page_size=12)), -1), (dict(pages=pages(page_size=4)), -1), (dict(pages=pages(n_pages=0)), -1), (dict(pages=pages(n_pages=2 ** 27)), -1),
     (dict(pages=pages(reserved=1)), -1), (dict(pages=pages(k=0)), -1), (dict(pages=pages(v=FAKE[11] + 8)), -1), (dict(pages=pages(row_stride=64)), -1),
     (dict(pages=pages(row_stride=516)), -1), (dict(pages=pages(head_stride=0)), -1), (dict(pages=pages(page_stride=-8192)), -1),
-    (dict(pages=pages(page_stride=2 ** 60)), -1), (dict(pages=pages(row_stride=2 ** 26)), B.TR_ERR_UNSUPPORTED)])
+    (dict(pages=pages(page_stride=2 ** 60)), B.TR_ERR_UNSUPPORTED), (dict(pages=pages(page_stride=2 ** 31)), B.TR_ERR_UNSUPPORTED),
+    (dict(pages=pages(row_stride=2 ** 26)), B.TR_ERR_UNSUPPORTED)])
 def test_append_refusals(L, kw, code):
     assert append(L, **kw) == code and L.tr_last_error()
 
