@@ -285,7 +285,7 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)shape->head_dim));
     if (shape->dtype == TR_F32) return tr_launch_paged_decode_f32(a, shape->head_dim, (hipStream_t)stream);
     const DecodePlan plan = decode_plan(shape, n_req, (int64_t)max_blocks * pages->page_size);
-    if (plan.bound > INT_LIMIT) return tr_fail(TR_ERR_UNSUPPORTED, "%s: the table has room for 2^31 steps of 128 keys or more", who);
+    if (plan.bound > ((int64_t)1 << 30)) return tr_fail(TR_ERR_UNSUPPORTED, "%s: the table has room for more than 2^30 steps of 128 keys", who);
     if (plan.bytes) {
         if (!workspace || ((uintptr_t)workspace & 255)) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace missing or not 256-byte aligned", who);
         if (workspace_bytes < plan.bytes) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace holds %zu bytes, %zu needed", who, workspace_bytes, plan.bytes);

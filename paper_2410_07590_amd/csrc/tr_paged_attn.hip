@@ -26,6 +26,8 @@
 
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int NW = 4, UNIT = 32, STEP = NW * UNIT; // waves, keys of a wave, keys of a step
 static_assert(STEP == TR_PAGED_STEP_KEYS, "");
 constexpr float SLACK = 8.0f;        // log2 units by which a score may exceed the reference before it moves
@@ -71,6 +73,14 @@ __device__ __forceinline__ Walk walk_of(const TrPagedDecodeArgs& a, int kv_len)
     return w;
 }
 
+// A barrier behind this wave's accesses of LDS.  Loads on their way to LDS stay on their way: nobody else reads what they bring.
+__device__ __forceinline__ void sync_lds()
+{
+    wait_lds();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 template <bool MAX> __device__ __forceinline__ float column_reduce(float x) // over the four lanes of a query column
 {
     auto op = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
@@ -93,10 +103,22 @@ template <int D> struct Rows {
     __device__ static __forceinline__ int vchunk(int row, int lane) { return (((lane % CPR) >> 1) ^ vsw(row)) * 2 + (lane & 1); }
 };
 
-// One unit of a wave: its first key, which of its keys are seen, and where its page ids are among the wave's.
+// One unit of a wave: where its KV head begins, its first key, which of its keys are seen, and where its page ids are among the
+// wave's.
 struct UnitRef {
+    int64_t head;
     int key0, at;
     uint32_t seen;
+};
+
+// A run of steps of one item that one worker walks.
+struct Piece {
+    int r, item, step0, n, steps; // n == 0: there is none
+    Walk w;
+    __device__ __forceinline__ int u0() const { return NW * step0; }
+    __device__ __forceinline__ int u1() const { return min(NW * (step0 + n), w.units); }
+    __device__ __forceinline__ int own(int wave) const { return max((u1() - u0() - wave + NW - 1) / NW, 0); } // units of a wave
+    __device__ __forceinline__ bool whole() const { return n == steps; }
 };
 
 // What one wave accumulates: O^T (element e of block b is channel 16 b + 4 (lane / 16) + e of query column lane % 16), reference
@@ -106,38 +128,61 @@ template <int D, int NT> struct Acc {
     float m[NT], l[NT];
 };
 
-// A wave's walk over its units of a piece.  A function of its own with restricted pointers, LDS by whole addresses: the
-// compiler otherwise takes the reads of LDS to depend on every load on its way to it.
-template <int D, int NT>
-__device__ __forceinline__ void walk_units(const char* __restrict__ k, const char* __restrict__ v, const int32_t* __restrict__ table, const TrPool& pool,
-                                           const Walk& w, const bf16x8 (&q)[NT][D / 32], int u0, int u1, float scale, uint32_t ring,
-                                           int wave, int lane, Acc<D, NT>& acc)
-{
+// A wave's loads.
+template <int D> struct Stream {
     using R = Rows<D>;
-    constexpr int LPU = R::LPU;
-    static_assert(FLIGHT <= 2 * LPU, "");
-    const int n_own = (u1 - u0 - wave + NW - 1) / NW;
-    if (n_own <= 0) return;
-    const int page = 1 << pool.page_shift;
-    const int sub_shift = min(pool.page_shift, 5), per_unit_shift = 5 - sub_shift; // rows of a page within a unit; pages of a unit
-    const int refill = 64 >> per_unit_shift;                                         // units whose ids a register holds
-    const int c16 = lane & 15, quad = lane >> 4;
+    static constexpr int LPU = R::LPU;
+    uint32_t kring, vring, row_bytes, page_bytes;
+    int wave, lane, page_shift, sub_shift, per_unit_shift, n_pages; // sub_shift: rows of a page within a unit; per_unit_shift: pages of a unit
+    int32_t max_blocks;
+    int64_t head_stride;
+    uint32_t dk[LPU], dv[LPU]; // what a lane adds to the start of a unit's page for load i
 
-    auto fetch_ids = [&](int j0) {
-        const int j = j0 + (lane >> per_unit_shift), u = u0 + wave + NW * j;
-        const int key = w.unit(u) * UNIT + ((lane & ((1 << per_unit_shift) - 1)) << sub_shift);
+    __device__ __forceinline__ Stream(const TrPagedDecodeArgs& a, uint32_t ring, int wave_, int lane_) : wave(wave_), lane(lane_)
+    {
+        kring = (uint32_t)uniform((int)ring);
+        vring = kring + R::BYTES;
+        row_bytes = (uint32_t)a.pool.row_stride;
+        page_bytes = (uint32_t)a.pool.page_stride;
+        head_stride = a.pool.head_stride;
+        page_shift = a.pool.page_shift;
+        n_pages = a.pool.n_pages;
+        max_blocks = a.max_blocks;
+        sub_shift = min(page_shift, 5);
+        per_unit_shift = 5 - sub_shift;
+#pragma unroll
+        for (int i = 0; i < LPU; ++i) {
+            const int row = i * R::RPI + lane / R::CPR;
+            const uint32_t in = (uint32_t)(row & ((1 << sub_shift) - 1)) * row_bytes;
+            dk[i] = in + R::kchunk(row, lane) * 16;
+            dv[i] = in + R::vchunk(row, lane) * 16;
+        }
+    }
+    __device__ __forceinline__ int refill() const { return 64 >> per_unit_shift; } // units whose ids a register holds
+
+    // Page ids of the wave's units from its j0-th of a piece on, a lane each; -1 where there is none.
+    __device__ __forceinline__ int fetch_ids(const int32_t* __restrict__ table, const Piece& p, int j0) const
+    {
+        const int j = j0 + (lane >> per_unit_shift), u = p.u0() + wave + NW * j;
+        const int key = p.w.unit(u) * UNIT + ((lane & ((1 << per_unit_shift) - 1)) << sub_shift);
         int id = -1;
-        if (u < u1 && key < w.len) id = table[key >> pool.page_shift];
-        if ((uint32_t)id >= (uint32_t)pool.n_pages) id = -1;
+        if (u < p.u1() && key < p.w.len) id = table[(int64_t)p.r * max_blocks + (key >> page_shift)];
+        return id;
+    }
+    __device__ __forceinline__ int checked(int id) const
+    {
+        if ((uint32_t)id >= (uint32_t)n_pages) id = -1;
         asm volatile("" : "+v"(id)); // waited for here, once for many units, and not wherever an id is taken out
         return id;
-    };
-    auto ref = [&](int j, uint64_t none) {
+    }
+    __device__ __forceinline__ UnitRef ref(const Piece& p, int kvh, int j, int ids) const
+    {
         UnitRef u;
-        u.key0 = uniform(w.unit(u0 + wave + NW * j) * UNIT);
-        u.at = (j & (refill - 1)) << per_unit_shift;
-        u.seen = w.seen(u.key0);
-        uint32_t holes = (uint32_t)(none >> u.at) & low_bits(1 << per_unit_shift);
+        u.head = kvh * head_stride;
+        u.key0 = uniform(p.w.unit(p.u0() + wave + NW * j) * UNIT);
+        u.at = (j & (refill() - 1)) << per_unit_shift;
+        u.seen = p.w.seen(u.key0);
+        uint32_t holes = (uint32_t)(__ballot(ids < 0) >> u.at) & low_bits(1 << per_unit_shift);
         while (holes) { // pages that are none
             const int s = __builtin_ctz(holes);
             holes &= holes - 1;
@@ -145,68 +190,57 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
         }
         u.seen = (uint32_t)uniform((int)u.seen);
         return u;
-    };
-    // What a lane adds to the start of a unit's page for load i (i: its row within the page, where pages are shorter than units).
-    const int r_in = lane / R::CPR;
-    const uint32_t row_bytes = (uint32_t)pool.row_stride, page_bytes = (uint32_t)pool.page_stride;
-    uint32_t dk[LPU], dv[LPU];
-#pragma unroll
-    for (int i = 0; i < LPU; ++i) {
-        const int row = i * R::RPI + r_in;
-        const uint32_t in = (uint32_t)(row & ((1 << sub_shift) - 1)) * row_bytes;
-        dk[i] = in + R::kchunk(row, lane) * 16;
-        dv[i] = in + R::vchunk(row, lane) * 16;
     }
-    auto issue = [&](const char* base, const uint32_t (&d)[LPU], const UnitRef& u, int ids, uint32_t lds, bool is_v, auto later) {
-        constexpr bool LATER = decltype(later)::value; // not the first unit: no more than FLIGHT loads on their way
-        const char* const first_row = base + (uint64_t)(uint32_t)(u.key0 & (page - 1)) * row_bytes;
-        if (u.seen == 0xffffffffu) { // the rows of a load lie in one page
+    // LATER: not the worker's first unit: no more than FLIGHT loads on their way.  The rows of a load lie in one page; where that is
+    // none, they are read from page 0, and rows behind the last key from wherever they would be: both exist, and neither is seen.
+    template <bool V, bool LATER> __device__ __forceinline__ void issue(const char* __restrict__ base, const UnitRef& u, int ids) const
+    {
+        const char* const first_row = base + u.head + (uint64_t)(uint32_t)(u.key0 & ((1 << page_shift) - 1)) * row_bytes;
 #pragma unroll
-            for (int i = 0; i < LPU; ++i) {
-                if (LATER && i + LPU >= FLIGHT) wait_vm<FLIGHT - 1>();
-                const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(ids, u.at + ((i * R::RPI) >> sub_shift));
-                __builtin_amdgcn_global_load_lds((const GLB_AS void*)(first_row + (uint64_t)id * page_bytes + d[i]), (LDS_AS void*)(uintptr_t)(lds + i * 1024), 16, 0,
-                                                 DMA_STREAM);
-            }
-        } else { // rows that are not seen read one that is: what lies there may be anything
-            const int first = u.seen ? __builtin_ctz(u.seen) : 0;
-#pragma unroll 1
-            for (int i = 0; i < LPU; ++i) {
-                if (LATER) wait_vm<FLIGHT - 1>();
-                const int row = i * R::RPI + r_in, src = (u.seen >> row) & 1 ? row : first;
-                const uint32_t id = (uint32_t)max(__shfl(ids, u.at + (src >> sub_shift)), 0);
-                const char* p = first_row + (uint64_t)id * page_bytes + (uint64_t)(uint32_t)(src & ((1 << sub_shift) - 1)) * row_bytes +
-                                (is_v ? R::vchunk(row, lane) : R::kchunk(row, lane)) * 16;
-                __builtin_amdgcn_global_load_lds((const GLB_AS void*)p, (LDS_AS void*)(uintptr_t)(uint32_t)uniform((int)(lds + i * 1024)), 16, 0, DMA_STREAM);
-            }
+        for (int i = 0; i < LPU; ++i) {
+            if (LATER && i + LPU >= FLIGHT) wait_vm<FLIGHT - 1>();
+            const uint32_t id = (uint32_t)max(__builtin_amdgcn_readlane(ids, u.at + ((i * R::RPI) >> sub_shift)), 0);
+            __builtin_amdgcn_global_load_lds((const GLB_AS void*)(first_row + (uint64_t)id * page_bytes + (V ? dv[i] : dk[i])),
+                                             (LDS_AS void*)(uintptr_t)((V ? vring : kring) + i * 1024), 16, 0, DMA_STREAM);
         }
-    };
-    const std::false_type at_once;
-    const std::true_type in_turn;
+    }
+};
 
-    const uint32_t kring = ring, vring = ring + R::BYTES;
+// A wave's walk over its units of piece p, the first of which is on its way; at its end the first unit of piece `then` is, whose
+// page ids it leaves in ids.  Loads return in order, so the counts below say which of them have: a unit's keys once no more
+// than the loads of its values are left, its values once no more than those of the next unit's keys are.
+// A function of its own with restricted pointers, LDS by whole addresses: the compiler otherwise takes the reads of LDS to
+// depend on every load on its way to it.
+template <int D, int NT>
+__device__ __forceinline__ void walk_units(const char* __restrict__ k, const char* __restrict__ v, const int32_t* __restrict__ table, const Stream<D>& st,
+                                           const Piece& p, int kvh, const Piece& then, int then_kvh, const bf16x8 (&q)[NT][D / 32], float scale, int& ids,
+                                           UnitRef& cur, Acc<D, NT>& acc)
+{
+    using R = Rows<D>;
+    constexpr int LPU = R::LPU;
+    static_assert(FLIGHT <= 2 * LPU, "");
+    const int lane = st.lane, c16 = lane & 15, quad = lane >> 4;
     int koff[D / 32], voff[D / 16];
 #pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) koff[ks] = (int)kring + c16 * D * 2 + (((4 * ks + quad) ^ R::ksw(c16)) * 16);
+    for (int ks = 0; ks < D / 32; ++ks) koff[ks] = (int)st.kring + c16 * D * 2 + (((4 * ks + quad) ^ R::ksw(c16)) * 16);
     const int vrow = 4 * quad + (c16 >> 2);
 #pragma unroll
-    for (int cb = 0; cb < D / 16; ++cb) voff[cb] = (int)vring + vrow * D * 2 + ((cb ^ R::vsw(vrow)) * 32) + (c16 & 3) * 8;
+    for (int cb = 0; cb < D / 16; ++cb) voff[cb] = (int)st.vring + vrow * D * 2 + ((cb ^ R::vsw(vrow)) * 32) + (c16 & 3) * 8;
     LDS_AS const char* lds = (LDS_AS const char*)(uintptr_t)0;
 
-    int ids = fetch_ids(0);
-    uint64_t none = __ballot(ids < 0);
-    UnitRef cur = ref(0, none);
-    issue(k, dk, cur, ids, kring, false, at_once);
-    issue(v, dv, cur, ids, vring, true, at_once);
-    for (int t = 0; t < n_own; ++t) {
-        const bool more = t + 1 < n_own;
+    const int n_own = p.own(st.wave), n_then = then.own(st.wave);
+    int ids_then = st.fetch_ids(table, then, 0);
+    int t = 0;
+    do { // a wave without units in this piece comes by once for the next one's sake; cur.seen is 0 then
         UnitRef next = cur;
-        if (more) {
-            if (((t + 1) & (refill - 1)) == 0) {
-                ids = fetch_ids(t + 1);
-                none = __ballot(ids < 0);
-            }
-            next = ref(t + 1, none);
+        const bool last = t + 1 >= n_own, more = !last || n_then > 0;
+        if (!last) {
+            if (((t + 1) & (st.refill() - 1)) == 0) ids = st.checked(st.fetch_ids(table, p, t + 1));
+            next = st.ref(p, kvh, t + 1, ids);
+        } else {
+            ids = st.checked(ids_then);
+            next = st.ref(then, then_kvh, 0, ids);
+            if (!more) next.seen = 0;
         }
         wait_vm<LPU>(); // K(t)
         asm volatile("" ::: "memory");
@@ -217,6 +251,7 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
 #pragma unroll
             for (int ks = 0; ks < D / 32; ++ks) ka[kb][ks] = *(LDS_AS const bf16x8*)(lds + koff[ks] + kb * 16 * D * 2);
         wait_lds(); // the unit's keys are read
+        if (more) st.template issue<false, true>(k, next, ids);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -224,7 +259,6 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
                     s[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[kb][ks], q[n][ks], ks == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[n][kb], 0, 0, 0);
-        if (more) issue(k, dk, next, ids, kring, false, in_turn);
         // element e of block kb is key 16 kb + 4 quad + e of the unit
         if (cur.seen != 0xffffffffu) {
             const uint32_t mine = cur.seen >> (4 * quad);
@@ -255,10 +289,10 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[n][i >> 2][i & 3], scale, -acc.m[n]));
-                sum += p;
-                hi[n][i] = (__bf16)p;
-                lo[n][i] = (__bf16)(p - (float)hi[n][i]);
+                const float w = __builtin_amdgcn_exp2f(fmaf(s[n][i >> 2][i & 3], scale, -acc.m[n]));
+                sum += w;
+                hi[n][i] = (__bf16)w;
+                lo[n][i] = (__bf16)(w - (float)hi[n][i]);
             }
             acc.l[n] += sum;
         }
@@ -273,8 +307,19 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             va[cb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
         }
         wait_lds(); // the unit's values are read
-        if (more) issue(v, dv, next, ids, vring, true, in_turn);
-        if (cur.seen) { // else: values that are nobody's, for weights of zero
+        if (more) st.template issue<true, true>(v, next, ids);
+        if (cur.seen != 0xffffffffu) { // what is not seen may be anything, and even a weight of zero would make NaN of NaN
+            const uint32_t mine = cur.seen >> (4 * quad);
+            u32x4 keep; // element j of an operand is key 16 (j >> 2) + 4 quad + (j & 3)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int bit = 16 * (i >> 1) + 2 * (i & 1);
+                keep[i] = ((mine >> bit) & 1 ? 0xffffu : 0u) | ((mine >> bit) & 2 ? 0xffff0000u : 0u);
+            }
+#pragma unroll
+            for (int cb = 0; cb < D / 16; ++cb) va[cb] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, va[cb]) & keep);
+        }
+        {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -284,26 +329,24 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
                 }
         }
         cur = next;
-    }
+    } while (++t < n_own);
 }
 
-template <int D, int NT> constexpr int park_row_bytes() { return D * 4 + 16; }
-template <int D, int NT> constexpr int lds_bytes()
-{
-    const int ring = NW * 2 * Rows<D>::BYTES, park = NW * 16 * NT * park_row_bytes<D, NT>();
-    return (ring > park ? ring : park) + NW * 16 * NT * 8;
-}
+// LDS: the waves' rings, and the rows that they park to be joined (only the rows there are, at most 16 NT).
+template <int D> constexpr int PARK_ROW_BYTES = D * 4 + 16;
+template <int D> constexpr int RING_BYTES = NW * 2 * Rows<D>::BYTES;
+template <int D> constexpr int lds_bytes(int rows) { return RING_BYTES<D> + NW * rows * (PARK_ROW_BYTES<D> + 8); }
 
 template <int D, int NT>
-__global__ __launch_bounds__(64 * NW, 2) void paged_decode_kernel(const TrPagedDecodeArgs a)
+__global__ __launch_bounds__(64 * NW, NT == 1 ? 2 : 1) void paged_decode_kernel(const TrPagedDecodeArgs a)
 {
-    constexpr int ROWS = 16 * NT, ROWB = park_row_bytes<D, NT>();
+    constexpr int ROWS = 16 * NT, ROWB = PARK_ROW_BYTES<D>;
     extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
     LDS_AS char* smem = (LDS_AS char*)smem_raw;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c16 = lane & 15, quad = lane >> 4;
     const int tiles = (a.group + ROWS - 1) / ROWS, per_req = a.n_kv_heads * tiles; // items of a request
-    const int worker = blockIdx.x;
+    const int worker = blockIdx.x, park_rows = a.ws_rows;
 
     // the batch's steps, and the request that this worker's share begins in
     auto len_of = [&](int r) { return r < a.n_req ? a.kv_lens[r] : 0; };
@@ -316,7 +359,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_decode_kernel(const TrPagedD
     const int begin = share * worker;
     if (begin >= total) return;
     const int end = min(begin + share, total);
-    int left = end - begin;
+    int left = end - begin; // behind the pieces described so far
     const int step = begin / per_req; // in steps of all heads together
     int before = 0, r0 = 0;
     while (before + __builtin_amdgcn_readlane(sums, 63) <= step && r0 + 64 < a.n_req) {
@@ -325,29 +368,61 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_decode_kernel(const TrPagedD
         lens = len_of(r0 + lane), own = steps_of(r0 + lane, lens), sums = wave_scan(own);
     }
     const int at = __builtin_ctzll(__ballot(before + sums > step));
-    int r = r0 + at;
     before += __builtin_amdgcn_readlane(sums, at) - __builtin_amdgcn_readlane(own, at);
-    Walk w = walk_of(a, __builtin_amdgcn_readlane(lens, at));
-    int steps = w.steps();
-    const int local = begin - before * per_req;
-    int item = uniform(local / steps), step0 = local - item * steps;
 
-    while (true) {
-        const int n = min(steps - step0, left);
-        const int kvh = uniform(item / tiles), tile = item - kvh * tiles;
-        const int head0 = kvh * a.group + tile * ROWS, rows = min(a.group - tile * ROWS, ROWS);
-        bf16x8 q[NT][D / 32];
+    Piece p;
+    p.r = r0 + at;
+    p.w = walk_of(a, __builtin_amdgcn_readlane(lens, at));
+    p.steps = p.w.steps();
+    const int local = begin - before * per_req;
+    p.item = uniform(local / p.steps);
+    p.step0 = local - p.item * p.steps;
+    p.n = min(p.steps - p.step0, left);
+    left -= p.n;
+    auto following = [&](const Piece& from) {
+        Piece x = from;
+        x.step0 = x.n = 0;
+        if (left == 0) return x;
+        if (++x.item == per_req) {
+            x.item = 0;
+            if (++x.r == a.n_req) { // not reached unless the lengths are written meanwhile
+                left = 0;
+                return x;
+            }
+            int len;
+            if (x.r < r0 + 64) len = __builtin_amdgcn_readlane(lens, x.r - r0);
+            else len = uniform(a.kv_lens[x.r]);
+            x.w = walk_of(a, len);
+            x.steps = x.w.steps();
+        }
+        x.n = min(x.steps, left);
+        left -= x.n;
+        return x;
+    };
+    bf16x8 q[NT][D / 32];
+    auto load_q = [&](const Piece& x) { // columns without a query head repeat one: nothing of theirs is looked at
+        const int kvh = x.item / tiles, tile = x.item - kvh * tiles, rows = min(a.group - tile * ROWS, ROWS);
+        const __bf16* const first = (const __bf16*)a.q + ((int64_t)x.r * a.n_q_heads + kvh * a.group + tile * ROWS) * D + 8 * quad;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) {
-                bf16x8 x;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = (__bf16)0.0f;
-                if (16 * t + c16 < rows)
-                    x = *(const bf16x8*)((const __bf16*)a.q + ((int64_t)r * a.n_q_heads + head0 + 16 * t + c16) * D + 32 * ks + 8 * quad);
-                q[t][ks] = x;
-            }
+            for (int ks = 0; ks < D / 32; ++ks) q[t][ks] = *(const bf16x8*)(first + min(16 * t + c16, rows - 1) * D + 32 * ks);
+    };
+
+    Stream<D> st(a, (uint32_t)(uintptr_t)(smem + wave * 2 * Rows<D>::BYTES), wave, lane);
+    load_q(p);
+    int kvh = uniform(p.item / tiles);
+    int ids = st.checked(st.fetch_ids(a.table, p, 0));
+    UnitRef cur = st.ref(p, kvh, 0, ids);
+    if (p.own(wave) > 0) {
+        st.template issue<false, false>(a.pool.k, cur, ids);
+        st.template issue<true, false>(a.pool.v, cur, ids);
+    } else {
+        cur.seen = 0;
+    }
+    while (true) {
+        const Piece then = following(p);
+        const int then_kvh = uniform(then.item / tiles);
         Acc<D, NT> acc;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -355,73 +430,68 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_decode_kernel(const TrPagedD
             acc.l[t] = 0.0f;
 #pragma unroll
             for (int cb = 0; cb < D / 16; ++cb) acc.o[t][cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) asm volatile("" : "+v"(q[t][ks])); // waited for here and not at each use in the walk
         }
-        const int64_t head = kvh * a.pool.head_stride;
-        walk_units<D, NT>(a.pool.k + head, a.pool.v + head, a.table + (int64_t)r * a.max_blocks, a.pool, w, q, NW * step0, min(NW * (step0 + n), w.units),
-                          a.scale_log2e, (uint32_t)(uintptr_t)(smem + wave * 2 * Rows<D>::BYTES), wave, lane, acc);
+        walk_units<D, NT>(a.pool.k, a.pool.v, a.table, st, p, kvh, then, then_kvh, q, a.scale_log2e, ids, cur, acc);
+        if (then.n) load_q(then);
 
-        // join the four waves' keys: every wave parks its sums where the rings were
-        __syncthreads();
-        LDS_AS char* park = smem + wave * ROWS * ROWB;
-        LDS_AS float* ml = (LDS_AS float*)(smem + lds_bytes<D, NT>() - NW * ROWS * 8);
+        // join the four waves' keys: every wave parks its sums
+        const int tile = p.item - kvh * tiles, head0 = kvh * a.group + tile * ROWS, rows = min(a.group - tile * ROWS, ROWS);
+        LDS_AS char* const parked = smem + RING_BYTES<D>;
+        LDS_AS float* ml = (LDS_AS float*)(parked + NW * park_rows * ROWB);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const float l = column_reduce<false>(acc.l[t]);
             if (16 * t + c16 < rows) {
+                const int row = wave * park_rows + 16 * t + c16;
 #pragma unroll
-                for (int cb = 0; cb < D / 16; ++cb) *(LDS_AS f32x4*)(park + (16 * t + c16) * ROWB + (16 * cb + 4 * quad) * 4) = acc.o[t][cb];
+                for (int cb = 0; cb < D / 16; ++cb) *(LDS_AS f32x4*)(parked + row * ROWB + (16 * cb + 4 * quad) * 4) = acc.o[t][cb];
                 if (quad == 0) {
-                    ml[(wave * ROWS + 16 * t + c16) * 2] = acc.m[t];
-                    ml[(wave * ROWS + 16 * t + c16) * 2 + 1] = l;
+                    ml[row * 2] = acc.m[t];
+                    ml[row * 2 + 1] = l;
                 }
             }
         }
-        __syncthreads();
-        const bool whole = step0 == 0 && n == steps;
+        sync_lds();
         constexpr int LPR = D / 8; // threads of a row, eight channels each
         for (int row = tid / LPR; row < rows; row += 64 * NW / LPR) {
             const int ch = tid % LPR * 8;
             float mw[NW], M = NOTHING, L = 0.0f, o[8];
 #pragma unroll
-            for (int i = 0; i < NW; ++i) M = fmaxf(M, mw[i] = ml[(i * ROWS + row) * 2]);
+            for (int i = 0; i < NW; ++i) M = fmaxf(M, mw[i] = ml[(i * park_rows + row) * 2]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = 0.0f;
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
                 const float f = __builtin_amdgcn_exp2f(mw[i] - M);
-                L = fmaf(f, ml[(i * ROWS + row) * 2 + 1], L);
-                const f32x4 x = *(LDS_AS const f32x4*)(smem + i * ROWS * ROWB + row * ROWB + ch * 4);
-                const f32x4 y = *(LDS_AS const f32x4*)(smem + i * ROWS * ROWB + row * ROWB + ch * 4 + 16);
+                L = fmaf(f, ml[(i * park_rows + row) * 2 + 1], L);
+                const f32x4 x = *(LDS_AS const f32x4*)(parked + (i * park_rows + row) * ROWB + ch * 4);
+                const f32x4 y = *(LDS_AS const f32x4*)(parked + (i * park_rows + row) * ROWB + ch * 4 + 16);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[e], o[e]), o[4 + e] = fmaf(f, y[e], o[4 + e]);
             }
-            if (whole) {
+            if (p.whole()) {
                 const float inv = L == 0.0f ? 0.0f : 1.0f / L; // a row without any weight is zero
                 bf16x8 y;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = (__bf16)(o[e] * inv);
-                *(bf16x8*)((__bf16*)a.out + ((int64_t)r * a.n_q_heads + head0 + row) * D + ch) = y;
+                *(bf16x8*)((__bf16*)a.out + ((int64_t)p.r * a.n_q_heads + head0 + row) * D + ch) = y;
             } else {
-                const int64_t slot = (int64_t)(2 * worker + (step0 == 0)) * a.ws_rows + row; // a share cuts at most its first and its last item
+                const int64_t slot = (int64_t)(2 * worker + (p.step0 == 0)) * a.ws_rows + row; // a share cuts at most its first and its last item
                 *(f32x4*)(a.ws_o + slot * D + ch) = f32x4{o[0], o[1], o[2], o[3]};
                 *(f32x4*)(a.ws_o + slot * D + ch + 4) = f32x4{o[4], o[5], o[6], o[7]};
                 if (ch == 0) *(float2*)(a.ws_ml + slot * 2) = make_float2(M, L);
             }
         }
-        if (a.cut && step0 == 0 && tid == 0) { // who begins an item says who else has a piece of it
-            const int pieces = whole ? 1 : (end - left + steps - 1) / share - worker + 1;
-            *(int2*)(a.ws_items + 2 * ((int64_t)r * per_req + item)) = make_int2(worker, pieces);
+        if (a.cut && p.step0 == 0 && tid == 0) { // who begins an item says who else has a piece of it
+            const int pieces = p.whole() ? 1 : (end - left - then.n - p.n + p.steps - 1) / share - worker + 1;
+            *(int2*)(a.ws_items + 2 * ((int64_t)p.r * per_req + p.item)) = make_int2(worker, pieces);
         }
-        left -= n;
-        if (left == 0) break;
-        step0 = 0;
-        if (++item == per_req) {
-            item = 0;
-            if (++r == a.n_req) break; // not reached unless the lengths are written meanwhile
-            w = walk_of(a, uniform(a.kv_lens[r]));
-            steps = w.steps();
-        }
-        __syncthreads(); // the parked sums are read
+        if (then.n == 0) break;
+        p = then;
+        kvh = then_kvh;
+        sync_lds(); // the parked sums are read
     }
 }
 
@@ -494,8 +564,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs
 template <int D, int NT> int launch_decode(const TrPagedDecodeArgs& a, int grid, hipStream_t s)
 {
     static std::atomic<uint64_t> raised{0};
-    constexpr int lds = lds_bytes<D, NT>();
-    if (const int rc = tr_raise_lds_limit((const void*)paged_decode_kernel<D, NT>, lds, &raised)) return rc;
+    if (const int rc = tr_raise_lds_limit((const void*)paged_decode_kernel<D, NT>, lds_bytes<D>(16 * NT), &raised)) return rc;
+    const int lds = lds_bytes<D>(a.ws_rows);
     paged_decode_kernel<D, NT><<<dim3(grid), dim3(64 * NW), lds, s>>>(a);
     TR_HIP(hipGetLastError());
     if (a.cut) {
