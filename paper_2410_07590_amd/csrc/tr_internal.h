@@ -425,10 +425,10 @@ struct TrPagedAppendArgs {
     float eps, amplitude;
     double freq[64];
 };
-// Decode: each of TR_PAGED_WORKERS workgroups takes an equal share of the batch's steps, of at least TR_PAGED_MIN_STEPS.
-#define TR_PAGED_STEP_KEYS 128
-#define TR_PAGED_WORKERS 512
-#define TR_PAGED_MIN_STEPS 1
+// Decode: each of TR_PAGED_WORKERS waves takes an equal share of the batch's units, of at least TR_PAGED_MIN_UNITS.
+#define TR_PAGED_UNIT_KEYS 32
+#define TR_PAGED_WORKERS 1024
+#define TR_PAGED_MIN_UNITS 1
 static inline int tr_paged_tile_rows(int group) { return group <= 16 ? 16 : 32; }
 struct TrPagedDecodeArgs {
     const void* q;
@@ -439,7 +439,7 @@ struct TrPagedDecodeArgs {
     int32_t n_req, max_blocks, window, n_sink;
     int32_t n_q_heads, n_kv_heads, group;
     float scale_log2e; // log2(e) / sqrt(head_dim)
-    int32_t workers;   // shares; not the number of workgroups, which may be fewer where the table bounds the work
+    int32_t workers;   // shares; not the number of waves, which may be fewer where the table bounds the work
     int32_t cut;       // items may be cut: a second launch joins their pieces
     int32_t ws_rows;   // rows of a piece
     int32_t pad_;

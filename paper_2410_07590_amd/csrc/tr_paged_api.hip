@@ -223,7 +223,7 @@ namespace {
 // What the pieces of cut items need: sums and statistics of two pieces per worker, and who has pieces of which item.  None of it
 // depends on the lengths, which are not known here.
 struct DecodePlan {
-    int64_t items, bound; // items of the batch; most steps that they can have
+    int64_t items, bound; // items of the batch; most units that they can have
     int32_t ws_rows;
     size_t ml_at, items_at, bytes;
 };
@@ -232,10 +232,10 @@ DecodePlan decode_plan(const tr_shape* sh, int64_t n_req, int64_t keys)
     DecodePlan p;
     const int group = sh->n_q_heads / sh->n_kv_heads, tile = tr_paged_tile_rows(group);
     p.items = n_req * sh->n_kv_heads * ((group + tile - 1) / tile);
-    const int64_t steps = std::max<int64_t>((keys + TR_PAGED_STEP_KEYS - 1) / TR_PAGED_STEP_KEYS, 1);
-    p.bound = p.items * steps;
+    const int64_t units = std::max<int64_t>((keys + TR_PAGED_UNIT_KEYS - 1) / TR_PAGED_UNIT_KEYS, 1);
+    p.bound = p.items * units;
     p.ws_rows = std::min(group, tile);
-    const bool none = sh->dtype == TR_F32 || steps == 1; // a step is never cut
+    const bool none = sh->dtype == TR_F32 || keys <= TR_PAGED_UNIT_KEYS; // a unit is never cut
     p.ml_at = tr_align256(2ull * TR_PAGED_WORKERS * p.ws_rows * sh->head_dim * 4);
     p.items_at = p.ml_at + tr_align256(2ull * TR_PAGED_WORKERS * p.ws_rows * 8);
     p.bytes = none ? 0 : p.items_at + tr_align256((size_t)p.items * 8);
@@ -285,7 +285,7 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)shape->head_dim));
     if (shape->dtype == TR_F32) return tr_launch_paged_decode_f32(a, shape->head_dim, (hipStream_t)stream);
     const DecodePlan plan = decode_plan(shape, n_req, (int64_t)max_blocks * pages->page_size);
-    if (plan.bound > ((int64_t)1 << 30)) return tr_fail(TR_ERR_UNSUPPORTED, "%s: the table has room for more than 2^30 steps of 128 keys", who);
+    if (plan.bound > ((int64_t)1 << 30)) return tr_fail(TR_ERR_UNSUPPORTED, "%s: the table has room for more than 2^30 units of 32 keys", who);
     if (plan.bytes) {
         if (!workspace || ((uintptr_t)workspace & 255)) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace missing or not 256-byte aligned", who);
         if (workspace_bytes < plan.bytes) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace holds %zu bytes, %zu needed", who, workspace_bytes, plan.bytes);
@@ -296,7 +296,7 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     a.cut = plan.bytes != 0;
     a.ws_rows = plan.ws_rows;
     a.workers = TR_PAGED_WORKERS;
-    const int64_t workers = std::min<int64_t>((plan.bound + TR_PAGED_MIN_STEPS - 1) / TR_PAGED_MIN_STEPS, TR_PAGED_WORKERS);
+    const int64_t workers = std::min<int64_t>((plan.bound + TR_PAGED_MIN_UNITS - 1) / TR_PAGED_MIN_UNITS, TR_PAGED_WORKERS);
     return tr_launch_paged_decode_bf16(a, shape->head_dim, (int)workers, (hipStream_t)stream);
     });
 }

@@ -3,21 +3,21 @@
 // Bound by the stream of keys and values (4 g flops per 4 bytes for g query heads to a KV head), so the design is about
 // keeping requests for memory on their way on every compute unit, whatever the lengths are:
 //
-// Work.  An item is a (request, KV head, block of at most 16 NT query heads).  Its visible keys are walked in steps of 128:
-// 32 for each of the four waves, which all hold the same queries and share the keys.  The host does not know the lengths, so the
-// launch is a fixed number of workers, each of which takes an equal share of all steps of the batch, in order of items: it works
-// out the batch's sum from kv_lens and finds its own range in it.  No share is longer than another by more than a step,
-// whatever the mix of lengths, and at most the first and the last item of a share are cut.  Pieces of cut items go to the
-// workspace and a second, small launch joins them.
+// Work.  An item is a (request, KV head, block of at most 16 NT query heads).  Its visible keys are walked in units of 32 by
+// single waves that share nothing.  The host does not know the lengths, so the launch is a fixed number of waves, each of which
+// takes an equal share of all units of the batch, in order of items: it works out the batch's sum from kv_lens and finds its own
+// range in it.  No share is longer than another by more than a unit, whatever the mix of lengths, and at most the first and the
+// last item of a share are cut.  Pieces of cut items go to the workspace and a second, small launch joins them.
 //
 // Products.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, keys and values as the A operands from LDS (V through
 // the transposing read), so that a lane owns one query column: its maximum and denominator are scalars, and its share of S^T
 // is, up to the order of the keys, its B operand of the second product.  The weights go into it as two bf16 parts, which
 // keeps 16 bits of them: the matrix unit is idle most of the time, and the result is as exact as fp32 weights would give.
 //
-// Data movement.  Each wave has room for one unit (32 rows) of K and of V and refills them as soon as their operands
-// are read, straight from memory to LDS, counted waits instead of barriers.  A page id is needed for every 8 rows at the most: a wave
-// keeps the ids of its next units in one register, a lane each, and takes them out as scalars.
+// Data movement.  A wave has room for one unit of K and of V and refills them as soon as their operands are read, straight
+// from memory to LDS, counted waits instead of barriers; the first unit of its next item is on its way before it is done with
+// the last one of this.  A page id is needed for every 8 rows at the most: a wave keeps the ids of its next units in one
+// register, a lane each, and takes them out as scalars.
 #include "tr_device.h"
 #include "tr_internal.h"
 
@@ -27,9 +27,10 @@
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int NW = 4, UNIT = 32, STEP = NW * UNIT; // waves, keys of a wave, keys of a step
-static_assert(STEP == TR_PAGED_STEP_KEYS, "");
+constexpr int UNIT = TR_PAGED_UNIT_KEYS;
+static_assert(UNIT == 32, "");
 constexpr float SLACK = 8.0f;        // log2 units by which a score may exceed the reference before it moves
 constexpr float NOTHING = -3.0e38f;  // reference of a row that has seen no key
 constexpr int DMA_STREAM = 2;        // non-temporal: every key is read once
@@ -53,8 +54,7 @@ __device__ __forceinline__ int wave_scan(int x)
 
 // The keys of a request as units of 32: the first `su` hold the sinks, the others run from unit `lu` to the end.
 struct Walk {
-    int len, lo, sink, su, lu, units;
-    __device__ __forceinline__ int steps() const { return max((units + NW - 1) / NW, 1); } // at least one, which writes the result
+    int len, lo, sink, su, lu, units; // at least one unit, which writes the result
     __device__ __forceinline__ int unit(int i) const { return i < su ? i : i - su + lu; }
     __device__ __forceinline__ uint32_t seen(int first_key) const // bit b: key first_key + b is visible
     {
@@ -69,16 +69,8 @@ __device__ __forceinline__ Walk walk_of(const TrPagedDecodeArgs& a, int kv_len)
     w.sink = min(a.n_sink, w.lo);
     w.su = (w.sink + UNIT - 1) / UNIT;
     w.lu = max(w.lo / UNIT, w.su);
-    w.units = w.su + max((w.len + UNIT - 1) / UNIT - w.lu, 0);
+    w.units = max(w.su + max((w.len + UNIT - 1) / UNIT - w.lu, 0), 1);
     return w;
-}
-
-// A barrier behind this wave's accesses of LDS.  Loads on their way to LDS stay on their way: nobody else reads what they bring.
-__device__ __forceinline__ void sync_lds()
-{
-    wait_lds();
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
 }
 
 template <bool MAX> __device__ __forceinline__ float column_reduce(float x) // over the four lanes of a query column
@@ -111,14 +103,11 @@ struct UnitRef {
     uint32_t seen;
 };
 
-// A run of steps of one item that one worker walks.
+// A run of units of one item that one wave walks.
 struct Piece {
-    int r, item, step0, n, steps; // n == 0: there is none
+    int r, item, u0, n; // n == 0: there is none
     Walk w;
-    __device__ __forceinline__ int u0() const { return NW * step0; }
-    __device__ __forceinline__ int u1() const { return min(NW * (step0 + n), w.units); }
-    __device__ __forceinline__ int own(int wave) const { return max((u1() - u0() - wave + NW - 1) / NW, 0); } // units of a wave
-    __device__ __forceinline__ bool whole() const { return n == steps; }
+    __device__ __forceinline__ bool whole() const { return n == w.units; }
 };
 
 // What one wave accumulates: O^T (element e of block b is channel 16 b + 4 (lane / 16) + e of query column lane % 16), reference
@@ -133,12 +122,12 @@ template <int D> struct Stream {
     using R = Rows<D>;
     static constexpr int LPU = R::LPU;
     uint32_t kring, vring, row_bytes, page_bytes;
-    int wave, lane, page_shift, sub_shift, per_unit_shift, n_pages; // sub_shift: rows of a page within a unit; per_unit_shift: pages of a unit
+    int lane, page_shift, sub_shift, per_unit_shift, n_pages; // sub_shift: rows of a page within a unit; per_unit_shift: pages of a unit
     int32_t max_blocks;
     int64_t head_stride;
     uint32_t dk[LPU], dv[LPU]; // what a lane adds to the start of a unit's page for load i
 
-    __device__ __forceinline__ Stream(const TrPagedDecodeArgs& a, uint32_t ring, int wave_, int lane_) : wave(wave_), lane(lane_)
+    __device__ __forceinline__ Stream(const TrPagedDecodeArgs& a, uint32_t ring, int lane_) : lane(lane_)
     {
         kring = (uint32_t)uniform((int)ring);
         vring = kring + R::BYTES;
@@ -160,26 +149,33 @@ template <int D> struct Stream {
     }
     __device__ __forceinline__ int refill() const { return 64 >> per_unit_shift; } // units whose ids a register holds
 
-    // Page ids of the wave's units from its j0-th of a piece on, a lane each; -1 where there is none.
-    __device__ __forceinline__ int fetch_ids(const int32_t* __restrict__ table, const Piece& p, int j0) const
+    // Page ids of a piece's units from its j0-th on, a lane each; -1 where there is none.  They are requested into LDS and taken
+    // from there when they are needed: the wait for a register's load would be a wait for all keys and values behind it.
+    __device__ __forceinline__ int entry(const Piece& p, int j0) const
     {
-        const int j = j0 + (lane >> per_unit_shift), u = p.u0() + wave + NW * j;
-        const int key = p.w.unit(u) * UNIT + ((lane & ((1 << per_unit_shift) - 1)) << sub_shift);
-        int id = -1;
-        if (u < p.u1() && key < p.w.len) id = table[(int64_t)p.r * max_blocks + (key >> page_shift)];
-        return id;
+        const int j = j0 + (lane >> per_unit_shift);
+        const int key = p.w.unit(p.u0 + j) * UNIT + ((lane & ((1 << per_unit_shift) - 1)) << sub_shift);
+        return j < p.n && key < p.w.len ? key >> page_shift : -1;
     }
-    __device__ __forceinline__ int checked(int id) const
+    __device__ __forceinline__ void request_ids(const int32_t* __restrict__ table, const Piece& p, int j0) const
     {
-        if ((uint32_t)id >= (uint32_t)n_pages) id = -1;
-        asm volatile("" : "+v"(id)); // waited for here, once for many units, and not wherever an id is taken out
+        const int e = entry(p, j0);
+        if (e >= 0)
+            __builtin_amdgcn_global_load_lds((const GLB_AS void*)(table + (int64_t)p.r * max_blocks + e), (LDS_AS void*)(uintptr_t)(vring + R::BYTES), 4, 0, 0);
+    }
+    __device__ __forceinline__ int take_ids(const Piece& p, int j0) const
+    {
+        LDS_AS const int* const from = (LDS_AS const int*)(uintptr_t)(vring + R::BYTES);
+        int id = from[lane];
+        if (entry(p, j0) < 0 || (uint32_t)id >= (uint32_t)n_pages) id = -1;
+        asm volatile("" : "+v"(id) : : "memory"); // read before the next request overwrites it
         return id;
     }
     __device__ __forceinline__ UnitRef ref(const Piece& p, int kvh, int j, int ids) const
     {
         UnitRef u;
         u.head = kvh * head_stride;
-        u.key0 = uniform(p.w.unit(p.u0() + wave + NW * j) * UNIT);
+        u.key0 = uniform(p.w.unit(p.u0 + j) * UNIT);
         u.at = (j & (refill() - 1)) << per_unit_shift;
         u.seen = p.w.seen(u.key0);
         uint32_t holes = (uint32_t)(__ballot(ids < 0) >> u.at) & low_bits(1 << per_unit_shift);
@@ -191,7 +187,7 @@ template <int D> struct Stream {
         u.seen = (uint32_t)uniform((int)u.seen);
         return u;
     }
-    // LATER: not the worker's first unit: no more than FLIGHT loads on their way.  The rows of a load lie in one page; where that is
+    // LATER: not the wave's first unit: no more than FLIGHT loads on their way.  The rows of a load lie in one page; where that is
     // none, they are read from page 0, and rows behind the last key from wherever they would be: both exist, and neither is seen.
     template <bool V, bool LATER> __device__ __forceinline__ void issue(const char* __restrict__ base, const UnitRef& u, int ids) const
     {
@@ -228,22 +224,24 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
     for (int cb = 0; cb < D / 16; ++cb) voff[cb] = (int)st.vring + vrow * D * 2 + ((cb ^ R::vsw(vrow)) * 32) + (c16 & 3) * 8;
     LDS_AS const char* lds = (LDS_AS const char*)(uintptr_t)0;
 
-    const int n_own = p.own(st.wave), n_then = then.own(st.wave);
-    int ids_then = st.fetch_ids(table, then, 0);
-    int t = 0;
-    do { // a wave without units in this piece comes by once for the next one's sake; cur.seen is 0 then
-        UnitRef next = cur;
-        const bool last = t + 1 >= n_own, more = !last || n_then > 0;
+    auto request = [&](int j0) { j0 < p.n ? st.request_ids(table, p, j0) : st.request_ids(table, then, 0); };
+    request(st.refill());
+    for (int t = 0; t < p.n; ++t) {
+        UnitRef next;
+        const bool last = t + 1 == p.n, more = !last || then.n > 0;
+        if (p.n == 1) wait_vm<0>(); // with K(t), the ids
+        else wait_vm<LPU>();        // K(t); ids were requested in front of K(1)
+        asm volatile("" ::: "memory");
         if (!last) {
-            if (((t + 1) & (st.refill() - 1)) == 0) ids = st.checked(st.fetch_ids(table, p, t + 1));
+            if (((t + 1) & (st.refill() - 1)) == 0) {
+                ids = st.take_ids(p, t + 1);
+                request(t + 1 + st.refill());
+            }
             next = st.ref(p, kvh, t + 1, ids);
         } else {
-            ids = st.checked(ids_then);
+            ids = st.take_ids(then, 0);
             next = st.ref(then, then_kvh, 0, ids);
-            if (!more) next.seen = 0;
         }
-        wait_vm<LPU>(); // K(t)
-        asm volatile("" ::: "memory");
         f32x4 s[NT][2];
         bf16x8 ka[2][D / 32];
 #pragma unroll
@@ -329,59 +327,51 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
                 }
         }
         cur = next;
-    } while (++t < n_own);
+    }
 }
 
-// LDS: the waves' rings, and the rows that they park to be joined (only the rows there are, at most 16 NT).
-template <int D> constexpr int PARK_ROW_BYTES = D * 4 + 16;
-template <int D> constexpr int RING_BYTES = NW * 2 * Rows<D>::BYTES;
-template <int D> constexpr int lds_bytes(int rows) { return RING_BYTES<D> + NW * rows * (PARK_ROW_BYTES<D> + 8); }
-
 template <int D, int NT>
-__global__ __launch_bounds__(64 * NW, NT == 1 ? 2 : 1) void paged_decode_kernel(const TrPagedDecodeArgs a)
+__global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const TrPagedDecodeArgs a)
 {
-    constexpr int ROWS = 16 * NT, ROWB = PARK_ROW_BYTES<D>;
-    extern __shared__ __attribute__((aligned(1024))) char smem_raw[];
-    LDS_AS char* smem = (LDS_AS char*)smem_raw;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int c16 = lane & 15, quad = lane >> 4;
+    constexpr int ROWS = 16 * NT;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int lane = threadIdx.x, c16 = lane & 15, quad = lane >> 4;
     const int tiles = (a.group + ROWS - 1) / ROWS, per_req = a.n_kv_heads * tiles; // items of a request
-    const int worker = blockIdx.x, park_rows = a.ws_rows;
+    const int worker = blockIdx.x;
 
-    // the batch's steps, and the request that this worker's share begins in
+    // the batch's units, and the request that this wave's share begins in
     auto len_of = [&](int r) { return r < a.n_req ? a.kv_lens[r] : 0; };
-    auto steps_of = [&](int r, int len) { return r < a.n_req ? walk_of(a, len).steps() : 0; };
-    int lens = len_of(lane), own = steps_of(lane, lens), sums = wave_scan(own); // of the 64 requests from r0 on
+    auto units_of = [&](int r, int len) { return r < a.n_req ? walk_of(a, len).units : 0; };
+    int lens = len_of(lane), own = units_of(lane, lens), sums = wave_scan(own); // of the 64 requests from r0 on
     int total = __builtin_amdgcn_readlane(sums, 63);
-    for (int r0 = 64; r0 < a.n_req; r0 += 64) total += __builtin_amdgcn_readlane(wave_scan(steps_of(r0 + lane, len_of(r0 + lane))), 63);
+    for (int r0 = 64; r0 < a.n_req; r0 += 64) total += __builtin_amdgcn_readlane(wave_scan(units_of(r0 + lane, len_of(r0 + lane))), 63);
     total *= per_req;
-    const int share = max((total + a.workers - 1) / a.workers, TR_PAGED_MIN_STEPS);
+    const int share = max((total + a.workers - 1) / a.workers, TR_PAGED_MIN_UNITS);
     const int begin = share * worker;
     if (begin >= total) return;
     const int end = min(begin + share, total);
     int left = end - begin; // behind the pieces described so far
-    const int step = begin / per_req; // in steps of all heads together
+    const int unit = begin / per_req; // in units of all heads together
     int before = 0, r0 = 0;
-    while (before + __builtin_amdgcn_readlane(sums, 63) <= step && r0 + 64 < a.n_req) {
+    while (before + __builtin_amdgcn_readlane(sums, 63) <= unit && r0 + 64 < a.n_req) {
         before += __builtin_amdgcn_readlane(sums, 63);
         r0 += 64;
-        lens = len_of(r0 + lane), own = steps_of(r0 + lane, lens), sums = wave_scan(own);
+        lens = len_of(r0 + lane), own = units_of(r0 + lane, lens), sums = wave_scan(own);
     }
-    const int at = __builtin_ctzll(__ballot(before + sums > step));
+    const int at = __builtin_ctzll(__ballot(before + sums > unit));
     before += __builtin_amdgcn_readlane(sums, at) - __builtin_amdgcn_readlane(own, at);
 
     Piece p;
     p.r = r0 + at;
     p.w = walk_of(a, __builtin_amdgcn_readlane(lens, at));
-    p.steps = p.w.steps();
     const int local = begin - before * per_req;
-    p.item = uniform(local / p.steps);
-    p.step0 = local - p.item * p.steps;
-    p.n = min(p.steps - p.step0, left);
+    p.item = uniform(local / p.w.units);
+    p.u0 = local - p.item * p.w.units;
+    p.n = min(p.w.units - p.u0, left);
     left -= p.n;
     auto following = [&](const Piece& from) {
         Piece x = from;
-        x.step0 = x.n = 0;
+        x.u0 = x.n = 0;
         if (left == 0) return x;
         if (++x.item == per_req) {
             x.item = 0;
@@ -393,9 +383,8 @@ __global__ __launch_bounds__(64 * NW, NT == 1 ? 2 : 1) void paged_decode_kernel(
             if (x.r < r0 + 64) len = __builtin_amdgcn_readlane(lens, x.r - r0);
             else len = uniform(a.kv_lens[x.r]);
             x.w = walk_of(a, len);
-            x.steps = x.w.steps();
         }
-        x.n = min(x.steps, left);
+        x.n = min(x.w.units, left);
         left -= x.n;
         return x;
     };
@@ -409,17 +398,16 @@ __global__ __launch_bounds__(64 * NW, NT == 1 ? 2 : 1) void paged_decode_kernel(
             for (int ks = 0; ks < D / 32; ++ks) q[t][ks] = *(const bf16x8*)(first + min(16 * t + c16, rows - 1) * D + 32 * ks);
     };
 
-    Stream<D> st(a, (uint32_t)(uintptr_t)(smem + wave * 2 * Rows<D>::BYTES), wave, lane);
+    Stream<D> st(a, (uint32_t)(uintptr_t)(LDS_AS char*)smem, lane);
     load_q(p);
     int kvh = uniform(p.item / tiles);
-    int ids = st.checked(st.fetch_ids(a.table, p, 0));
+    st.request_ids(a.table, p, 0);
+    wait_vm<0>();
+    asm volatile("" ::: "memory");
+    int ids = st.take_ids(p, 0);
     UnitRef cur = st.ref(p, kvh, 0, ids);
-    if (p.own(wave) > 0) {
-        st.template issue<false, false>(a.pool.k, cur, ids);
-        st.template issue<true, false>(a.pool.v, cur, ids);
-    } else {
-        cur.seen = 0;
-    }
+    st.template issue<false, false>(a.pool.k, cur, ids);
+    st.template issue<true, false>(a.pool.v, cur, ids);
     while (true) {
         const Piece then = following(p);
         const int then_kvh = uniform(then.item / tiles);
@@ -436,62 +424,32 @@ __global__ __launch_bounds__(64 * NW, NT == 1 ? 2 : 1) void paged_decode_kernel(
         walk_units<D, NT>(a.pool.k, a.pool.v, a.table, st, p, kvh, then, then_kvh, q, a.scale_log2e, ids, cur, acc);
         if (then.n) load_q(then);
 
-        // join the four waves' keys: every wave parks its sums
         const int tile = p.item - kvh * tiles, head0 = kvh * a.group + tile * ROWS, rows = min(a.group - tile * ROWS, ROWS);
-        LDS_AS char* const parked = smem + RING_BYTES<D>;
-        LDS_AS float* ml = (LDS_AS float*)(parked + NW * park_rows * ROWB);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const float l = column_reduce<false>(acc.l[t]);
-            if (16 * t + c16 < rows) {
-                const int row = wave * park_rows + 16 * t + c16;
-#pragma unroll
-                for (int cb = 0; cb < D / 16; ++cb) *(LDS_AS f32x4*)(parked + row * ROWB + (16 * cb + 4 * quad) * 4) = acc.o[t][cb];
-                if (quad == 0) {
-                    ml[row * 2] = acc.m[t];
-                    ml[row * 2 + 1] = l;
-                }
-            }
-        }
-        sync_lds();
-        constexpr int LPR = D / 8; // threads of a row, eight channels each
-        for (int row = tid / LPR; row < rows; row += 64 * NW / LPR) {
-            const int ch = tid % LPR * 8;
-            float mw[NW], M = NOTHING, L = 0.0f, o[8];
-#pragma unroll
-            for (int i = 0; i < NW; ++i) M = fmaxf(M, mw[i] = ml[(i * park_rows + row) * 2]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < NW; ++i) {
-                const float f = __builtin_amdgcn_exp2f(mw[i] - M);
-                L = fmaf(f, ml[(i * park_rows + row) * 2 + 1], L);
-                const f32x4 x = *(LDS_AS const f32x4*)(parked + (i * park_rows + row) * ROWB + ch * 4);
-                const f32x4 y = *(LDS_AS const f32x4*)(parked + (i * park_rows + row) * ROWB + ch * 4 + 16);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[e], o[e]), o[4 + e] = fmaf(f, y[e], o[4 + e]);
-            }
+            const int row = 16 * t + c16;
+            if (row >= rows) continue;
             if (p.whole()) {
-                const float inv = L == 0.0f ? 0.0f : 1.0f / L; // a row without any weight is zero
-                bf16x8 y;
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l; // a row without any weight is zero
+                __bf16* const to = (__bf16*)a.out + ((int64_t)p.r * a.n_q_heads + head0 + row) * D + 4 * quad;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = (__bf16)(o[e] * inv);
-                *(bf16x8*)((__bf16*)a.out + ((int64_t)p.r * a.n_q_heads + head0 + row) * D + ch) = y;
+                for (int cb = 0; cb < D / 16; ++cb) *(bf16x4*)(to + 16 * cb) = __builtin_convertvector(acc.o[t][cb] * inv, bf16x4);
             } else {
-                const int64_t slot = (int64_t)(2 * worker + (p.step0 == 0)) * a.ws_rows + row; // a share cuts at most its first and its last item
-                *(f32x4*)(a.ws_o + slot * D + ch) = f32x4{o[0], o[1], o[2], o[3]};
-                *(f32x4*)(a.ws_o + slot * D + ch + 4) = f32x4{o[4], o[5], o[6], o[7]};
-                if (ch == 0) *(float2*)(a.ws_ml + slot * 2) = make_float2(M, L);
+                const int64_t slot = (int64_t)(2 * worker + (p.u0 == 0)) * a.ws_rows + row; // a share cuts at most its first and its last item
+                float* const to = a.ws_o + slot * D + 4 * quad;
+#pragma unroll
+                for (int cb = 0; cb < D / 16; ++cb) *(f32x4*)(to + 16 * cb) = acc.o[t][cb];
+                if (quad == 0) *(float2*)(a.ws_ml + slot * 2) = make_float2(acc.m[t], l);
             }
         }
-        if (a.cut && p.step0 == 0 && tid == 0) { // who begins an item says who else has a piece of it
-            const int pieces = p.whole() ? 1 : (end - left - then.n - p.n + p.steps - 1) / share - worker + 1;
+        if (a.cut && p.u0 == 0 && lane == 0) { // who begins an item says who else has a piece of it
+            const int pieces = p.whole() ? 1 : (end - left - then.n - p.n + p.w.units - 1) / share - worker + 1;
             *(int2*)(a.ws_items + 2 * ((int64_t)p.r * per_req + p.item)) = make_int2(worker, pieces);
         }
         if (then.n == 0) break;
         p = then;
         kvh = then_kvh;
-        sync_lds(); // the parked sums are read
     }
 }
 
@@ -554,7 +512,6 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs
         for (int e = 0; e < 4; ++e) y[e] = fmaf(f, os[g][piece][e], y[e]);
     }
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     bf16x4 z;
 #pragma unroll
     for (int e = 0; e < 4; ++e) z[e] = (__bf16)(y[e] * inv);
@@ -563,10 +520,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs
 
 template <int D, int NT> int launch_decode(const TrPagedDecodeArgs& a, int grid, hipStream_t s)
 {
-    static std::atomic<uint64_t> raised{0};
-    if (const int rc = tr_raise_lds_limit((const void*)paged_decode_kernel<D, NT>, lds_bytes<D>(16 * NT), &raised)) return rc;
-    const int lds = lds_bytes<D>(a.ws_rows);
-    paged_decode_kernel<D, NT><<<dim3(grid), dim3(64 * NW), lds, s>>>(a);
+    // LDS for as many waves as a compute unit is meant to run: they then spread evenly over the chip
+    constexpr int lds = 160 * 1024 / (TR_PAGED_WORKERS / TrChip::CUS);
+    static_assert(lds >= 2 * Rows<D>::BYTES + 256 && lds <= 64 * 1024, "");
+    paged_decode_kernel<D, NT><<<dim3(grid), dim3(64), lds, s>>>(a);
     TR_HIP(hipGetLastError());
     if (a.cut) {
         paged_join_kernel<D><<<dim3(a.n_req * a.n_q_heads), dim3(256), 0, s>>>(a, 16 * NT);
