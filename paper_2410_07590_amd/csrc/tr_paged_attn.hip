@@ -29,6 +29,8 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
+#define CONST_AS __attribute__((address_space(4)))
+
 constexpr int UNIT = TR_PAGED_UNIT_KEYS;
 static_assert(UNIT == 32, "");
 constexpr float SLACK = 8.0f;        // log2 units by which a score may exceed the reference before it moves
@@ -105,7 +107,8 @@ struct UnitRef {
 
 // A run of units of one item that one wave walks.
 struct Piece {
-    int r, item, u0, n; // n == 0: there is none
+    int r, item, u0, n; // item: which of the request's; n == 0: there is none
+    int kvh, tile;      // what it is an item of
     Walk w;
     __device__ __forceinline__ bool whole() const { return n == w.units; }
 };
@@ -121,7 +124,7 @@ template <int D, int NT> struct Acc {
 template <int D> struct Stream {
     using R = Rows<D>;
     static constexpr int LPU = R::LPU;
-    uint32_t kring, vring, row_bytes, page_bytes;
+    uint32_t kring, vring, idring, qring, row_bytes, page_bytes;
     int lane, page_shift, sub_shift, per_unit_shift, n_pages; // sub_shift: rows of a page within a unit; per_unit_shift: pages of a unit
     int32_t max_blocks;
     int64_t head_stride;
@@ -131,6 +134,8 @@ template <int D> struct Stream {
     {
         kring = (uint32_t)uniform((int)ring);
         vring = kring + R::BYTES;
+        idring = vring + R::BYTES;
+        qring = idring + 256;
         row_bytes = (uint32_t)a.pool.row_stride;
         page_bytes = (uint32_t)a.pool.page_stride;
         head_stride = a.pool.head_stride;
@@ -161,20 +166,38 @@ template <int D> struct Stream {
     {
         const int e = entry(p, j0);
         if (e >= 0)
-            __builtin_amdgcn_global_load_lds((const GLB_AS void*)(table + (int64_t)p.r * max_blocks + e), (LDS_AS void*)(uintptr_t)(vring + R::BYTES), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((const GLB_AS void*)(table + (int64_t)p.r * max_blocks + e), (LDS_AS void*)(uintptr_t)idring, 4, 0, 0);
     }
     __device__ __forceinline__ int take_ids(const Piece& p, int j0) const
     {
-        LDS_AS const int* const from = (LDS_AS const int*)(uintptr_t)(vring + R::BYTES);
+        LDS_AS const int* const from = (LDS_AS const int*)(uintptr_t)idring;
         int id = from[lane];
         if (entry(p, j0) < 0 || (uint32_t)id >= (uint32_t)n_pages) id = -1;
         asm volatile("" : "+v"(id) : : "memory"); // read before the next request overwrites it
         return id;
     }
-    __device__ __forceinline__ UnitRef ref(const Piece& p, int kvh, int j, int ids) const
+    // The query rows of an item, likewise; rows past the last one repeat it, and nothing of theirs is looked at.
+    template <int NT> __device__ __forceinline__ void request_q(const __bf16* __restrict__ first, int rows) const
+    {
+#pragma unroll
+        for (int i = 0; i < 16 * NT / R::RPI; ++i)
+            __builtin_amdgcn_global_load_lds((const GLB_AS void*)(first + min(i * R::RPI + lane / R::CPR, rows - 1) * D + lane % R::CPR * 8),
+                                             (LDS_AS void*)(uintptr_t)(qring + i * 1024), 16, 0, 0);
+    }
+    template <int NT> __device__ __forceinline__ void take_q(bf16x8 (&q)[NT][D / 32]) const
+    {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) {
+                q[t][ks] = *(LDS_AS const bf16x8*)(uintptr_t)(qring + (uint32_t)((16 * t + (lane & 15)) * D * 2 + (4 * ks + (lane >> 4)) * 16));
+                asm volatile("" : "+v"(q[t][ks]) : : "memory");
+            }
+    }
+    __device__ __forceinline__ UnitRef ref(const Piece& p, int j, int ids) const
     {
         UnitRef u;
-        u.head = kvh * head_stride;
+        u.head = p.kvh * head_stride;
         u.key0 = uniform(p.w.unit(p.u0 + j) * UNIT);
         u.at = (j & (refill() - 1)) << per_unit_shift;
         u.seen = p.w.seen(u.key0);
@@ -202,15 +225,15 @@ template <int D> struct Stream {
     }
 };
 
-// A wave's walk over its units of piece p, the first of which is on its way; at its end the first unit of piece `then` is, whose
-// page ids it leaves in ids.  Loads return in order, so the counts below say which of them have: a unit's keys once no more
+// A wave's walk over its units of piece p, the first of which is on its way; at its end the keys of the first unit of piece `then`
+// are, whose page ids and queries it leaves in ids and in LDS.  Loads return in order, so the counts below say which of them have: a unit's keys once no more
 // than the loads of its values are left, its values once no more than those of the next unit's keys are.
 // A function of its own with restricted pointers, LDS by whole addresses: the compiler otherwise takes the reads of LDS to
 // depend on every load on its way to it.
 template <int D, int NT>
 __device__ __forceinline__ void walk_units(const char* __restrict__ k, const char* __restrict__ v, const int32_t* __restrict__ table, const Stream<D>& st,
-                                           const Piece& p, int kvh, const Piece& then, int then_kvh, const bf16x8 (&q)[NT][D / 32], float scale, int& ids,
-                                           UnitRef& cur, Acc<D, NT>& acc)
+                                           const Piece& p, const Piece& then, const __bf16* __restrict__ then_q, int then_rows,
+                                           const bf16x8 (&q)[NT][D / 32], float scale, bool first, int& ids, UnitRef& cur, Acc<D, NT>& acc)
 {
     using R = Rows<D>;
     constexpr int LPU = R::LPU;
@@ -224,23 +247,28 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
     for (int cb = 0; cb < D / 16; ++cb) voff[cb] = (int)st.vring + vrow * D * 2 + ((cb ^ R::vsw(vrow)) * 32) + (c16 & 3) * 8;
     LDS_AS const char* lds = (LDS_AS const char*)(uintptr_t)0;
 
-    auto request = [&](int j0) { j0 < p.n ? st.request_ids(table, p, j0) : st.request_ids(table, then, 0); };
-    request(st.refill());
+    auto request_ids = [&](int j0) { j0 < p.n ? st.request_ids(table, p, j0) : st.request_ids(table, then, 0); };
     for (int t = 0; t < p.n; ++t) {
         UnitRef next;
         const bool last = t + 1 == p.n, more = !last || then.n > 0;
-        if (p.n == 1) wait_vm<0>(); // with K(t), the ids
-        else wait_vm<LPU>();        // K(t); ids were requested in front of K(1)
+        // K(t).  Behind the keys of a piece that is not the first there are, besides its values, the results of the last one.
+        if (t == 0 && !first) wait_vm<LPU + D / 16>();
+        else wait_vm<LPU>();
+        if (t == 0) { // in front of K(1), so that whoever waits for that has them
+            request_ids(st.refill());
+            if (then.n > 0) st.template request_q<NT>(then_q, then_rows);
+            if (last) wait_vm<0>();
+        }
         asm volatile("" ::: "memory");
         if (!last) {
             if (((t + 1) & (st.refill() - 1)) == 0) {
                 ids = st.take_ids(p, t + 1);
-                request(t + 1 + st.refill());
+                request_ids(t + 1 + st.refill());
             }
-            next = st.ref(p, kvh, t + 1, ids);
+            next = st.ref(p, t + 1, ids);
         } else {
             ids = st.take_ids(then, 0);
-            next = st.ref(then, then_kvh, 0, ids);
+            next = st.ref(then, 0, ids);
         }
         f32x4 s[NT][2];
         bf16x8 ka[2][D / 32];
@@ -249,7 +277,10 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
 #pragma unroll
             for (int ks = 0; ks < D / 32; ++ks) ka[kb][ks] = *(LDS_AS const bf16x8*)(lds + koff[ks] + kb * 16 * D * 2);
         wait_lds(); // the unit's keys are read
-        if (more) st.template issue<false, true>(k, next, ids);
+        if (more) {
+            if (t == 0) st.template issue<false, false>(k, next, ids); // not behind the requests and results above
+            else st.template issue<false, true>(k, next, ids);
+        }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -305,7 +336,7 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             va[cb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
         }
         wait_lds(); // the unit's values are read
-        if (more) st.template issue<true, true>(v, next, ids);
+        if (!last) st.template issue<true, true>(v, next, ids);
         if (cur.seen != 0xffffffffu) { // what is not seen may be anything, and even a weight of zero would make NaN of NaN
             const uint32_t mine = cur.seen >> (4 * quad);
             u32x4 keep; // element j of an operand is key 16 (j >> 2) + 4 quad + (j & 3)
@@ -367,6 +398,11 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
     const int local = begin - before * per_req;
     p.item = uniform(local / p.w.units);
     p.u0 = local - p.item * p.w.units;
+    auto place = [&](Piece& x) {
+        x.kvh = uniform(x.item / tiles);
+        x.tile = x.item - x.kvh * tiles;
+    };
+    place(p);
     p.n = min(p.w.units - p.u0, left);
     left -= p.n;
     auto following = [&](const Piece& from) {
@@ -374,43 +410,41 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
         x.u0 = x.n = 0;
         if (left == 0) return x;
         if (++x.item == per_req) {
-            x.item = 0;
-            if (++x.r == a.n_req) { // not reached unless the lengths are written meanwhile
-                left = 0;
+            if (x.r + 1 == a.n_req) { // not reached unless the lengths are written meanwhile
+                x.item = left = 0;
                 return x;
             }
+            x.item = 0;
+            ++x.r;
             int len;
             if (x.r < r0 + 64) len = __builtin_amdgcn_readlane(lens, x.r - r0);
-            else len = uniform(a.kv_lens[x.r]);
+            else len = ((const CONST_AS int32_t*)(uintptr_t)a.kv_lens)[x.r]; // through the scalar cache: no wait for what is on its way
             x.w = walk_of(a, len);
         }
+        place(x);
         x.n = min(x.w.units, left);
         left -= x.n;
         return x;
     };
-    bf16x8 q[NT][D / 32];
-    auto load_q = [&](const Piece& x) { // columns without a query head repeat one: nothing of theirs is looked at
-        const int kvh = x.item / tiles, tile = x.item - kvh * tiles, rows = min(a.group - tile * ROWS, ROWS);
-        const __bf16* const first = (const __bf16*)a.q + ((int64_t)x.r * a.n_q_heads + kvh * a.group + tile * ROWS) * D + 8 * quad;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) q[t][ks] = *(const bf16x8*)(first + min(16 * t + c16, rows - 1) * D + 32 * ks);
-    };
+    auto rows_of = [&](const Piece& x) { return min(a.group - x.tile * ROWS, ROWS); };
+    auto head0_of = [&](const Piece& x) { return (int64_t)x.r * a.n_q_heads + x.kvh * a.group + x.tile * ROWS; }; // of all heads of the batch
+    auto first_q = [&](const Piece& x) { return (const __bf16*)a.q + head0_of(x) * D; };
 
     Stream<D> st(a, (uint32_t)(uintptr_t)(LDS_AS char*)smem, lane);
-    load_q(p);
-    int kvh = uniform(p.item / tiles);
     st.request_ids(a.table, p, 0);
-    wait_vm<0>();
+    st.template request_q<NT>(first_q(p), rows_of(p));
+    wait_vm<16 * NT / Rows<D>::RPI>(); // the ids
     asm volatile("" ::: "memory");
     int ids = st.take_ids(p, 0);
-    UnitRef cur = st.ref(p, kvh, 0, ids);
+    UnitRef cur = st.ref(p, 0, ids);
     st.template issue<false, false>(a.pool.k, cur, ids);
     st.template issue<true, false>(a.pool.v, cur, ids);
-    while (true) {
+    wait_vm<2 * Rows<D>::LPU>(); // the queries
+    for (bool first = true;; first = false) {
         const Piece then = following(p);
-        const int then_kvh = uniform(then.item / tiles);
+        bf16x8 q[NT][D / 32];
+        asm volatile("" ::: "memory");
+        st.template take_q<NT>(q);
         Acc<D, NT> acc;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -418,13 +452,12 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
             acc.l[t] = 0.0f;
 #pragma unroll
             for (int cb = 0; cb < D / 16; ++cb) acc.o[t][cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) asm volatile("" : "+v"(q[t][ks])); // waited for here and not at each use in the walk
         }
-        walk_units<D, NT>(a.pool.k, a.pool.v, a.table, st, p, kvh, then, then_kvh, q, a.scale_log2e, ids, cur, acc);
-        if (then.n) load_q(then);
+        walk_units<D, NT>(a.pool.k, a.pool.v, a.table, st, p, then, first_q(then), rows_of(then), q, a.scale_log2e, first, ids, cur, acc);
+        if (then.n) st.template issue<true, false>(a.pool.v, cur, ids);
+        asm volatile("" ::: "memory");
 
-        const int tile = p.item - kvh * tiles, head0 = kvh * a.group + tile * ROWS, rows = min(a.group - tile * ROWS, ROWS);
+        const int rows = rows_of(p);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const float l = column_reduce<false>(acc.l[t]);
@@ -432,7 +465,7 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
             if (row >= rows) continue;
             if (p.whole()) {
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l; // a row without any weight is zero
-                __bf16* const to = (__bf16*)a.out + ((int64_t)p.r * a.n_q_heads + head0 + row) * D + 4 * quad;
+                __bf16* const to = (__bf16*)a.out + (head0_of(p) + row) * D + 4 * quad;
 #pragma unroll
                 for (int cb = 0; cb < D / 16; ++cb) *(bf16x4*)(to + 16 * cb) = __builtin_convertvector(acc.o[t][cb] * inv, bf16x4);
             } else {
@@ -449,7 +482,6 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
         }
         if (then.n == 0) break;
         p = then;
-        kvh = then_kvh;
     }
 }
 
@@ -522,7 +554,7 @@ template <int D, int NT> int launch_decode(const TrPagedDecodeArgs& a, int grid,
 {
     // LDS for as many waves as a compute unit is meant to run: they then spread evenly over the chip
     constexpr int lds = 160 * 1024 / (TR_PAGED_WORKERS / TrChip::CUS);
-    static_assert(lds >= 2 * Rows<D>::BYTES + 256 && lds <= 64 * 1024, "");
+    static_assert(lds >= 2 * Rows<D>::BYTES + 256 + 16 * NT * D * 2 && lds <= 64 * 1024, "");
     paged_decode_kernel<D, NT><<<dim3(grid), dim3(64), lds, s>>>(a);
     TR_HIP(hipGetLastError());
     if (a.cut) {
