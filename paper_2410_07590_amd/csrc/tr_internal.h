@@ -429,6 +429,7 @@ struct TrPagedAppendArgs {
 #define TR_PAGED_UNIT_KEYS 32
 #define TR_PAGED_WORKERS 1024
 #define TR_PAGED_MIN_UNITS 1
+enum { TR_PAGED_JOIN_BY_ROW = 1, TR_PAGED_JOIN_BY_WAVE = 2 };
 static inline int tr_paged_tile_rows(int group) { return group <= 16 ? 16 : 32; }
 struct TrPagedDecodeArgs {
     const void* q;
@@ -440,12 +441,12 @@ struct TrPagedDecodeArgs {
     int32_t n_q_heads, n_kv_heads, group;
     float scale_log2e; // log2(e) / sqrt(head_dim)
     int32_t workers;   // shares; not the number of waves, which may be fewer where the table bounds the work
-    int32_t cut;       // items may be cut: a second launch joins their pieces
+    int32_t cut;       // 0: no item can be cut; else a second launch joins their pieces: TR_PAGED_JOIN_BY_ROW, _BY_WAVE
     int32_t ws_rows;   // rows of a piece
     int32_t pad_;
     float* ws_o;       // [2 workers][ws_rows][head_dim] sums of a piece: 2 w of the item that worker w continues, 2 w + 1 of the one it begins
     float* ws_ml;      // [2 workers][ws_rows][2] reference maximum (log2 domain) and denominator
-    int32_t* ws_items; // [items][2] worker that begins an item, number of its pieces
+    int32_t* ws_items; // by row: [items][2] wave that begins an item, number of its pieces; by wave: [waves][2] item it begins and cuts, number of pieces
 };
 int tr_launch_page_map(const TrPageMapArgs& a, hipStream_t s);
 int tr_launch_paged_append(const TrPagedAppendArgs& a, int dtype, int head_dim, int layout, hipStream_t s);

@@ -238,7 +238,7 @@ DecodePlan decode_plan(const tr_shape* sh, int64_t n_req, int64_t keys)
     const bool none = sh->dtype == TR_F32 || keys <= TR_PAGED_UNIT_KEYS; // a unit is never cut
     p.ml_at = tr_align256(2ull * TR_PAGED_WORKERS * p.ws_rows * sh->head_dim * 4);
     p.items_at = p.ml_at + tr_align256(2ull * TR_PAGED_WORKERS * p.ws_rows * 8);
-    p.bytes = none ? 0 : p.items_at + tr_align256((size_t)p.items * 8);
+    p.bytes = none ? 0 : p.items_at + tr_align256((size_t)std::max<int64_t>(p.items, TR_PAGED_WORKERS) * 8);
     return p;
 }
 } // namespace
@@ -293,10 +293,13 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
         a.ws_ml = (float*)((char*)workspace + plan.ml_at);
         a.ws_items = (int32_t*)((char*)workspace + plan.items_at);
     }
-    a.cut = plan.bytes != 0;
     a.ws_rows = plan.ws_rows;
     a.workers = TR_PAGED_WORKERS;
     const int64_t workers = std::min<int64_t>((plan.bound + TR_PAGED_MIN_UNITS - 1) / TR_PAGED_MIN_UNITS, TR_PAGED_WORKERS);
+    // The join's workgroups, most of which find nothing to do, are what it costs (some 1 600 a microsecond): it looks at the rows of
+    // the result or at those that each wave may have cut, whichever are fewer (us, whole call: 512 requests of 256 rows, 32/8
+    // heads of 128, 16384 rows or 4096: 106.4, 98.6; TODO)
+    if (plan.bytes) a.cut = (int64_t)n_req * shape->n_q_heads <= workers * plan.ws_rows ? TR_PAGED_JOIN_BY_ROW : TR_PAGED_JOIN_BY_WAVE;
     return tr_launch_paged_decode_bf16(a, shape->head_dim, (int)workers, (hipStream_t)stream);
     });
 }

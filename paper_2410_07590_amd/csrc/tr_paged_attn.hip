@@ -379,7 +379,14 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
     total *= per_req;
     const int share = max((total + a.workers - 1) / a.workers, TR_PAGED_MIN_UNITS);
     const int begin = share * worker;
-    if (begin >= total) return;
+    // who has pieces of the cut items, by the item or by the wave that begins it (a share begins at most one)
+    auto record = [&](int64_t at, int x, int pieces) {
+        if (lane == 0) *(int2*)(a.ws_items + 2 * at) = make_int2(x, pieces);
+    };
+    if (begin >= total) {
+        if (a.cut == TR_PAGED_JOIN_BY_WAVE) record(worker, 0, 0);
+        return;
+    }
     const int end = min(begin + share, total);
     int left = end - begin; // behind the pieces described so far
     const int unit = begin / per_req; // in units of all heads together
@@ -476,9 +483,11 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
                 if (quad == 0) *(float2*)(a.ws_ml + slot * 2) = make_float2(acc.m[t], l);
             }
         }
-        if (a.cut && p.u0 == 0 && lane == 0) { // who begins an item says who else has a piece of it
-            const int pieces = p.whole() ? 1 : (end - left - then.n - p.n + p.w.units - 1) / share - worker + 1;
-            *(int2*)(a.ws_items + 2 * ((int64_t)p.r * per_req + p.item)) = make_int2(worker, pieces);
+        const int pieces = p.whole() || p.u0 ? 1 : (end - left - then.n - p.n + p.w.units - 1) / share - worker + 1; // of the item that begins here
+        if (a.cut == TR_PAGED_JOIN_BY_WAVE) {
+            if (then.n == 0) record(worker, p.r * per_req + p.item, pieces);
+        } else if (a.cut && p.u0 == 0) {
+            record((int64_t)p.r * per_req + p.item, worker, pieces);
         }
         if (then.n == 0) break;
         p = then;
@@ -486,7 +495,8 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
 }
 
 // Joins the pieces of cut items: out = sum_p f_p O_p / sum_p f_p l_p with f_p = 2^(m_p - max m).  One workgroup per row of the
-// result; groups of D / 4 lanes take every GROUPS-th piece and are joined through LDS.
+// result, or per row of the item that a wave of the first launch begins; groups of D / 4 lanes take every GROUPS-th piece and
+// are joined through LDS.
 template <int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs a, int rows_per_tile)
 {
@@ -494,10 +504,25 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs
     __shared__ f32x4 os[GROUPS][LPR];
     __shared__ float2 mls[GROUPS];
     const int tid = threadIdx.x, grp = tid / LPR, piece = tid % LPR;
-    const int r = blockIdx.x / a.n_q_heads, h = blockIdx.x - r * a.n_q_heads;
-    const int tiles = (a.group + rows_per_tile - 1) / rows_per_tile, kvh = h / a.group, in = h - kvh * a.group;
-    const int tile = in / rows_per_tile, row = in - tile * rows_per_tile;
-    const int2 item = *(const int2*)(a.ws_items + 2 * (((int64_t)r * a.n_kv_heads + kvh) * tiles + tile));
+    const int tiles = (a.group + rows_per_tile - 1) / rows_per_tile;
+    int2 item; // first wave, pieces
+    int row, tile, head; // row of the tile, tile of the group, head of the batch
+    if (a.cut == TR_PAGED_JOIN_BY_WAVE) {
+        const int worker = blockIdx.x / a.ws_rows;
+        item = *(const int2*)(a.ws_items + 2 * worker);
+        row = blockIdx.x - worker * a.ws_rows;
+        const int kvh = item.x / tiles; // of the batch
+        tile = item.x - kvh * tiles;
+        head = kvh * a.group + tile * rows_per_tile + row;
+        item.x = worker;
+        if (tile * rows_per_tile + row >= a.group) return;
+    } else {
+        head = blockIdx.x;
+        const int kvh = head / a.group, in = head - kvh * a.group;
+        tile = in / rows_per_tile;
+        row = in - tile * rows_per_tile;
+        item = *(const int2*)(a.ws_items + 2 * ((int64_t)kvh * tiles + tile));
+    }
     if (item.y <= 1) return;
     float M = NOTHING, L = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -547,7 +572,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs
     bf16x4 z;
 #pragma unroll
     for (int e = 0; e < 4; ++e) z[e] = (__bf16)(y[e] * inv);
-    *(bf16x4*)((__bf16*)a.out + (int64_t)blockIdx.x * D + 4 * piece) = z;
+    *(bf16x4*)((__bf16*)a.out + (int64_t)head * D + 4 * piece) = z;
 }
 
 template <int D, int NT> int launch_decode(const TrPagedDecodeArgs& a, int grid, hipStream_t s)
@@ -558,7 +583,7 @@ template <int D, int NT> int launch_decode(const TrPagedDecodeArgs& a, int grid,
     paged_decode_kernel<D, NT><<<dim3(grid), dim3(64), lds, s>>>(a);
     TR_HIP(hipGetLastError());
     if (a.cut) {
-        paged_join_kernel<D><<<dim3(a.n_req * a.n_q_heads), dim3(256), 0, s>>>(a, 16 * NT);
+        paged_join_kernel<D><<<dim3(a.cut == TR_PAGED_JOIN_BY_WAVE ? grid * a.ws_rows : a.n_req * a.n_q_heads), dim3(256), 0, s>>>(a, 16 * NT);
         TR_HIP(hipGetLastError());
     }
     return TR_OK;
