@@ -380,7 +380,7 @@ int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* 
  * workspace: tr_paged_decode_attn_workspace_size() bytes, 256-byte aligned, else TR_ERR_WORKSPACE; it depends on the arguments
  * of the query alone, not on the lengths; calls that may overlap need one each.  q, out and pages 16-byte aligned.
  * max_blocks * page_size <= 2^30; n_req <= 65536, n_req * n_q_heads < 2^24 and
- * n_req * n_q_heads * max_blocks * page_size < 2^34 (else TR_ERR_UNSUPPORTED); n_req == 0 is a no-op. */
+ * n_req * n_q_heads * max_blocks * page_size < 2^33 (else TR_ERR_UNSUPPORTED); n_req == 0 is a no-op. */
 size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size);
 int tr_paged_decode_attn(const tr_shape* shape, const void* q, const tr_pages* pages, const int32_t* block_table /*device*/,
                          int32_t max_blocks, const int32_t* kv_lens /*device*/, int32_t n_req, int32_t window, int32_t n_sink,

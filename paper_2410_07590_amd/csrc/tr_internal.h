@@ -426,7 +426,7 @@ struct TrPagedAppendArgs {
     double freq[64];
 };
 // Decode: each of TR_PAGED_WORKERS waves takes an equal share of the batch's units, of at least TR_PAGED_MIN_UNITS.
-#define TR_PAGED_UNIT_KEYS 32
+__host__ __device__ constexpr int tr_paged_unit_keys(int dtype) { return dtype == TR_BF16 ? 32 : 16; }
 #define TR_PAGED_WORKERS 1024
 #define TR_PAGED_MIN_UNITS 1
 enum { TR_PAGED_JOIN_BY_ROW = 1, TR_PAGED_JOIN_BY_WAVE = 2 };
@@ -450,5 +450,4 @@ struct TrPagedDecodeArgs {
 };
 int tr_launch_page_map(const TrPageMapArgs& a, hipStream_t s);
 int tr_launch_paged_append(const TrPagedAppendArgs& a, int dtype, int head_dim, int layout, hipStream_t s);
-int tr_launch_paged_decode_f32(const TrPagedDecodeArgs& a, int head_dim, hipStream_t s);
-int tr_launch_paged_decode_bf16(const TrPagedDecodeArgs& a, int head_dim, int grid, hipStream_t s);
+int tr_launch_paged_decode(const TrPagedDecodeArgs& a, int dtype, int head_dim, int grid, hipStream_t s);

@@ -241,66 +241,6 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const TrPagedAppendAr
     }
 }
 
-// ---- decode attention over pages ----------------------------------------------------------------------------------------------
-// One workgroup per (request, query head): groups of LPH lanes share a key, each walks its own keys and keeps its own running
-// maximum, denominator and weighted sum; the groups are merged once, through LDS.
-template <int DTYPE, int D>
-__global__ __launch_bounds__(256) void paged_decode_kernel(const TrPagedDecodeArgs a)
-{
-    using V = Vec<DTYPE>;
-    constexpr int N = V::N, LPH = D / N, GROUPS = 256 / LPH;
-    __shared__ float os[GROUPS][D];
-    __shared__ float ml[GROUPS][2];
-    const int r = blockIdx.x / a.n_q_heads, h = blockIdx.x % a.n_q_heads;
-    const int tid = threadIdx.x, grp = tid / LPH, piece = tid % LPH;
-    const int shift = a.pool.page_shift;
-    const int len = min(max(a.kv_lens[r], 0), a.max_blocks << shift);
-    float q[N], o[N];
-    V::open(((const u32x4*)a.q)[(int64_t)blockIdx.x * LPH + piece], q);
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = 0.0f;
-    float m = -INFINITY, l = 0.0f;
-    const int lo = a.window ? max(len - a.window, 0) : 0, sinks = min(a.n_sink, lo);
-    const int64_t head = (h / a.group) * a.pool.head_stride;
-    for (int i = grp; i < sinks + len - lo; i += GROUPS) {
-        const int j = i < sinks ? i : lo + i - sinks;
-        const int page = a.table[(int64_t)r * a.max_blocks + (j >> shift)];
-        if (page < 0 || page >= a.pool.n_pages) continue;
-        const int64_t at = page * a.pool.page_stride + (j & ((1 << shift) - 1)) * a.pool.row_stride + head;
-        float k[N], v[N];
-        V::open(((const u32x4*)(a.pool.k + at))[piece], k);
-        V::open(((const u32x4*)(a.pool.v + at))[piece], v);
-        float s = 0.0f;
-#pragma unroll
-        for (int e = 0; e < N; ++e) s = fmaf(q[e], k[e], s);
-        s = lanes_sum<LPH>(s) * a.scale_log2e;
-        if (s == -INFINITY) continue;
-        const float top = fmaxf(m, s), alpha = exp2f(m - top), p = exp2f(s - top);
-        l = fmaf(l, alpha, p);
-#pragma unroll
-        for (int e = 0; e < N; ++e) o[e] = fmaf(o[e], alpha, p * v[e]);
-        m = top;
-    }
-#pragma unroll
-    for (int e = 0; e < N; ++e) os[grp][piece * N + e] = o[e];
-    if (piece == 0) ml[grp][0] = m, ml[grp][1] = l;
-    __syncthreads();
-    if (grp != 0) return;
-    float M = -INFINITY, L = 0.0f, y[N];
-    for (int g = 0; g < GROUPS; ++g) M = fmaxf(M, ml[g][0]);
-#pragma unroll
-    for (int e = 0; e < N; ++e) y[e] = 0.0f;
-    for (int g = 0; g < GROUPS; ++g) {
-        const float w = ml[g][1] == 0.0f ? 0.0f : exp2f(ml[g][0] - M);
-        L = fmaf(w, ml[g][1], L);
-#pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = fmaf(w, os[g][piece * N + e], y[e]);
-    }
-#pragma unroll
-    for (int e = 0; e < N; ++e) y[e] = L == 0.0f ? 0.0f : y[e] / L;
-    ((u32x4*)a.out)[(int64_t)blockIdx.x * LPH + piece] = V::close(y);
-}
-
 } // namespace
 
 int tr_launch_page_map(const TrPageMapArgs& a, hipStream_t s)
@@ -321,14 +261,6 @@ int tr_launch_paged_append(const TrPagedAppendArgs& a, int dtype, int head_dim, 
 {
     if (dtype == TR_BF16) head_dim == 128 ? launch_append<TR_BF16, 128>(a, layout, s) : launch_append<TR_BF16, 64>(a, layout, s);
     else head_dim == 128 ? launch_append<TR_F32, 128>(a, layout, s) : launch_append<TR_F32, 64>(a, layout, s);
-    TR_HIP(hipGetLastError());
-    return TR_OK;
-}
-
-int tr_launch_paged_decode_f32(const TrPagedDecodeArgs& a, int head_dim, hipStream_t s)
-{
-    const dim3 grid(a.n_req * a.n_q_heads), block(256);
-    head_dim == 128 ? paged_decode_kernel<TR_F32, 128><<<grid, block, 0, s>>>(a) : paged_decode_kernel<TR_F32, 64><<<grid, block, 0, s>>>(a);
     TR_HIP(hipGetLastError());
     return TR_OK;
 }

@@ -232,10 +232,11 @@ DecodePlan decode_plan(const tr_shape* sh, int64_t n_req, int64_t keys)
     DecodePlan p;
     const int group = sh->n_q_heads / sh->n_kv_heads, tile = tr_paged_tile_rows(group);
     p.items = n_req * sh->n_kv_heads * ((group + tile - 1) / tile);
-    const int64_t units = std::max<int64_t>((keys + TR_PAGED_UNIT_KEYS - 1) / TR_PAGED_UNIT_KEYS, 1);
+    const int unit = tr_paged_unit_keys(sh->dtype);
+    const int64_t units = std::max<int64_t>((keys + unit - 1) / unit, 1);
     p.bound = p.items * units;
     p.ws_rows = std::min(group, tile);
-    const bool none = sh->dtype == TR_F32 || keys <= TR_PAGED_UNIT_KEYS; // a unit is never cut
+    const bool none = units == 1; // a unit is never cut
     p.ml_at = tr_align256(2ull * TR_PAGED_WORKERS * p.ws_rows * sh->head_dim * 4);
     p.items_at = p.ml_at + tr_align256(2ull * TR_PAGED_WORKERS * p.ws_rows * 8);
     p.bytes = none ? 0 : p.items_at + tr_align256((size_t)std::max<int64_t>(p.items, TR_PAGED_WORKERS) * 8);
@@ -283,9 +284,8 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     a.n_kv_heads = shape->n_kv_heads;
     a.group = shape->n_q_heads / shape->n_kv_heads;
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)shape->head_dim));
-    if (shape->dtype == TR_F32) return tr_launch_paged_decode_f32(a, shape->head_dim, (hipStream_t)stream);
     const DecodePlan plan = decode_plan(shape, n_req, (int64_t)max_blocks * pages->page_size);
-    if (plan.bound > ((int64_t)1 << 30)) return tr_fail(TR_ERR_UNSUPPORTED, "%s: the table has room for more than 2^30 units of 32 keys", who);
+    if (plan.bound > ((int64_t)1 << 30)) return tr_fail(TR_ERR_UNSUPPORTED, "%s: the table has room for more than 2^30 units of 32 (fp32: 16) keys", who);
     if (plan.bytes) {
         if (!workspace || ((uintptr_t)workspace & 255)) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace missing or not 256-byte aligned", who);
         if (workspace_bytes < plan.bytes) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace holds %zu bytes, %zu needed", who, workspace_bytes, plan.bytes);
@@ -300,6 +300,6 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     // the result or at those that each wave may have cut, whichever are fewer (us, whole call: 512 requests of 256 rows, 32/8
     // heads of 128, 16384 rows or 4096: 106.4, 98.6; TODO)
     if (plan.bytes) a.cut = (int64_t)n_req * shape->n_q_heads <= workers * plan.ws_rows ? TR_PAGED_JOIN_BY_ROW : TR_PAGED_JOIN_BY_WAVE;
-    return tr_launch_paged_decode_bf16(a, shape->head_dim, (int)workers, (hipStream_t)stream);
+    return tr_launch_paged_decode(a, shape->dtype, shape->head_dim, (int)workers, (hipStream_t)stream);
     });
 }

@@ -1,4 +1,4 @@
-// bf16 decode attention over a paged cache: one new token per request, lengths and page ids known on the GPU only.
+// Decode attention over a paged cache: one new token per request, lengths and page ids known on the GPU only.
 //
 // Bound by the stream of keys and values (4 g flops per 4 bytes for g query heads to a KV head), so the design is about
 // keeping requests for memory on their way on every compute unit, whatever the lengths are:
@@ -31,8 +31,6 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 #define CONST_AS __attribute__((address_space(4)))
 
-constexpr int UNIT = TR_PAGED_UNIT_KEYS;
-static_assert(UNIT == 32, "");
 constexpr float SLACK = 8.0f;        // log2 units by which a score may exceed the reference before it moves
 constexpr float NOTHING = -3.0e38f;  // reference of a row that has seen no key
 constexpr int DMA_STREAM = 2;        // non-temporal: every key is read once
@@ -54,18 +52,18 @@ __device__ __forceinline__ int wave_scan(int x)
     return x;
 }
 
-// The keys of a request as units of 32: the first `su` hold the sinks, the others run from unit `lu` to the end.
-struct Walk {
+// The keys of a request as units: the first `su` hold the sinks, the others run from unit `lu` to the end.
+template <int UNIT> struct Walk {
     int len, lo, sink, su, lu, units; // at least one unit, which writes the result
     __device__ __forceinline__ int unit(int i) const { return i < su ? i : i - su + lu; }
     __device__ __forceinline__ uint32_t seen(int first_key) const // bit b: key first_key + b is visible
     {
-        return low_bits(len - first_key) & (low_bits(sink - first_key) | ~low_bits(lo - first_key));
+        return low_bits(UNIT) & low_bits(len - first_key) & (low_bits(sink - first_key) | ~low_bits(lo - first_key));
     }
 };
-__device__ __forceinline__ Walk walk_of(const TrPagedDecodeArgs& a, int kv_len)
+template <int UNIT> __device__ __forceinline__ Walk<UNIT> walk_of(const TrPagedDecodeArgs& a, int kv_len)
 {
-    Walk w;
+    Walk<UNIT> w;
     w.len = min(max(kv_len, 0), a.max_blocks << a.pool.page_shift);
     w.lo = a.window ? max(w.len - a.window, 0) : 0;
     w.sink = min(a.n_sink, w.lo);
@@ -86,16 +84,22 @@ template <bool MAX> __device__ __forceinline__ float column_reduce(float x) // o
     return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 
-// Where a wave's loads of a unit go and what its lanes add to them.  Load i fills rows RPI i .. of the unit, lane after lane;
-// K: 16-byte chunk c of row r sits at c ^ ksw(r), V: 32-byte group g of row r at g ^ vsw(r), so that the reads of operands
-// spread over all banks.
-template <int D> struct Rows {
-    static constexpr int CPR = D / 8, RPI = 64 / CPR, LPU = UNIT / RPI, BYTES = UNIT * D * 2;
-    __device__ static __forceinline__ int ksw(int r) { return (r / (16 / CPR)) & (CPR - 1); }
-    __device__ static __forceinline__ int vsw(int r) { return (r / (16 / CPR)) & (CPR / 2 - 1); }
+// A unit is 8 KB of K and 8 KB of V for heads of 128 channels (half of that for 64): 32 rows of bf16 or 16 of fp32.
+// Where a wave's loads of it go: load i fills rows RPI i .. of the unit, lane after lane.  K: 16-byte chunk c of row r sits at
+// c ^ ksw(r), so that the reads of operands spread over all banks; V: bf16 32-byte group g of row r at g ^ vsw(r), for the same
+// reason, fp32 as it comes.
+template <int DTYPE, int D> struct Rows {
+    static constexpr bool BF16 = DTYPE == TR_BF16;
+    static constexpr int UNIT = tr_paged_unit_keys(DTYPE), ROW = D * (BF16 ? 2 : 4);
+    static constexpr int CPR = ROW / 16, RPI = 64 / CPR, LPU = UNIT / RPI, BYTES = UNIT * ROW;
+    __device__ static __forceinline__ int ksw(int r) { return CPR >= 16 ? r & 15 : (r / (16 / CPR)) & (CPR - 1); }
+    __device__ static __forceinline__ int vsw(int r) { return CPR >= 16 ? r & 7 : (r / (16 / CPR)) & (CPR / 2 - 1); }
     __device__ static __forceinline__ int kchunk(int row, int lane) { return (lane % CPR) ^ ksw(row); }
-    __device__ static __forceinline__ int vchunk(int row, int lane) { return (((lane % CPR) >> 1) ^ vsw(row)) * 2 + (lane & 1); }
+    __device__ static __forceinline__ int vchunk(int row, int lane) { return BF16 ? (((lane % CPR) >> 1) ^ vsw(row)) * 2 + (lane & 1) : lane % CPR; }
 };
+// What a lane holds of 16 query rows, keys or values as an operand: 16 bytes for every 64 bytes of a row.
+template <int DTYPE> struct Operand { typedef bf16x8 T; };
+template <> struct Operand<TR_F32> { typedef f32x4 T; };
 
 // One unit of a wave: where its KV head begins, its first key, which of its keys are seen, and where its page ids are among the
 // wave's.
@@ -106,24 +110,26 @@ struct UnitRef {
 };
 
 // A run of units of one item that one wave walks.
-struct Piece {
+template <int UNIT> struct Piece {
     int r, item, u0, n; // item: which of the request's; n == 0: there is none
     int kvh, tile;      // what it is an item of
-    Walk w;
+    Walk<UNIT> w;
     __device__ __forceinline__ bool whole() const { return n == w.units; }
 };
 
-// What one wave accumulates: O^T (element e of block b is channel 16 b + 4 (lane / 16) + e of query column lane % 16), reference
-// maximum (log2 domain) and this lane's share of the denominator.
+// What one wave accumulates: O^T of query column lane % 16 (bf16: element e of block b is channel 16 b + 4 (lane / 16) + e; fp32:
+// channel 64 (b / 4) + 16 (lane / 16) + 4 e + b % 4), reference maximum (log2 domain) and this lane's share of the denominator.
 template <int D, int NT> struct Acc {
     f32x4 o[NT][D / 16];
     float m[NT], l[NT];
 };
 
 // A wave's loads.
-template <int D> struct Stream {
-    using R = Rows<D>;
-    static constexpr int LPU = R::LPU;
+template <int DTYPE, int D> struct Stream {
+    using R = Rows<DTYPE, D>;
+    using P = Piece<R::UNIT>;
+    typedef typename Operand<DTYPE>::T Op;
+    static constexpr int LPU = R::LPU, UNIT = R::UNIT, UNIT_SHIFT = UNIT == 32 ? 5 : 4;
     uint32_t kring, vring, idring, qring, row_bytes, page_bytes;
     int lane, page_shift, sub_shift, per_unit_shift, n_pages; // sub_shift: rows of a page within a unit; per_unit_shift: pages of a unit
     int32_t max_blocks;
@@ -142,8 +148,8 @@ template <int D> struct Stream {
         page_shift = a.pool.page_shift;
         n_pages = a.pool.n_pages;
         max_blocks = a.max_blocks;
-        sub_shift = min(page_shift, 5);
-        per_unit_shift = 5 - sub_shift;
+        sub_shift = min(page_shift, UNIT_SHIFT);
+        per_unit_shift = UNIT_SHIFT - sub_shift;
 #pragma unroll
         for (int i = 0; i < LPU; ++i) {
             const int row = i * R::RPI + lane / R::CPR;
@@ -156,19 +162,19 @@ template <int D> struct Stream {
 
     // Page ids of a piece's units from its j0-th on, a lane each; -1 where there is none.  They are requested into LDS and taken
     // from there when they are needed: the wait for a register's load would be a wait for all keys and values behind it.
-    __device__ __forceinline__ int entry(const Piece& p, int j0) const
+    __device__ __forceinline__ int entry(const P& p, int j0) const
     {
         const int j = j0 + (lane >> per_unit_shift);
         const int key = p.w.unit(p.u0 + j) * UNIT + ((lane & ((1 << per_unit_shift) - 1)) << sub_shift);
         return j < p.n && key < p.w.len ? key >> page_shift : -1;
     }
-    __device__ __forceinline__ void request_ids(const int32_t* __restrict__ table, const Piece& p, int j0) const
+    __device__ __forceinline__ void request_ids(const int32_t* __restrict__ table, const P& p, int j0) const
     {
         const int e = entry(p, j0);
         if (e >= 0)
             __builtin_amdgcn_global_load_lds((const GLB_AS void*)(table + (int64_t)p.r * max_blocks + e), (LDS_AS void*)(uintptr_t)idring, 4, 0, 0);
     }
-    __device__ __forceinline__ int take_ids(const Piece& p, int j0) const
+    __device__ __forceinline__ int take_ids(const P& p, int j0) const
     {
         LDS_AS const int* const from = (LDS_AS const int*)(uintptr_t)idring;
         int id = from[lane];
@@ -177,24 +183,24 @@ template <int D> struct Stream {
         return id;
     }
     // The query rows of an item, likewise; rows past the last one repeat it, and nothing of theirs is looked at.
-    template <int NT> __device__ __forceinline__ void request_q(const __bf16* __restrict__ first, int rows) const
+    template <int NT> __device__ __forceinline__ void request_q(const char* __restrict__ first, int rows) const
     {
 #pragma unroll
         for (int i = 0; i < 16 * NT / R::RPI; ++i)
-            __builtin_amdgcn_global_load_lds((const GLB_AS void*)(first + min(i * R::RPI + lane / R::CPR, rows - 1) * D + lane % R::CPR * 8),
+            __builtin_amdgcn_global_load_lds((const GLB_AS void*)(first + min(i * R::RPI + lane / R::CPR, rows - 1) * R::ROW + lane % R::CPR * 16),
                                              (LDS_AS void*)(uintptr_t)(qring + i * 1024), 16, 0, 0);
     }
-    template <int NT> __device__ __forceinline__ void take_q(bf16x8 (&q)[NT][D / 32]) const
+    template <int NT> __device__ __forceinline__ void take_q(Op (&q)[NT][R::ROW / 64]) const
     {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) {
-                q[t][ks] = *(LDS_AS const bf16x8*)(uintptr_t)(qring + (uint32_t)((16 * t + (lane & 15)) * D * 2 + (4 * ks + (lane >> 4)) * 16));
+            for (int ks = 0; ks < R::ROW / 64; ++ks) {
+                q[t][ks] = *(LDS_AS const Op*)(uintptr_t)(qring + (uint32_t)((16 * t + (lane & 15)) * R::ROW + (4 * ks + (lane >> 4)) * 16));
                 asm volatile("" : "+v"(q[t][ks]) : : "memory");
             }
     }
-    __device__ __forceinline__ UnitRef ref(const Piece& p, int j, int ids) const
+    __device__ __forceinline__ UnitRef ref(const P& p, int j, int ids) const
     {
         UnitRef u;
         u.head = p.kvh * head_stride;
@@ -230,21 +236,26 @@ template <int D> struct Stream {
 // than the loads of its values are left, its values once no more than those of the next unit's keys are.
 // A function of its own with restricted pointers, LDS by whole addresses: the compiler otherwise takes the reads of LDS to
 // depend on every load on its way to it.
-template <int D, int NT>
-__device__ __forceinline__ void walk_units(const char* __restrict__ k, const char* __restrict__ v, const int32_t* __restrict__ table, const Stream<D>& st,
-                                           const Piece& p, const Piece& then, const __bf16* __restrict__ then_q, int then_rows,
-                                           const bf16x8 (&q)[NT][D / 32], float scale, bool first, int& ids, UnitRef& cur, Acc<D, NT>& acc)
+template <int DTYPE, int D, int NT>
+__device__ __forceinline__ void walk_units(const char* __restrict__ k, const char* __restrict__ v, const int32_t* __restrict__ table,
+                                           const Stream<DTYPE, D>& st, const Piece<Rows<DTYPE, D>::UNIT>& p, const Piece<Rows<DTYPE, D>::UNIT>& then,
+                                           const char* __restrict__ then_q, int then_rows, const typename Operand<DTYPE>::T (&q)[NT][Rows<DTYPE, D>::ROW / 64],
+                                           float scale, bool first, int& ids, UnitRef& cur, Acc<D, NT>& acc)
 {
-    using R = Rows<D>;
-    constexpr int LPU = R::LPU;
+    using R = Rows<DTYPE, D>;
+    typedef typename Operand<DTYPE>::T Op;
+    constexpr bool BF16 = R::BF16;
+    constexpr int LPU = R::LPU, KB = R::UNIT / 16, KS = R::ROW / 64; // blocks of 16 keys; 64-byte steps of a row
+    constexpr uint32_t ALL = BF16 ? 0xffffffffu : 0xffffu;
     static_assert(FLIGHT <= 2 * LPU, "");
     const int lane = st.lane, c16 = lane & 15, quad = lane >> 4;
-    int koff[D / 32], voff[D / 16];
+    int koff[KS], voff[D / 16]; // V: fp32 four rows of two or one 256-byte groups, bf16 a group of 16 channels each
 #pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) koff[ks] = (int)st.kring + c16 * D * 2 + (((4 * ks + quad) ^ R::ksw(c16)) * 16);
+    for (int ks = 0; ks < KS; ++ks) koff[ks] = (int)st.kring + c16 * R::ROW + (((4 * ks + quad) ^ R::ksw(c16)) * 16);
     const int vrow = 4 * quad + (c16 >> 2);
 #pragma unroll
-    for (int cb = 0; cb < D / 16; ++cb) voff[cb] = (int)st.vring + vrow * D * 2 + ((cb ^ R::vsw(vrow)) * 32) + (c16 & 3) * 8;
+    for (int cb = 0; cb < D / 16; ++cb)
+        voff[cb] = BF16 ? (int)st.vring + vrow * R::ROW + ((cb ^ R::vsw(vrow)) * 32) + (c16 & 3) * 8 : (int)st.vring + (4 * quad + (cb & 3)) * R::ROW + (cb >> 2) * 256 + c16 * 16;
     LDS_AS const char* lds = (LDS_AS const char*)(uintptr_t)0;
 
     auto request_ids = [&](int j0) { j0 < p.n ? st.request_ids(table, p, j0) : st.request_ids(table, then, 0); };
@@ -270,40 +281,52 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             ids = st.take_ids(then, 0);
             next = st.ref(then, 0, ids);
         }
-        f32x4 s[NT][2];
-        bf16x8 ka[2][D / 32];
+        f32x4 s[NT][KB];
+        Op ka[KB][KS];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) ka[kb][ks] = *(LDS_AS const bf16x8*)(lds + koff[ks] + kb * 16 * D * 2);
+            for (int ks = 0; ks < KS; ++ks) ka[kb][ks] = *(LDS_AS const Op*)(lds + koff[ks] + kb * 16 * R::ROW);
         wait_lds(); // the unit's keys are read
         if (more) {
             if (t == 0) st.template issue<false, false>(k, next, ids); // not behind the requests and results above
             else st.template issue<false, true>(k, next, ids);
         }
+        if constexpr (BF16) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks)
+                for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-                    s[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[kb][ks], q[n][ks], ks == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[n][kb], 0, 0, 0);
+                    for (int n = 0; n < NT; ++n)
+                        s[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[kb][ks], q[n][ks], ks == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[n][kb], 0, 0, 0);
+        } else { // which channels make up a product does not matter, as long as both operands agree; two chains, for their length
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f32x4 x[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[0][ks][e], q[n][ks][e], x[e & 1], 0, 0, 0);
+                s[n][0] = x[0] + x[1];
+            }
+        }
         // element e of block kb is key 16 kb + 4 quad + e of the unit
-        if (cur.seen != 0xffffffffu) {
-            const uint32_t mine = cur.seen >> (4 * quad);
+        const uint32_t mine = cur.seen >> (4 * quad);
+        if (cur.seen != ALL) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
+                for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (!(mine & (1u << (16 * kb + e)))) s[n][kb][e] = -INFINITY;
         }
-        bf16x8 hi[NT], lo[NT];
+        bf16x8 hi[NT], lo[NT]; // fp32: the weights stay in s
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
-                              fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
+            float top = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3]));
+            if (KB == 2) top = fmaxf(top, fmaxf(fmaxf(s[n][KB - 1][0], s[n][KB - 1][1]), fmaxf(s[n][KB - 1][2], s[n][KB - 1][3])));
             top *= scale;
             // the reference is exact wherever it is: it only has to stay near enough for the exponential's range
             if (__any(top > acc.m[n] + SLACK)) {
@@ -317,53 +340,69 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             }
             float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4 * KB; ++i) {
                 const float w = __builtin_amdgcn_exp2f(fmaf(s[n][i >> 2][i & 3], scale, -acc.m[n]));
                 sum += w;
-                hi[n][i] = (__bf16)w;
-                lo[n][i] = (__bf16)(w - (float)hi[n][i]);
+                if constexpr (BF16) {
+                    hi[n][i] = (__bf16)w;
+                    lo[n][i] = (__bf16)(w - (float)hi[n][i]);
+                } else {
+                    s[n][0][i] = w;
+                }
             }
             acc.l[n] += sum;
         }
         if (more) wait_vm<LPU>(); // V(t)
         else wait_vm<0>();
         asm volatile("" ::: "memory");
-        bf16x8 va[D / 16];
+        Op va[D / 16];
 #pragma unroll
         for (int cb = 0; cb < D / 16; ++cb) {
-            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(lds + voff[cb]));
-            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(lds + voff[cb] + 16 * D * 2));
-            va[cb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+            if constexpr (BF16) {
+                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(lds + voff[cb]));
+                const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(lds + voff[cb] + 16 * R::ROW));
+                va[cb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+            } else {
+                va[cb] = *(LDS_AS const f32x4*)(lds + voff[cb]); // key 4 quad + cb % 4, channels 64 (cb / 4) + 4 c16 ..
+            }
         }
         wait_lds(); // the unit's values are read
         if (!last) st.template issue<true, true>(v, next, ids);
-        if (cur.seen != 0xffffffffu) { // what is not seen may be anything, and even a weight of zero would make NaN of NaN
-            const uint32_t mine = cur.seen >> (4 * quad);
-            u32x4 keep; // element j of an operand is key 16 (j >> 2) + 4 quad + (j & 3)
+        if (cur.seen != ALL) { // what is not seen may be anything, and even a weight of zero would make NaN of NaN
+            u32x4 keep; // bf16: element j of an operand is key 16 (j >> 2) + 4 quad + (j & 3)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int bit = 16 * (i >> 1) + 2 * (i & 1);
-                keep[i] = ((mine >> bit) & 1 ? 0xffffu : 0u) | ((mine >> bit) & 2 ? 0xffff0000u : 0u);
+                const int bit = BF16 ? 16 * (i >> 1) + 2 * (i & 1) : i;
+                keep[i] = BF16 ? ((mine >> bit) & 1 ? 0xffffu : 0u) | ((mine >> bit) & 2 ? 0xffff0000u : 0u) : (mine >> bit) & 1 ? 0xffffffffu : 0u;
             }
 #pragma unroll
-            for (int cb = 0; cb < D / 16; ++cb) va[cb] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, va[cb]) & keep);
+            for (int cb = 0; cb < D / 16; ++cb) {
+                const u32x4 mask = BF16 ? keep : u32x4{keep[cb & 3], keep[cb & 3], keep[cb & 3], keep[cb & 3]};
+                va[cb] = __builtin_bit_cast(Op, __builtin_bit_cast(u32x4, va[cb]) & mask);
+            }
         }
-        {
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int cb = 0; cb < D / 16; ++cb) {
+            for (int cb = 0; cb < D / 16; ++cb) {
+                if constexpr (BF16) {
                     acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], hi[n], acc.o[n][cb], 0, 0, 0);
                     acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], lo[n], acc.o[n][cb], 0, 0, 0);
+                } else { // operand cb holds key cb % 4 of the four; its channel i goes to block 4 (cb / 4) + i
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        acc.o[n][(cb & ~3) | i] = __builtin_amdgcn_mfma_f32_16x16x4f32(va[cb][i], s[n][0][cb & 3], acc.o[n][(cb & ~3) | i], 0, 0, 0);
                 }
-        }
+            }
         cur = next;
     }
 }
 
-template <int D, int NT>
+template <int DTYPE, int D, int NT>
 __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const TrPagedDecodeArgs a)
 {
+    using R = Rows<DTYPE, D>;
+    using P = Piece<R::UNIT>;
     constexpr int ROWS = 16 * NT;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x, c16 = lane & 15, quad = lane >> 4;
@@ -372,7 +411,7 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
 
     // the batch's units, and the request that this wave's share begins in
     auto len_of = [&](int r) { return r < a.n_req ? a.kv_lens[r] : 0; };
-    auto units_of = [&](int r, int len) { return r < a.n_req ? walk_of(a, len).units : 0; };
+    auto units_of = [&](int r, int len) { return r < a.n_req ? walk_of<R::UNIT>(a, len).units : 0; };
     int lens = len_of(lane), own = units_of(lane, lens), sums = wave_scan(own); // of the 64 requests from r0 on
     int total = __builtin_amdgcn_readlane(sums, 63);
     for (int r0 = 64; r0 < a.n_req; r0 += 64) total += __builtin_amdgcn_readlane(wave_scan(units_of(r0 + lane, len_of(r0 + lane))), 63);
@@ -399,21 +438,21 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
     const int at = __builtin_ctzll(__ballot(before + sums > unit));
     before += __builtin_amdgcn_readlane(sums, at) - __builtin_amdgcn_readlane(own, at);
 
-    Piece p;
+    P p;
     p.r = r0 + at;
-    p.w = walk_of(a, __builtin_amdgcn_readlane(lens, at));
+    p.w = walk_of<R::UNIT>(a, __builtin_amdgcn_readlane(lens, at));
     const int local = begin - before * per_req;
     p.item = uniform(local / p.w.units);
     p.u0 = local - p.item * p.w.units;
-    auto place = [&](Piece& x) {
+    auto place = [&](P& x) {
         x.kvh = uniform(x.item / tiles);
         x.tile = x.item - x.kvh * tiles;
     };
     place(p);
     p.n = min(p.w.units - p.u0, left);
     left -= p.n;
-    auto following = [&](const Piece& from) {
-        Piece x = from;
+    auto following = [&](const P& from) {
+        P x = from;
         x.u0 = x.n = 0;
         if (left == 0) return x;
         if (++x.item == per_req) {
@@ -426,30 +465,30 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
             int len;
             if (x.r < r0 + 64) len = __builtin_amdgcn_readlane(lens, x.r - r0);
             else len = ((const CONST_AS int32_t*)(uintptr_t)a.kv_lens)[x.r]; // through the scalar cache: no wait for what is on its way
-            x.w = walk_of(a, len);
+            x.w = walk_of<R::UNIT>(a, len);
         }
         place(x);
         x.n = min(x.w.units, left);
         left -= x.n;
         return x;
     };
-    auto rows_of = [&](const Piece& x) { return min(a.group - x.tile * ROWS, ROWS); };
-    auto head0_of = [&](const Piece& x) { return (int64_t)x.r * a.n_q_heads + x.kvh * a.group + x.tile * ROWS; }; // of all heads of the batch
-    auto first_q = [&](const Piece& x) { return (const __bf16*)a.q + head0_of(x) * D; };
+    auto rows_of = [&](const P& x) { return min(a.group - x.tile * ROWS, ROWS); };
+    auto head0_of = [&](const P& x) { return (int64_t)x.r * a.n_q_heads + x.kvh * a.group + x.tile * ROWS; }; // of all heads of the batch
+    auto first_q = [&](const P& x) { return (const char*)a.q + head0_of(x) * R::ROW; };
 
-    Stream<D> st(a, (uint32_t)(uintptr_t)(LDS_AS char*)smem, lane);
+    Stream<DTYPE, D> st(a, (uint32_t)(uintptr_t)(LDS_AS char*)smem, lane);
     st.request_ids(a.table, p, 0);
     st.template request_q<NT>(first_q(p), rows_of(p));
-    wait_vm<16 * NT / Rows<D>::RPI>(); // the ids
+    wait_vm<16 * NT / R::RPI>(); // the ids
     asm volatile("" ::: "memory");
     int ids = st.take_ids(p, 0);
     UnitRef cur = st.ref(p, 0, ids);
     st.template issue<false, false>(a.pool.k, cur, ids);
     st.template issue<true, false>(a.pool.v, cur, ids);
-    wait_vm<2 * Rows<D>::LPU>(); // the queries
+    wait_vm<2 * R::LPU>(); // the queries
     for (bool first = true;; first = false) {
-        const Piece then = following(p);
-        bf16x8 q[NT][D / 32];
+        const P then = following(p);
+        typename Operand<DTYPE>::T q[NT][R::ROW / 64];
         asm volatile("" ::: "memory");
         st.template take_q<NT>(q);
         Acc<D, NT> acc;
@@ -460,7 +499,7 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
 #pragma unroll
             for (int cb = 0; cb < D / 16; ++cb) acc.o[t][cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        walk_units<D, NT>(a.pool.k, a.pool.v, a.table, st, p, then, first_q(then), rows_of(then), q, a.scale_log2e, first, ids, cur, acc);
+        walk_units<DTYPE, D, NT>(a.pool.k, a.pool.v, a.table, st, p, then, first_q(then), rows_of(then), q, a.scale_log2e, first, ids, cur, acc);
         if (then.n) st.template issue<true, false>(a.pool.v, cur, ids);
         asm volatile("" ::: "memory");
 
@@ -470,18 +509,24 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
             const float l = column_reduce<false>(acc.l[t]);
             const int row = 16 * t + c16;
             if (row >= rows) continue;
-            if (p.whole()) {
-                const float inv = l == 0.0f ? 0.0f : 1.0f / l; // a row without any weight is zero
-                __bf16* const to = (__bf16*)a.out + (head0_of(p) + row) * D + 4 * quad;
+            const bool whole = p.whole();
+            const float f = !whole ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l; // a row without any weight is zero
+            const int64_t slot = (int64_t)(2 * worker + (p.u0 == 0)) * a.ws_rows + row; // a share cuts at most its first and its last item
+            float* const sums = a.ws_o + slot * D;
 #pragma unroll
-                for (int cb = 0; cb < D / 16; ++cb) *(bf16x4*)(to + 16 * cb) = __builtin_convertvector(acc.o[t][cb] * inv, bf16x4);
-            } else {
-                const int64_t slot = (int64_t)(2 * worker + (p.u0 == 0)) * a.ws_rows + row; // a share cuts at most its first and its last item
-                float* const to = a.ws_o + slot * D + 4 * quad;
-#pragma unroll
-                for (int cb = 0; cb < D / 16; ++cb) *(f32x4*)(to + 16 * cb) = acc.o[t][cb];
-                if (quad == 0) *(float2*)(a.ws_ml + slot * 2) = make_float2(acc.m[t], l);
+            for (int cb = 0; cb < D / 16; ++cb) {
+                const f32x4* const o = acc.o[t];
+                if constexpr (R::BF16) {
+                    const int ch = 16 * cb + 4 * quad;
+                    if (whole) *(bf16x4*)((__bf16*)a.out + (head0_of(p) + row) * D + ch) = __builtin_convertvector(o[cb] * f, bf16x4);
+                    else *(f32x4*)(sums + ch) = o[cb];
+                } else {
+                    const int b = cb & ~3, e = cb & 3;
+                    float* const to = whole ? (float*)a.out + (head0_of(p) + row) * D : sums;
+                    *(f32x4*)(to + 16 * b + 16 * quad + 4 * e) = f32x4{o[b][e], o[b + 1][e], o[b + 2][e], o[b + 3][e]} * f;
+                }
             }
+            if (!whole && quad == 0) *(float2*)(a.ws_ml + slot * 2) = make_float2(acc.m[t], l);
         }
         const int pieces = p.whole() || p.u0 ? 1 : (end - left - then.n - p.n + p.w.units - 1) / share - worker + 1; // of the item that begins here
         if (a.cut == TR_PAGED_JOIN_BY_WAVE) {
@@ -497,7 +542,7 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
 // Joins the pieces of cut items: out = sum_p f_p O_p / sum_p f_p l_p with f_p = 2^(m_p - max m).  One workgroup per row of the
 // result, or per row of the item that a wave of the first launch begins; groups of D / 4 lanes take every GROUPS-th piece and
 // are joined through LDS.
-template <int D>
+template <int DTYPE, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs a, int rows_per_tile)
 {
     constexpr int LPR = D / 4, GROUPS = 256 / LPR;
@@ -569,30 +614,33 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs
         for (int e = 0; e < 4; ++e) y[e] = fmaf(f, os[g][piece][e], y[e]);
     }
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    bf16x4 z;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = (__bf16)(y[e] * inv);
-    *(bf16x4*)((__bf16*)a.out + (int64_t)head * D + 4 * piece) = z;
+    const f32x4 z = y * inv;
+    if constexpr (DTYPE == TR_BF16) *(bf16x4*)((__bf16*)a.out + (int64_t)head * D + 4 * piece) = __builtin_convertvector(z, bf16x4);
+    else *(f32x4*)((float*)a.out + (int64_t)head * D + 4 * piece) = z;
 }
 
-template <int D, int NT> int launch_decode(const TrPagedDecodeArgs& a, int grid, hipStream_t s)
+template <int DTYPE, int D, int NT> int launch_decode(const TrPagedDecodeArgs& a, int grid, hipStream_t s)
 {
     // LDS for as many waves as a compute unit is meant to run: they then spread evenly over the chip
     constexpr int lds = 160 * 1024 / (TR_PAGED_WORKERS / TrChip::CUS);
-    static_assert(lds >= 2 * Rows<D>::BYTES + 256 + 16 * NT * D * 2 && lds <= 64 * 1024, "");
-    paged_decode_kernel<D, NT><<<dim3(grid), dim3(64), lds, s>>>(a);
+    static_assert(lds >= 2 * Rows<DTYPE, D>::BYTES + 256 + 16 * NT * Rows<DTYPE, D>::ROW && lds <= 64 * 1024, "");
+    paged_decode_kernel<DTYPE, D, NT><<<dim3(grid), dim3(64), lds, s>>>(a);
     TR_HIP(hipGetLastError());
     if (a.cut) {
-        paged_join_kernel<D><<<dim3(a.cut == TR_PAGED_JOIN_BY_WAVE ? grid * a.ws_rows : a.n_req * a.n_q_heads), dim3(256), 0, s>>>(a, 16 * NT);
+        paged_join_kernel<DTYPE, D><<<dim3(a.cut == TR_PAGED_JOIN_BY_WAVE ? grid * a.ws_rows : a.n_req * a.n_q_heads), dim3(256), 0, s>>>(a, 16 * NT);
         TR_HIP(hipGetLastError());
     }
     return TR_OK;
 }
+template <int DTYPE> int launch_decode(const TrPagedDecodeArgs& a, int head_dim, int grid, hipStream_t s)
+{
+    if (a.group <= 16) return head_dim == 128 ? launch_decode<DTYPE, 128, 1>(a, grid, s) : launch_decode<DTYPE, 64, 1>(a, grid, s);
+    return head_dim == 128 ? launch_decode<DTYPE, 128, 2>(a, grid, s) : launch_decode<DTYPE, 64, 2>(a, grid, s);
+}
 
 } // namespace
 
-int tr_launch_paged_decode_bf16(const TrPagedDecodeArgs& a, int head_dim, int grid, hipStream_t s)
+int tr_launch_paged_decode(const TrPagedDecodeArgs& a, int dtype, int head_dim, int grid, hipStream_t s)
 {
-    if (a.group <= 16) return head_dim == 128 ? launch_decode<128, 1>(a, grid, s) : launch_decode<64, 1>(a, grid, s);
-    return head_dim == 128 ? launch_decode<128, 2>(a, grid, s) : launch_decode<64, 2>(a, grid, s);
+    return dtype == TR_BF16 ? launch_decode<TR_BF16>(a, head_dim, grid, s) : launch_decode<TR_F32>(a, head_dim, grid, s);
 }
