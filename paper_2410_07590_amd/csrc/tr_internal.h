@@ -405,9 +405,10 @@ struct TrPageMapArgs {
 struct TrPool {
     char* k;
     char* v;
-    int64_t page_stride, row_stride, head_stride;
+    uint32_t page_stride, row_stride, head_stride;
     int32_t n_pages, page_shift;
 };
+#define TR_PAGED_APPEND_TOKENS 8 // at most, of a workgroup
 struct TrPagedAppendArgs {
     const char* q;
     const char* k;
@@ -422,6 +423,7 @@ struct TrPagedAppendArgs {
     int32_t n_tokens;
     int32_t n_q_heads, n_kv_heads; // 0 where the side is absent
     int32_t rotary_dim;
+    int32_t tile_tokens; // tokens of a workgroup
     float eps, amplitude;
     double freq[64];
 };
@@ -440,10 +442,8 @@ struct TrPagedDecodeArgs {
     int32_t n_req, max_blocks, window, n_sink;
     int32_t n_q_heads, n_kv_heads, group;
     float scale_log2e; // log2(e) / sqrt(head_dim)
-    int32_t workers;   // shares; not the number of waves, which may be fewer where the table bounds the work
     int32_t cut;       // 0: no item can be cut; else a second launch joins their pieces: TR_PAGED_JOIN_BY_ROW, _BY_WAVE
     int32_t ws_rows;   // rows of a piece
-    int32_t pad_;
     float* ws_o;       // [2 workers][ws_rows][head_dim] sums of a piece: 2 w of the item that worker w continues, 2 w + 1 of the one it begins
     float* ws_ml;      // [2 workers][ws_rows][2] reference maximum (log2 domain) and denominator
     int32_t* ws_items; // by row: [items][2] wave that begins an item, number of its pieces; by wave: [waves][2] item it begins and cuts, number of pieces

@@ -158,86 +158,120 @@ template <> struct Vec<TR_F32> {
     }
 };
 
+// Sum over LANES neighbouring lanes, within a row of 16 on the vector unit's cross-lane path.
 template <int LANES> __device__ __forceinline__ float lanes_sum(float x)
 {
-#pragma unroll
-    for (int o = LANES / 2; o >= 1; o >>= 1) x += __shfl_xor(x, o);
+    static_assert(LANES == 8 || LANES == 16 || LANES == 32, "");
+    auto bits = [&]() { return __builtin_bit_cast(int, x); };
+    auto add = [&](int y) { x += __builtin_bit_cast(float, y); };
+    add(__builtin_amdgcn_update_dpp(bits(), bits(), 0xB1, 0xf, 0xf, false));                   // quad_perm [1,0,3,2]
+    add(__builtin_amdgcn_update_dpp(bits(), bits(), 0x4E, 0xf, 0xf, false));                   // quad_perm [2,3,0,1]
+    add(__builtin_amdgcn_update_dpp(bits(), bits(), 0x141, 0xf, 0xf, false));                  // row_half_mirror
+    if (LANES >= 16) add(__builtin_amdgcn_update_dpp(bits(), bits(), 0x140, 0xf, 0xf, false)); // row_mirror
+    if (LANES == 32) x += __shfl_xor(x, 16);
     return x;
 }
 
-// A workgroup owns one token; LPH neighbouring lanes own a head, a 16-byte unit each.  The token's angles are worked out once
-// (a thread per pair, 64 bits) into LDS for all of its heads.
+// Bound by memory: a head is read once and written once.  A workgroup owns a few tokens; LPH neighbouring lanes own a head, a
+// 16-byte unit each, so a norm and a rotation stay within a wave.  The tokens' angles (a thread per pair, 64 bits) are worked out
+// once for all of their heads, while the first UNITS loads of every thread are on their way.
+constexpr int APPEND_UNITS = 4;
 template <int DTYPE, int D, bool HALF>
 __global__ __launch_bounds__(256) void paged_append_kernel(const TrPagedAppendArgs a)
 {
     using V = Vec<DTYPE>;
-    constexpr int N = V::N, LPH = D / N;
-    __shared__ float2 turn[64]; // cosine and sine of each pair, times the amplitude
+    constexpr int N = V::N, LPH = D / N, UNITS = APPEND_UNITS, HEAD = D * 16 / N; // channels of a unit, units and bytes of a head
+    __shared__ float2 turn[TR_PAGED_APPEND_TOKENS * 64]; // cosine and sine of each token's pairs, times the amplitude
     const int tid = threadIdx.x, piece = tid % LPH;
-    const int pairs = a.rotary_dim / 2;
-    const int half_units = pairs / N; // units of half the turned channels
+    const int pairs = a.rotary_dim / 2, half_units = pairs / N; // units of half the turned channels
     const bool turns = piece * N < a.rotary_dim, low = piece < half_units;
+    const int partner = !HALF || !turns ? (tid & 63) : (tid & 63) + (low ? half_units : -half_units);
+    const int m0 = HALF ? (low ? piece : piece - half_units) * N : piece * (N / 2); // first pair of the unit
     const int n_heads = a.n_q_heads + 2 * a.n_kv_heads;
+    const int64_t t0 = (int64_t)blockIdx.x * a.tile_tokens;
+    const int tokens = (int)min((int64_t)a.tile_tokens, a.n_tokens - t0), heads = tokens * n_heads;
+
     float qw[N], kw[N];
     if (a.q_norm) V::open(((const u32x4*)a.q_norm)[piece], qw);
     if (a.k_norm) V::open(((const u32x4*)a.k_norm)[piece], kw);
-    for (int64_t t = blockIdx.x; t < a.n_tokens; t += gridDim.x) {
-        __syncthreads();
-        if (tid < pairs) {
-            double sn, cn;
-            tr_sincos((double)a.pos[t] * a.freq[tid], &sn, &cn);
-            turn[tid] = make_float2((float)(cn * a.amplitude), (float)(sn * a.amplitude));
+    struct Unit {
+        u32x4 x;
+        int tok, h; // of the tile; head of the token: queries, keys, values
+    };
+    auto load = [&](int i) { // the i-th head that this thread has part in
+        Unit u;
+        const int at = tid / LPH + i * (256 / LPH);
+        if (at >= heads) {
+            u.h = -1;
+            return u;
         }
-        __syncthreads();
-        const int slot = a.n_kv_heads ? a.slots[t] : -1;
-        const int page = slot >> a.pool.page_shift;
-        const bool stored = slot >= 0 && page < a.pool.n_pages;
-        const int64_t row = (int64_t)page * a.pool.page_stride + (int64_t)(slot & ((1 << a.pool.page_shift) - 1)) * a.pool.row_stride;
-        for (int h = tid / LPH; h < n_heads; h += 256 / LPH) {
-            const bool is_q = h < a.n_q_heads, is_v = h >= a.n_q_heads + a.n_kv_heads;
-            const int hk = h - a.n_q_heads - (is_v ? a.n_kv_heads : 0);
-            const char* src = is_q ? a.q + t * a.q_stride + (int64_t)h * D * sizeof(u32x4) / N
-                                   : (is_v ? a.v + t * a.v_stride : a.k + t * a.k_stride) + (int64_t)hk * D * sizeof(u32x4) / N;
-            u32x4 u = ((const u32x4*)src)[piece];
-            const bool normed = is_q ? a.q_norm != nullptr : a.k_norm != nullptr;
-            if (!is_v && (normed || pairs)) {
+        u.tok = a.tile_tokens == 1 ? 0 : at / n_heads;
+        u.h = at - u.tok * n_heads;
+        const int hk = u.h - a.n_q_heads, hv = hk - a.n_kv_heads;
+        const int64_t t = t0 + u.tok;
+        const char* src = hk < 0 ? a.q + t * a.q_stride + (int64_t)u.h * HEAD : hv < 0 ? a.k + t * a.k_stride + (int64_t)hk * HEAD : a.v + t * a.v_stride + (int64_t)hv * HEAD;
+        u.x = __builtin_nontemporal_load((const u32x4*)src + piece);
+        return u;
+    };
+    Unit u[UNITS];
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) u[i] = load(i);
+    for (int i = tid; i < tokens * pairs; i += 256) {
+        const int tok = i / pairs, m = i - tok * pairs;
+        double sn, cn;
+        tr_sincos((double)a.pos[t0 + tok] * a.freq[m], &sn, &cn);
+        turn[tok * 64 + m] = make_float2((float)(cn * a.amplitude), (float)(sn * a.amplitude));
+    }
+    __syncthreads();
+    for (int i0 = 0;; i0 += UNITS) {
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            if (u[i].h < 0) continue; // heads are dealt out whole, so the lanes of one are here together
+            const int h = u[i].h, hk = h - a.n_q_heads, hv = hk - a.n_kv_heads;
+            const int64_t t = t0 + u[i].tok;
+            const bool normed = hk < 0 ? a.q_norm != nullptr : a.k_norm != nullptr;
+            if (hv < 0 && (normed || pairs)) {
+                const float2* const e = turn + u[i].tok * 64 + m0;
                 float x[N];
-                V::open(u, x);
+                V::open(u[i].x, x);
                 if (normed) {
                     float ss = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) ss = fmaf(x[i], x[i], ss);
-                    const float r = 1.0f / sqrtf(lanes_sum<LPH>(ss) * (1.0f / D) + a.eps);
+                    for (int c = 0; c < N; ++c) ss = fmaf(x[c], x[c], ss);
+                    const float r = rsqrtf(lanes_sum<LPH>(ss) * (1.0f / D) + a.eps);
 #pragma unroll
-                    for (int i = 0; i < N; ++i) x[i] = x[i] * r * (is_q ? qw[i] : kw[i]);
+                    for (int c = 0; c < N; ++c) x[c] = x[c] * r * (hk < 0 ? qw[c] : kw[c]);
                 }
                 if (HALF) {
                     float y[N];
-                    const int partner = (tid & 63) + (low ? half_units : -half_units);
 #pragma unroll
-                    for (int i = 0; i < N; ++i) y[i] = __shfl(x[i], turns ? partner : tid & 63);
+                    for (int c = 0; c < N; ++c) y[c] = __shfl(x[c], partner);
                     if (turns) {
-                        const int m0 = (low ? piece : piece - half_units) * N;
 #pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            const float2 e = turn[m0 + i];
-                            x[i] = low ? x[i] * e.x - y[i] * e.y : x[i] * e.x + y[i] * e.y;
-                        }
+                        for (int c = 0; c < N; ++c) x[c] = x[c] * e[c].x + (low ? -y[c] : y[c]) * e[c].y;
                     }
                 } else if (turns) {
 #pragma unroll
-                    for (int i = 0; i < N / 2; ++i) {
-                        const float2 e = turn[piece * (N / 2) + i];
-                        const float p = x[2 * i], s = x[2 * i + 1];
-                        x[2 * i] = p * e.x - s * e.y;
-                        x[2 * i + 1] = s * e.x + p * e.y;
+                    for (int c = 0; c < N / 2; ++c) {
+                        const float p = x[2 * c], s = x[2 * c + 1];
+                        x[2 * c] = p * e[c].x - s * e[c].y;
+                        x[2 * c + 1] = s * e[c].x + p * e[c].y;
                     }
                 }
-                if (normed || turns) u = V::close(x);
+                if (normed || turns) u[i].x = V::close(x);
             }
-            if (is_q) ((u32x4*)(a.q_out + (t * a.n_q_heads + h) * (int64_t)(D * sizeof(u32x4) / N)))[piece] = u;
-            else if (stored) ((u32x4*)((is_v ? a.pool.v : a.pool.k) + row + hk * a.pool.head_stride))[piece] = u;
+            if (hk < 0) {
+                ((u32x4*)(a.q_out + (t * a.n_q_heads + h) * HEAD))[piece] = u[i].x;
+            } else {
+                const int slot = a.slots[t], page = slot >> a.pool.page_shift;
+                const int64_t row = (int64_t)page * a.pool.page_stride + (int64_t)(slot & ((1 << a.pool.page_shift) - 1)) * a.pool.row_stride;
+                if (slot >= 0 && page < a.pool.n_pages)
+                    ((u32x4*)(hv < 0 ? a.pool.k + row + (int64_t)hk * a.pool.head_stride : a.pool.v + row + (int64_t)hv * a.pool.head_stride))[piece] = u[i].x;
+            }
         }
+        if ((i0 + UNITS) * (256 / LPH) >= heads) break;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) u[i] = load(i0 + UNITS + i);
     }
 }
 
@@ -251,16 +285,25 @@ int tr_launch_page_map(const TrPageMapArgs& a, hipStream_t s)
     return TR_OK;
 }
 
-template <int DTYPE, int D> static void launch_append(const TrPagedAppendArgs& a, int layout, hipStream_t s)
+template <int DTYPE, int D> static void launch_append(const TrPagedAppendArgs& a, int blocks, int layout, hipStream_t s)
 {
-    const dim3 grid(std::min(a.n_tokens, TR_MAX_BLOCKS_256));
-    if (layout == TR_ROPE_HALF) paged_append_kernel<DTYPE, D, true><<<grid, dim3(256), 0, s>>>(a);
-    else paged_append_kernel<DTYPE, D, false><<<grid, dim3(256), 0, s>>>(a);
+    if (layout == TR_ROPE_HALF) paged_append_kernel<DTYPE, D, true><<<dim3(blocks), dim3(256), 0, s>>>(a);
+    else paged_append_kernel<DTYPE, D, false><<<dim3(blocks), dim3(256), 0, s>>>(a);
 }
-int tr_launch_paged_append(const TrPagedAppendArgs& a, int dtype, int head_dim, int layout, hipStream_t s)
+int tr_launch_paged_append(const TrPagedAppendArgs& args, int dtype, int head_dim, int layout, hipStream_t s)
 {
-    if (dtype == TR_BF16) head_dim == 128 ? launch_append<TR_BF16, 128>(a, layout, s) : launch_append<TR_BF16, 64>(a, layout, s);
-    else head_dim == 128 ? launch_append<TR_F32, 128>(a, layout, s) : launch_append<TR_F32, 64>(a, layout, s);
-    TR_HIP(hipGetLastError());
+    TrPagedAppendArgs a = args;
+    const int tile = a.tile_tokens;
+    // a launch has fewer than 2^32 threads
+    for (int64_t at = 0; at < args.n_tokens; at += (int64_t)TR_MAX_BLOCKS_256 * tile) {
+        a.n_tokens = (int32_t)std::min<int64_t>(args.n_tokens - at, (int64_t)TR_MAX_BLOCKS_256 * tile);
+        if (a.q) a.q = args.q + at * a.q_stride, a.q_out = args.q_out + at * a.n_q_heads * head_dim * (dtype == TR_F32 ? 4 : 2);
+        if (a.k) a.k = args.k + at * a.k_stride, a.v = args.v + at * a.v_stride, a.slots = args.slots + at;
+        if (a.pos) a.pos = args.pos + at;
+        const int blocks = (a.n_tokens + tile - 1) / tile;
+        if (dtype == TR_BF16) head_dim == 128 ? launch_append<TR_BF16, 128>(a, blocks, layout, s) : launch_append<TR_BF16, 64>(a, blocks, layout, s);
+        else head_dim == 128 ? launch_append<TR_F32, 128>(a, blocks, layout, s) : launch_append<TR_F32, 64>(a, blocks, layout, s);
+        TR_HIP(hipGetLastError());
+    }
     return TR_OK;
 }

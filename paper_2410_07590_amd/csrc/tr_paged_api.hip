@@ -32,7 +32,7 @@ int pool_of(const char* who, const tr_shape* sh, const tr_pages* p, TrPool* out)
     // a stride of a single page or head is never applied; the others have to keep rows apart
     if (p->row_stride < sh->head_dim || (p->n_kv_heads > 1 && p->head_stride < sh->head_dim) || (p->n_pages > 1 && p->page_stride < sh->head_dim))
         return tr_fail(TR_ERR_INVALID_ARG, "%s: strides of the pages are smaller than a head", who);
-    if (p->head_stride < 0 || p->page_stride < 0)
+    if (p->head_stride < 0 || p->page_stride < 0) // of a single head or page
         return tr_fail(TR_ERR_INVALID_ARG, "%s: strides of the pages are out of range", who);
     if (p->row_stride > widest / e || p->head_stride > widest / e || p->page_stride > (widest * 64 - 1) / e)
         return tr_fail(TR_ERR_UNSUPPORTED, "%s: rows or heads of the pages are more than 64 MiB apart, or pages 4 GiB", who);
@@ -40,9 +40,9 @@ int pool_of(const char* who, const tr_shape* sh, const tr_pages* p, TrPool* out)
         return tr_fail(TR_ERR_INVALID_ARG, "%s: pages and their strides must be 16-byte aligned", who);
     out->k = (char*)p->k;
     out->v = (char*)p->v;
-    out->page_stride = p->page_stride * e;
-    out->row_stride = p->row_stride * e;
-    out->head_stride = p->head_stride * e;
+    out->page_stride = (uint32_t)(p->page_stride * e);
+    out->row_stride = (uint32_t)(p->row_stride * e);
+    out->head_stride = (uint32_t)(p->head_stride * e);
     out->n_pages = p->n_pages;
     out->page_shift = shift;
     return TR_OK;
@@ -191,8 +191,8 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     if ((overlap(outs, qs) && !(q == q_out && (n_tokens == 1 || q_stride == q_row))) || overlap(outs, ks) || overlap(outs, vs))
         return tr_fail(TR_ERR_INVALID_ARG, "%s: q_out overlaps an input (it may be a contiguous q itself)", who);
     if (pages) {
-        const int64_t pool = (int64_t)(a.pool.n_pages - 1) * a.pool.page_stride + (pages->page_size - 1) * a.pool.row_stride +
-                             (pages->n_kv_heads - 1) * a.pool.head_stride + shape->head_dim * e;
+        const int64_t pool = (int64_t)(a.pool.n_pages - 1) * a.pool.page_stride + (int64_t)(pages->page_size - 1) * a.pool.row_stride +
+                             (int64_t)(pages->n_kv_heads - 1) * a.pool.head_stride + shape->head_dim * e;
         for (const Span& s : {Span{pages->k, pool}, Span{pages->v, pool}})
             if (overlap(s, qs) || overlap(s, ks) || overlap(s, vs) || overlap(s, outs))
                 return tr_fail(TR_ERR_INVALID_ARG, "%s: the pages overlap another tensor of the call", who);
@@ -215,6 +215,10 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     a.n_q_heads = q ? shape->n_q_heads : 0;
     a.n_kv_heads = k ? shape->n_kv_heads : 0;
     a.eps = (float)eps;
+    // Tokens of a workgroup: TODO
+    const int64_t units = (a.n_q_heads + 2 * a.n_kv_heads) * shape->head_dim * e / 16; // of a token
+    a.tile_tokens = 1;
+    while (a.tile_tokens < TR_PAGED_APPEND_TOKENS && a.tile_tokens * units * 2 <= 1024 && n_tokens >= 2048 * a.tile_tokens) a.tile_tokens *= 2;
     return tr_launch_paged_append(a, shape->dtype, shape->head_dim, layout, (hipStream_t)stream);
     });
 }
@@ -294,7 +298,6 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
         a.ws_items = (int32_t*)((char*)workspace + plan.items_at);
     }
     a.ws_rows = plan.ws_rows;
-    a.workers = TR_PAGED_WORKERS;
     const int64_t workers = std::min<int64_t>((plan.bound + TR_PAGED_MIN_UNITS - 1) / TR_PAGED_MIN_UNITS, TR_PAGED_WORKERS);
     // The join's workgroups, most of which find nothing to do, are what it costs (some 1 600 a microsecond): it looks at the rows of
     // the result or at those that each wave may have cut, whichever are fewer (us, whole call: 512 requests of 256 rows, 32/8

@@ -104,7 +104,7 @@ template <> struct Operand<TR_F32> { typedef f32x4 T; };
 // One unit of a wave: where its KV head begins, its first key, which of its keys are seen, and where its page ids are among the
 // wave's.
 struct UnitRef {
-    int64_t head;
+    uint64_t head;
     int key0, at;
     uint32_t seen;
 };
@@ -133,7 +133,7 @@ template <int DTYPE, int D> struct Stream {
     uint32_t kring, vring, idring, qring, row_bytes, page_bytes;
     int lane, page_shift, sub_shift, per_unit_shift, n_pages; // sub_shift: rows of a page within a unit; per_unit_shift: pages of a unit
     int32_t max_blocks;
-    int64_t head_stride;
+    uint32_t head_stride;
     uint32_t dk[LPU], dv[LPU]; // what a lane adds to the start of a unit's page for load i
 
     __device__ __forceinline__ Stream(const TrPagedDecodeArgs& a, uint32_t ring, int lane_) : lane(lane_)
@@ -142,8 +142,8 @@ template <int DTYPE, int D> struct Stream {
         vring = kring + R::BYTES;
         idring = vring + R::BYTES;
         qring = idring + 256;
-        row_bytes = (uint32_t)a.pool.row_stride;
-        page_bytes = (uint32_t)a.pool.page_stride;
+        row_bytes = a.pool.row_stride;
+        page_bytes = a.pool.page_stride;
         head_stride = a.pool.head_stride;
         page_shift = a.pool.page_shift;
         n_pages = a.pool.n_pages;
@@ -203,7 +203,7 @@ template <int DTYPE, int D> struct Stream {
     __device__ __forceinline__ UnitRef ref(const P& p, int j, int ids) const
     {
         UnitRef u;
-        u.head = p.kvh * head_stride;
+        u.head = (uint64_t)(uint32_t)p.kvh * head_stride;
         u.key0 = uniform(p.w.unit(p.u0 + j) * UNIT);
         u.at = (j & (refill() - 1)) << per_unit_shift;
         u.seen = p.w.seen(u.key0);
@@ -416,7 +416,7 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
     int total = __builtin_amdgcn_readlane(sums, 63);
     for (int r0 = 64; r0 < a.n_req; r0 += 64) total += __builtin_amdgcn_readlane(wave_scan(units_of(r0 + lane, len_of(r0 + lane))), 63);
     total *= per_req;
-    const int share = max((total + a.workers - 1) / a.workers, TR_PAGED_MIN_UNITS);
+    const int share = max((total + TR_PAGED_WORKERS - 1) / TR_PAGED_WORKERS, TR_PAGED_MIN_UNITS);
     const int begin = share * worker;
     // who has pieces of the cut items, by the item or by the wave that begins it (a share begins at most one)
     auto record = [&](int64_t at, int x, int pieces) {
@@ -445,7 +445,7 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
     p.item = uniform(local / p.w.units);
     p.u0 = local - p.item * p.w.units;
     auto place = [&](P& x) {
-        x.kvh = uniform(x.item / tiles);
+        x.kvh = tiles == 1 ? x.item : uniform(x.item / tiles);
         x.tile = x.item - x.kvh * tiles;
     };
     place(p);
