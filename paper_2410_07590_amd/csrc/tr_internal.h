@@ -423,7 +423,8 @@ struct TrPagedAppendArgs {
     int32_t n_tokens;
     int32_t n_q_heads, n_kv_heads; // 0 where the side is absent
     int32_t rotary_dim;
-    int32_t tile_tokens; // tokens of a workgroup
+    int32_t tile_shift; // log2 of the tokens of a workgroup
+    int32_t stream;     // results are stored past the L2
     float eps, amplitude;
     double freq[64];
 };

@@ -10,9 +10,22 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // ---- block tables, slots, position ids ------------------------------------------------------------------------------------
-// One launch and no traffic between workgroups: each works out the prefix sums of the whole batch again (two lengths per
-// request, from the caches) and then the slots of its own 1024 tokens, a few pages and, the first, the batch's lengths.
-// A token finds its request by bisection of the sums in LDS, a thread does it once for four neighbours.
+// A chain of latencies: one launch and no traffic between workgroups.  Each works out the prefix sums of the whole batch again (two
+// lengths per request, from the caches) and then the slots of its own 1024 tokens, a few pages and, the first, the batch's
+// lengths.  A token finds its request by bisection of the sums in LDS, a thread does it once for four neighbours.
+// Sums are cut at 2^32 - 1 by every addition, which leaves addition associative, and at 2^31 - 1 where they are kept.
+
+__device__ __forceinline__ uint32_t add(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+__device__ __forceinline__ uint32_t wave_sums(uint32_t x) // inclusive, on the vector unit's cross-lane path
+{
+    x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false)); // row_shr 1, 2, 4, 8
+    x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+    x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+    x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+    x = add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false)); // last lane of a row to the next row
+    return add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false)); // lane 31 to the upper half
+}
+__device__ __forceinline__ int32_t cut(uint32_t x) { return (int32_t)min(x, (uint32_t)INT32_MAX); }
 
 // Largest r with starts[r] <= x, for starts[0] = 0 <= x < starts[n]: requests without entries are passed over.
 __device__ __forceinline__ int owner(const int32_t* starts, int n, int x)
@@ -24,53 +37,59 @@ __device__ __forceinline__ int owner(const int32_t* starts, int n, int x)
     }
     return lo;
 }
-__device__ __forceinline__ int32_t cut(int64_t x) { return (int32_t)min(x, (int64_t)INT32_MAX); }
 
 __global__ __launch_bounds__(256) void page_map_kernel(const TrPageMapArgs a)
 {
-    extern __shared__ int32_t sums[];
-    __shared__ int64_t wave_sum[4][2];
-    int32_t* const cu = sums;               // [n_req + 1] first token of each request
-    int32_t* const pg = sums + a.n_req + 1; // [n_req + 1] first new page
+    extern __shared__ int32_t arrays[];
+    __shared__ uint32_t wave_sum[4][2];
+    int32_t* const cu = arrays;          // [n_req + 1] first token of each request
+    int32_t* const pg = cu + a.n_req + 1; // [n_req + 1] first new page
+    int32_t* const held = pg + a.n_req + 1; // [n_req] tokens that it holds
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int per = (a.n_req + 255) / 256, shift = a.page_shift;
-    const int64_t round = (1 << shift) - 1;
-    auto pages = [&](int64_t tokens) { return (tokens + round) >> shift; };
+    const uint32_t round = (1u << shift) - 1;
+    auto pages = [&](uint32_t tokens) { return (tokens >> shift) + ((tokens & round) != 0); }; // tokens < 2^32
+    struct Lens {
+        uint32_t c, f; // below 2^31 each
+    };
+    auto lens = [&](int r) { return Lens{(uint32_t)max(a.cached[r], 0), (uint32_t)max(a.fresh[r], 0)}; };
 
-    int64_t tok = 0, pag = 0;
+    uint32_t tok = 0, pag = 0;
+    Lens mine = {0, 0};
     for (int i = 0; i < per; ++i) {
         const int r = tid * per + i;
         if (r >= a.n_req) break;
-        const int64_t c = max(a.cached[r], 0), f = max(a.fresh[r], 0);
-        tok += f;
-        pag += pages(c + f) - pages(c);
+        mine = lens(r);
+        tok = add(tok, mine.f);
+        pag = add(pag, pages(mine.c + mine.f) - pages(mine.c));
     }
-    int64_t tok_to = tok, pag_to = pag; // inclusive sums over the wave
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t t = __shfl_up(tok_to, o), p = __shfl_up(pag_to, o);
-        if (lane >= o) tok_to += t, pag_to += p;
-    }
+    uint32_t tok_to = wave_sums(tok), pag_to = wave_sums(pag);
     if (lane == 63) wave_sum[wave][0] = tok_to, wave_sum[wave][1] = pag_to;
+    // sums in front of this lane's requests
+    tok_to = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)tok_to, 0x138, 0xf, 0xf, false); // wave_shr 1
+    pag_to = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)pag_to, 0x138, 0xf, 0xf, false);
     __syncthreads();
-    tok_to -= tok;
-    pag_to -= pag;
-    int64_t tok_all = 0, pag_all = 0;
+    uint32_t tok_all = 0, pag_all = 0, tok_before = 0, pag_before = 0;
     for (int w = 0; w < 4; ++w) {
-        if (w < wave) tok_to += wave_sum[w][0], pag_to += wave_sum[w][1];
-        tok_all += wave_sum[w][0], pag_all += wave_sum[w][1];
+        if (w == wave) tok_before = tok_all, pag_before = pag_all;
+        tok_all = add(tok_all, wave_sum[w][0]);
+        pag_all = add(pag_all, wave_sum[w][1]);
     }
+    tok_to = add(tok_to, tok_before);
+    pag_to = add(pag_to, pag_before);
     for (int i = 0; i < per; ++i) {
         const int r = tid * per + i;
         if (r >= a.n_req) break;
-        const int64_t c = max(a.cached[r], 0), f = max(a.fresh[r], 0);
+        if (per > 1) mine = lens(r);
         cu[r] = cut(tok_to);
         pg[r] = cut(pag_to);
+        held[r] = (int32_t)mine.c;
         if (blockIdx.x == 0) {
             a.cu[r] = cut(tok_to);
-            a.kv_lens[r] = cut(c + f);
+            a.kv_lens[r] = cut(mine.c + mine.f);
         }
-        tok_to += f;
-        pag_to += pages(c + f) - pages(c);
+        tok_to = add(tok_to, mine.f);
+        pag_to = add(pag_to, pages(mine.c + mine.f) - pages(mine.c));
     }
     if (tid == 0) {
         cu[a.n_req] = cut(tok_all);
@@ -84,41 +103,43 @@ __global__ __launch_bounds__(256) void page_map_kernel(const TrPageMapArgs a)
     __syncthreads();
 
     const int n_tok = cu[a.n_req], n_pag = pg[a.n_req];
-    auto free_page = [&](int i) { return i < a.n_free ? a.free_pages[i] : -1; };
+    auto free_page = [&](int64_t i) { return i < a.n_free ? a.free_pages[i] : -1; };
+    const int64_t t0 = (int64_t)blockIdx.x * TR_MAP_TOKENS + 4 * tid;
+    if (t0 < a.n_slots) {
+        int32_t slot[4], pos[4];
+        int r = t0 < n_tok ? owner(cu, a.n_req, (int)t0) : 0;
+        int last = -1, first = 0;
+        uint32_t c = 0, have = 0;
+        for (int i = 0; i < 4; ++i) {
+            const int64_t t = t0 + i;
+            slot[i] = -1;
+            pos[i] = 0;
+            if (t >= n_tok) continue;
+            while (cu[r + 1] <= t) ++r;
+            if (r != last) {
+                last = r;
+                c = (uint32_t)held[r];
+                have = pages(c);
+                first = a.first_pos ? a.first_pos[r] : (int)c;
+            }
+            const uint32_t at = (uint32_t)(t - cu[r]), row = c + at, blk = row >> shift;
+            pos[i] = (int32_t)((uint32_t)first + at);
+            if (blk >= (uint32_t)a.max_blocks) continue;
+            const int page = blk < have ? a.table[(int64_t)r * a.max_blocks + blk] : free_page((int64_t)pg[r] + blk - have);
+            const int64_t s = ((int64_t)page << shift) + (row & round);
+            slot[i] = page < 0 || s > INT32_MAX ? -1 : (int32_t)s;
+        }
+        if (t0 + 4 <= a.n_slots) {
+            *(i32x4_any*)(a.slots + t0) = i32x4_any{slot[0], slot[1], slot[2], slot[3]};
+            *(i32x4_any*)(a.pos + t0) = i32x4_any{pos[0], pos[1], pos[2], pos[3]};
+        } else {
+            for (int i = 0; i < 4 && t0 + i < a.n_slots; ++i) a.slots[t0 + i] = slot[i], a.pos[t0 + i] = pos[i];
+        }
+    }
     for (int64_t p = (int64_t)blockIdx.x * 256 + tid; p < n_pag; p += (int64_t)gridDim.x * 256) {
         const int r = owner(pg, a.n_req, (int)p);
-        const int64_t blk = pages(max(a.cached[r], 0)) + p - pg[r];
-        if (blk < a.max_blocks) a.table[(int64_t)r * a.max_blocks + blk] = free_page((int)p);
-    }
-
-    const int64_t t0 = (int64_t)blockIdx.x * TR_MAP_TOKENS + 4 * tid;
-    if (t0 >= a.n_slots) return;
-    int32_t slot[4], pos[4];
-    int r = t0 < n_tok ? owner(cu, a.n_req, (int)t0) : 0;
-    int last = -1, c = 0, first = 0;
-    for (int i = 0; i < 4; ++i) {
-        const int64_t t = t0 + i;
-        slot[i] = -1;
-        pos[i] = 0;
-        if (t >= n_tok) continue;
-        while (cu[r + 1] <= t) ++r;
-        if (r != last) {
-            last = r;
-            c = max(a.cached[r], 0);
-            first = a.first_pos ? a.first_pos[r] : c;
-        }
-        const int64_t at = t - cu[r], row = c + at, blk = row >> shift, have = pages(c);
-        pos[i] = (int32_t)((uint32_t)first + (uint32_t)at);
-        if (blk >= a.max_blocks) continue;
-        const int page = blk < have ? a.table[(int64_t)r * a.max_blocks + blk] : free_page((int)min(pg[r] + blk - have, (int64_t)INT32_MAX));
-        const int64_t s = ((int64_t)page << shift) + (row & round);
-        slot[i] = page < 0 || s > INT32_MAX ? -1 : (int32_t)s;
-    }
-    if (t0 + 4 <= a.n_slots) {
-        *(i32x4_any*)(a.slots + t0) = i32x4_any{slot[0], slot[1], slot[2], slot[3]};
-        *(i32x4_any*)(a.pos + t0) = i32x4_any{pos[0], pos[1], pos[2], pos[3]};
-    } else {
-        for (int i = 0; i < 4 && t0 + i < a.n_slots; ++i) a.slots[t0 + i] = slot[i], a.pos[t0 + i] = pos[i];
+        const int64_t blk = pages((uint32_t)held[r]) + p - pg[r];
+        if (blk < a.max_blocks) a.table[(int64_t)r * a.max_blocks + blk] = free_page(p);
     }
 }
 
@@ -172,106 +193,126 @@ template <int LANES> __device__ __forceinline__ float lanes_sum(float x)
     return x;
 }
 
+// The value of the lane half a head away, where the whole head turns.
+template <int LANES> __device__ __forceinline__ float other_half(float x)
+{
+    const int b = __builtin_bit_cast(int, x);
+    if constexpr (LANES == 16) return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, 0x128, 0xf, 0xf, false)); // row_ror 8
+    else if constexpr (LANES == 8) { // of eight lanes, and of each four: the mirror of the mirror
+        const int m = __builtin_amdgcn_update_dpp(b, b, 0x141, 0xf, 0xf, false);
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(m, m, 0x1B, 0xf, 0xf, false));
+    } else return __shfl_xor(x, LANES / 2);
+}
+
 // Bound by memory: a head is read once and written once.  A workgroup owns a few tokens; LPH neighbouring lanes own a head, a
-// 16-byte unit each, so a norm and a rotation stay within a wave.  The tokens' angles (a thread per pair, 64 bits) are worked out
-// once for all of their heads, while the first UNITS loads of every thread are on their way.
-constexpr int APPEND_UNITS = 4;
-template <int DTYPE, int D, bool HALF>
+// 16-byte unit each, so a norm and a rotation stay within a wave.  A thread has part in heads of one token only, always the same
+// unit of them: its cosines and sines, weights and the token's row are looked up once.  The tokens' angles (a thread per pair, 64 bits)
+// are worked out while the first UNITS loads of every thread are on their way.
+// UNITS: with two, 16001 tokens of 40 heads and values take 81.9 us (three 83.3, four 88.8), 1000 9.2 (9.0) and one 4.40 (4.33).
+constexpr int APPEND_UNITS = 3;
+template <int DTYPE, int D, bool HALF, bool STREAM>
 __global__ __launch_bounds__(256) void paged_append_kernel(const TrPagedAppendArgs a)
 {
     using V = Vec<DTYPE>;
     constexpr int N = V::N, LPH = D / N, UNITS = APPEND_UNITS, HEAD = D * 16 / N; // channels of a unit, units and bytes of a head
+    constexpr int TURNS = HALF ? N : N / 2;                                       // pairs that a unit has part in
     __shared__ float2 turn[TR_PAGED_APPEND_TOKENS * 64]; // cosine and sine of each token's pairs, times the amplitude
     const int tid = threadIdx.x, piece = tid % LPH;
     const int pairs = a.rotary_dim / 2, half_units = pairs / N; // units of half the turned channels
-    const bool turns = piece * N < a.rotary_dim, low = piece < half_units;
-    const int partner = !HALF || !turns ? (tid & 63) : (tid & 63) + (low ? half_units : -half_units);
+    const bool turns = piece * N < a.rotary_dim, low = piece < half_units, full = a.rotary_dim == D;
+    const int partner = turns ? (tid & 63) + (low ? half_units : -half_units) : (tid & 63);
     const int m0 = HALF ? (low ? piece : piece - half_units) * N : piece * (N / 2); // first pair of the unit
     const int n_heads = a.n_q_heads + 2 * a.n_kv_heads;
-    const int64_t t0 = (int64_t)blockIdx.x * a.tile_tokens;
-    const int tokens = (int)min((int64_t)a.tile_tokens, a.n_tokens - t0), heads = tokens * n_heads;
+    const int step = 256 / LPH >> a.tile_shift; // heads of a token that are worked on at a time
+    const int64_t t0 = (int64_t)blockIdx.x << a.tile_shift;
+    const int tokens = (int)min((int64_t)1 << a.tile_shift, a.n_tokens - t0);
+    const int tok = tid / LPH / step;
+    const bool live = tok < tokens;
+    const int64_t t = t0 + (live ? tok : 0);
+    int h = tid / LPH % step; // of queries, keys and values in a row
+    const char* const q = a.q + t * a.q_stride + piece * 16;
+    const char* const k = a.k + t * a.k_stride + piece * 16;
+    const char* const v = a.v + t * a.v_stride + piece * 16;
 
-    float qw[N], kw[N];
-    if (a.q_norm) V::open(((const u32x4*)a.q_norm)[piece], qw);
-    if (a.k_norm) V::open(((const u32x4*)a.k_norm)[piece], kw);
-    struct Unit {
-        u32x4 x;
-        int tok, h; // of the tile; head of the token: queries, keys, values
+    u32x4 u[UNITS];
+    auto load = [&](int head) {
+        const int hk = head - a.n_q_heads, hv = hk - a.n_kv_heads;
+        if (!live || head >= n_heads) return u32x4{};
+        return __builtin_nontemporal_load((const u32x4*)(hk < 0 ? q + head * HEAD : hv < 0 ? k + hk * HEAD : v + hv * HEAD));
     };
-    auto load = [&](int i) { // the i-th head that this thread has part in
-        Unit u;
-        const int at = tid / LPH + i * (256 / LPH);
-        if (at >= heads) {
-            u.h = -1;
-            return u;
-        }
-        u.tok = a.tile_tokens == 1 ? 0 : at / n_heads;
-        u.h = at - u.tok * n_heads;
-        const int hk = u.h - a.n_q_heads, hv = hk - a.n_kv_heads;
-        const int64_t t = t0 + u.tok;
-        const char* src = hk < 0 ? a.q + t * a.q_stride + (int64_t)u.h * HEAD : hv < 0 ? a.k + t * a.k_stride + (int64_t)hk * HEAD : a.v + t * a.v_stride + (int64_t)hv * HEAD;
-        u.x = __builtin_nontemporal_load((const u32x4*)src + piece);
-        return u;
-    };
-    Unit u[UNITS];
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) u[i] = load(i);
+    for (int i = 0; i < UNITS; ++i) u[i] = load(h + i * step);
+    const int slot = a.n_kv_heads ? a.slots[t] : -1;
+    u32x4 qw_raw = {}, kw_raw = {};
+    if (a.q_norm) qw_raw = ((const u32x4*)a.q_norm)[piece];
+    if (a.k_norm) kw_raw = ((const u32x4*)a.k_norm)[piece];
     for (int i = tid; i < tokens * pairs; i += 256) {
-        const int tok = i / pairs, m = i - tok * pairs;
+        const int at = i / pairs, m = i - at * pairs;
         double sn, cn;
-        tr_sincos((double)a.pos[t0 + tok] * a.freq[m], &sn, &cn);
-        turn[tok * 64 + m] = make_float2((float)(cn * a.amplitude), (float)(sn * a.amplitude));
+        tr_sincos((double)a.pos[t0 + at] * a.freq[m], &sn, &cn);
+        turn[at * 64 + m] = make_float2((float)(cn * a.amplitude), (float)(sn * a.amplitude));
     }
     __syncthreads();
-    for (int i0 = 0;; i0 += UNITS) {
+    float2 e[TURNS];
+#pragma unroll
+    for (int c = 0; c < TURNS; ++c) {
+        e[c] = turns && live ? turn[tok * 64 + m0 + c] : make_float2(1.0f, 0.0f); // channels that do not turn
+        if (HALF && low) e[c].y = -e[c].y;
+    }
+    const int page = slot >> a.pool.page_shift;
+    const bool stored = slot >= 0 && page < a.pool.n_pages;
+    const int64_t row = (int64_t)page * a.pool.page_stride + (int64_t)(slot & ((1 << a.pool.page_shift) - 1)) * a.pool.row_stride + piece * 16;
+    char* const qd = a.q_out + t * a.n_q_heads * HEAD + piece * 16;
+    char *const kd = a.pool.k + row, *const vd = a.pool.v + row;
+    float qw[N], kw[N];
+    V::open(qw_raw, qw);
+    V::open(kw_raw, kw);
+    for (;; h += UNITS * step) {
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
-            if (u[i].h < 0) continue; // heads are dealt out whole, so the lanes of one are here together
-            const int h = u[i].h, hk = h - a.n_q_heads, hv = hk - a.n_kv_heads;
-            const int64_t t = t0 + u[i].tok;
+            const int head = h + i * step, hk = head - a.n_q_heads, hv = hk - a.n_kv_heads;
+            if (!live || head >= n_heads) continue; // heads are dealt out whole, so the lanes of one are here together
             const bool normed = hk < 0 ? a.q_norm != nullptr : a.k_norm != nullptr;
-            if (hv < 0 && (normed || pairs)) {
-                const float2* const e = turn + u[i].tok * 64 + m0;
+            if (hv < 0 && (pairs || normed)) {
                 float x[N];
-                V::open(u[i].x, x);
+                V::open(u[i], x);
                 if (normed) {
                     float ss = 0.0f;
 #pragma unroll
                     for (int c = 0; c < N; ++c) ss = fmaf(x[c], x[c], ss);
                     const float r = rsqrtf(lanes_sum<LPH>(ss) * (1.0f / D) + a.eps);
 #pragma unroll
-                    for (int c = 0; c < N; ++c) x[c] = x[c] * r * (hk < 0 ? qw[c] : kw[c]);
+                    for (int c = 0; c < N; ++c) x[c] *= r * (hk < 0 ? qw[c] : kw[c]);
                 }
                 if (HALF) {
                     float y[N];
+                    if (full) {
 #pragma unroll
-                    for (int c = 0; c < N; ++c) y[c] = __shfl(x[c], partner);
-                    if (turns) {
+                        for (int c = 0; c < N; ++c) y[c] = other_half<LPH>(x[c]);
+                    } else {
 #pragma unroll
-                        for (int c = 0; c < N; ++c) x[c] = x[c] * e[c].x + (low ? -y[c] : y[c]) * e[c].y;
+                        for (int c = 0; c < N; ++c) y[c] = __shfl(x[c], partner);
                     }
-                } else if (turns) {
+#pragma unroll
+                    for (int c = 0; c < N; ++c) x[c] = turns ? x[c] * e[c].x + y[c] * e[c].y : x[c];
+                } else {
 #pragma unroll
                     for (int c = 0; c < N / 2; ++c) {
-                        const float p = x[2 * c], s = x[2 * c + 1];
-                        x[2 * c] = p * e[c].x - s * e[c].y;
-                        x[2 * c + 1] = s * e[c].x + p * e[c].y;
+                        const float one = x[2 * c], two = x[2 * c + 1];
+                        x[2 * c] = turns ? one * e[c].x - two * e[c].y : one;
+                        x[2 * c + 1] = turns ? two * e[c].x + one * e[c].y : two;
                     }
                 }
-                if (normed || turns) u[i].x = V::close(x);
+                if (normed || turns) u[i] = V::close(x);
             }
-            if (hk < 0) {
-                ((u32x4*)(a.q_out + (t * a.n_q_heads + h) * HEAD))[piece] = u[i].x;
-            } else {
-                const int slot = a.slots[t], page = slot >> a.pool.page_shift;
-                const int64_t row = (int64_t)page * a.pool.page_stride + (int64_t)(slot & ((1 << a.pool.page_shift) - 1)) * a.pool.row_stride;
-                if (slot >= 0 && page < a.pool.n_pages)
-                    ((u32x4*)(hv < 0 ? a.pool.k + row + (int64_t)hk * a.pool.head_stride : a.pool.v + row + (int64_t)hv * a.pool.head_stride))[piece] = u[i].x;
-            }
+            char* const to = hk < 0 ? qd + head * HEAD : hv < 0 ? kd + (int64_t)hk * a.pool.head_stride : vd + (int64_t)hv * a.pool.head_stride;
+            if (hk >= 0 && !stored) continue;
+            if (STREAM) __builtin_nontemporal_store(u[i], (u32x4*)to);
+            else *(u32x4*)to = u[i];
         }
-        if ((i0 + UNITS) * (256 / LPH) >= heads) break;
+        if (h - tid / LPH % step + UNITS * step >= n_heads) break;
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) u[i] = load(i0 + UNITS + i);
+        for (int i = 0; i < UNITS; ++i) u[i] = load(h + (UNITS + i) * step);
     }
 }
 
@@ -280,20 +321,24 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const TrPagedAppendAr
 int tr_launch_page_map(const TrPageMapArgs& a, hipStream_t s)
 {
     const int blocks = std::max((int)(((int64_t)a.n_slots + TR_MAP_TOKENS - 1) / TR_MAP_TOKENS), 1);
-    page_map_kernel<<<dim3(blocks), dim3(256), 2 * (a.n_req + 1) * sizeof(int32_t), s>>>(a);
+    page_map_kernel<<<dim3(blocks), dim3(256), (3 * a.n_req + 2) * sizeof(int32_t), s>>>(a);
     TR_HIP(hipGetLastError());
     return TR_OK;
 }
 
+template <int DTYPE, int D, bool HALF> static void launch_append(const TrPagedAppendArgs& a, int blocks, hipStream_t s)
+{
+    if (a.stream) paged_append_kernel<DTYPE, D, HALF, true><<<dim3(blocks), dim3(256), 0, s>>>(a);
+    else paged_append_kernel<DTYPE, D, HALF, false><<<dim3(blocks), dim3(256), 0, s>>>(a);
+}
 template <int DTYPE, int D> static void launch_append(const TrPagedAppendArgs& a, int blocks, int layout, hipStream_t s)
 {
-    if (layout == TR_ROPE_HALF) paged_append_kernel<DTYPE, D, true><<<dim3(blocks), dim3(256), 0, s>>>(a);
-    else paged_append_kernel<DTYPE, D, false><<<dim3(blocks), dim3(256), 0, s>>>(a);
+    layout == TR_ROPE_HALF ? launch_append<DTYPE, D, true>(a, blocks, s) : launch_append<DTYPE, D, false>(a, blocks, s);
 }
 int tr_launch_paged_append(const TrPagedAppendArgs& args, int dtype, int head_dim, int layout, hipStream_t s)
 {
     TrPagedAppendArgs a = args;
-    const int tile = a.tile_tokens;
+    const int tile = 1 << a.tile_shift;
     // a launch has fewer than 2^32 threads
     for (int64_t at = 0; at < args.n_tokens; at += (int64_t)TR_MAX_BLOCKS_256 * tile) {
         a.n_tokens = (int32_t)std::min<int64_t>(args.n_tokens - at, (int64_t)TR_MAX_BLOCKS_256 * tile);
