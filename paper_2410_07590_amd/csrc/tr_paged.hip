@@ -238,7 +238,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const TrPagedAppendAr
     auto load = [&](int head) {
         const int hk = head - a.n_q_heads, hv = hk - a.n_kv_heads;
         if (!live || head >= n_heads) return u32x4{};
-        return __builtin_nontemporal_load((const u32x4*)(hk < 0 ? q + head * HEAD : hv < 0 ? k + hk * HEAD : v + hv * HEAD));
+        return __builtin_nontemporal_load((const u32x4*)(hk < 0 ? q + (int64_t)head * HEAD : hv < 0 ? k + (int64_t)hk * HEAD : v + (int64_t)hv * HEAD));
     };
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) u[i] = load(h + i * step);
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const TrPagedAppendAr
                 }
                 if (normed || turns) u[i] = V::close(x);
             }
-            char* const to = hk < 0 ? qd + head * HEAD : hv < 0 ? kd + (int64_t)hk * a.pool.head_stride : vd + (int64_t)hv * a.pool.head_stride;
+            char* const to = hk < 0 ? qd + (int64_t)head * HEAD : hv < 0 ? kd + (int64_t)hk * a.pool.head_stride : vd + (int64_t)hv * a.pool.head_stride;
             if (hk >= 0 && !stored) continue;
             if (STREAM) __builtin_nontemporal_store(u[i], (u32x4*)to);
             else *(u32x4*)to = u[i];

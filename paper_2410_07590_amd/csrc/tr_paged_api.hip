@@ -60,6 +60,12 @@ bool overlap(const Span& a, const Span& b)
 Span ints(const int32_t* p, int64_t n) { return {p, p ? 4 * n : 0}; }
 // n rows of `row` bytes, a stride apart
 Span rows(const void* p, int64_t n, int64_t stride, int64_t row) { return {p, p ? (n - 1) * stride + row : 0}; }
+// all rows of a pool, and what lies between them
+Span pool_span(const TrPool& pool, const void* base, const tr_pages* p)
+{
+    return {base, (p->n_pages - 1) * (int64_t)pool.page_stride + (p->page_size - 1) * (int64_t)pool.row_stride +
+                      (p->n_kv_heads - 1) * (int64_t)pool.head_stride + p->head_dim * (int64_t)(p->dtype == TR_F32 ? 4 : 2)};
+}
 
 } // namespace
 
@@ -186,16 +192,19 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     // tokens may share a row of the input (a stride of 0), they may not overlap in part
     if ((q && (q_stride < 0 || q_stride > INT64_MAX / 8 / n_tokens)) || (k && (k_stride < 0 || k_stride > INT64_MAX / 8 / n_tokens || v_stride < 0 || v_stride > INT64_MAX / 8 / n_tokens)))
         return tr_fail(TR_ERR_INVALID_ARG, "%s: a stride is out of range", who);
-    const Span qs = rows(q, n_tokens, q_stride * e, q_row * e), ks = rows(k, n_tokens, k_stride * e, kv_row * e), vs = rows(v, n_tokens, v_stride * e, kv_row * e);
-    const Span outs = rows(q_out, n_tokens, q_row * e, q_row * e);
-    if ((overlap(outs, qs) && !(q == q_out && (n_tokens == 1 || q_stride == q_row))) || overlap(outs, ks) || overlap(outs, vs))
-        return tr_fail(TR_ERR_INVALID_ARG, "%s: q_out overlaps an input (it may be a contiguous q itself)", who);
+    const Span qs = rows(q, n_tokens, q_stride * e, q_row * e), outs = rows(q_out, n_tokens, q_row * e, q_row * e);
+    const Span in[] = {rows(k, n_tokens, k_stride * e, kv_row * e), rows(v, n_tokens, v_stride * e, kv_row * e), ints(pos, n_tokens), ints(slots, n_tokens),
+                       rows(q_norm, 1, 0, shape->head_dim * e), rows(k_norm, 1, 0, shape->head_dim * e)};
+    if (overlap(outs, qs) && !(q == q_out && (n_tokens == 1 || q_stride == q_row)))
+        return tr_fail(TR_ERR_INVALID_ARG, "%s: q_out overlaps q without being it (contiguous)", who);
+    for (const Span& s : in)
+        if (overlap(outs, s)) return tr_fail(TR_ERR_INVALID_ARG, "%s: q_out overlaps an input", who);
     if (pages) {
-        const int64_t pool = (int64_t)(a.pool.n_pages - 1) * a.pool.page_stride + (int64_t)(pages->page_size - 1) * a.pool.row_stride +
-                             (int64_t)(pages->n_kv_heads - 1) * a.pool.head_stride + shape->head_dim * e;
-        for (const Span& s : {Span{pages->k, pool}, Span{pages->v, pool}})
-            if (overlap(s, qs) || overlap(s, ks) || overlap(s, vs) || overlap(s, outs))
-                return tr_fail(TR_ERR_INVALID_ARG, "%s: the pages overlap another tensor of the call", who);
+        for (const Span& pool : {pool_span(a.pool, pages->k, pages), pool_span(a.pool, pages->v, pages)}) {
+            for (const Span& s : in)
+                if (overlap(pool, s)) return tr_fail(TR_ERR_INVALID_ARG, "%s: the pages overlap an input", who);
+            if (overlap(pool, qs) || overlap(pool, outs)) return tr_fail(TR_ERR_INVALID_ARG, "%s: the pages overlap q or q_out", who);
+        }
     }
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(q_norm) || !aligned16(k_norm) || (q && q_stride * e % 16) ||
         (k && (k_stride * e % 16 || v_stride * e % 16)))
@@ -281,6 +290,11 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     if (n_req == 0) return TR_OK;
     if (!q || !out || !kv_lens || (max_blocks > 0 && !block_table)) return tr_fail(TR_ERR_INVALID_ARG, "%s: an array is NULL", who);
     if (!aligned16(q) || !aligned16(out)) return tr_fail(TR_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned", who);
+    const int64_t row = (int64_t)shape->n_q_heads * shape->head_dim * tr_elem_bytes(shape);
+    const Span outs = rows(out, n_req, row, row);
+    if (overlap(outs, rows(q, n_req, row, row)) && out != q) return tr_fail(TR_ERR_INVALID_ARG, "%s: out overlaps q without being it", who);
+    for (const Span& s : {pool_span(a.pool, pages->k, pages), pool_span(a.pool, pages->v, pages), ints(block_table, (int64_t)n_req * max_blocks), ints(kv_lens, n_req)})
+        if (overlap(outs, s)) return tr_fail(TR_ERR_INVALID_ARG, "%s: out overlaps the pages, the table or the lengths", who);
     a.q = q;
     a.out = out;
     a.table = block_table;

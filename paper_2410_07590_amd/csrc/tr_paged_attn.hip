@@ -409,13 +409,20 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
     const int tiles = (a.group + ROWS - 1) / ROWS, per_req = a.n_kv_heads * tiles; // items of a request
     const int worker = blockIdx.x;
 
-    // the batch's units, and the request that this wave's share begins in
+    // the batch's units, and the request that this wave's share begins in: a lane sums up `per` neighbouring requests
     auto len_of = [&](int r) { return r < a.n_req ? a.kv_lens[r] : 0; };
     auto units_of = [&](int r, int len) { return r < a.n_req ? walk_of<R::UNIT>(a, len).units : 0; };
-    int lens = len_of(lane), own = units_of(lane, lens), sums = wave_scan(own); // of the 64 requests from r0 on
-    int total = __builtin_amdgcn_readlane(sums, 63);
-    for (int r0 = 64; r0 < a.n_req; r0 += 64) total += __builtin_amdgcn_readlane(wave_scan(units_of(r0 + lane, len_of(r0 + lane))), 63);
-    total *= per_req;
+    const int per = (a.n_req + 63) / 64;
+    int lens = len_of(lane * per), own = units_of(lane * per, lens);
+    for (int i = 1; i < per; i += 8) {
+        int l[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) l[j] = i + j < per ? len_of(lane * per + i + j) : 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) own += i + j < per ? units_of(lane * per + i + j, l[j]) : 0;
+    }
+    int sums = wave_scan(own);
+    const int total = __builtin_amdgcn_readlane(sums, 63) * per_req;
     const int share = max((total + TR_PAGED_WORKERS - 1) / TR_PAGED_WORKERS, TR_PAGED_MIN_UNITS);
     const int begin = share * worker;
     // who has pieces of the cut items, by the item or by the wave that begins it (a share begins at most one)
@@ -429,14 +436,20 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
     const int end = min(begin + share, total);
     int left = end - begin; // behind the pieces described so far
     const int unit = begin / per_req; // in units of all heads together
-    int before = 0, r0 = 0;
-    while (before + __builtin_amdgcn_readlane(sums, 63) <= unit && r0 + 64 < a.n_req) {
-        before += __builtin_amdgcn_readlane(sums, 63);
-        r0 += 64;
-        lens = len_of(r0 + lane), own = units_of(r0 + lane, lens), sums = wave_scan(own);
+    int at = __builtin_ctzll(__ballot(sums > unit)), r0 = 0;
+    int before = __builtin_amdgcn_readlane(sums, at) - __builtin_amdgcn_readlane(own, at);
+    if (per > 1) { // one of that lane's
+        r0 = at * per;
+        while (true) {
+            lens = len_of(r0 + lane), own = units_of(r0 + lane, lens), sums = wave_scan(own);
+            const int here = __builtin_amdgcn_readlane(sums, 63);
+            if (before + here > unit || r0 + 64 >= a.n_req) break;
+            before += here;
+            r0 += 64;
+        }
+        at = __builtin_ctzll(__ballot(before + sums > unit));
+        before += __builtin_amdgcn_readlane(sums, at) - __builtin_amdgcn_readlane(own, at);
     }
-    const int at = __builtin_ctzll(__ballot(before + sums > unit));
-    before += __builtin_amdgcn_readlane(sums, at) - __builtin_amdgcn_readlane(own, at);
 
     P p;
     p.r = r0 + at;
@@ -571,7 +584,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs
     if (item.y <= 1) return;
     float M = NOTHING, L = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int AHEAD = 4;
+    constexpr int AHEAD = 4; // with eight, 64 x 4096 rows take 94.4 us (90.9): most rows have fewer pieces
     for (int p0 = grp; p0 < item.y; p0 += GROUPS * AHEAD) {
         f32x4 x[AHEAD];
         float2 ml[AHEAD];

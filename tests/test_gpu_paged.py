@@ -345,6 +345,10 @@ def test_decode_long_and_many(B, dt):
     check_decode(B, dt, 4, 2, 128, [9000, 3, 5001, 0, 77], seed=2, hide=False, page=64)
     check_decode(B, dt, 2, 1, 64, list(np.random.default_rng(0).integers(0, 70, 700)), seed=3, hide=False)
     check_decode(B, dt, 2, 2, 64, [9, 4000] + [1] * 300, seed=4, hide=False)
+    # pieces joined by the waves that begin them; more requests than a wave has lanes, by more than one each
+    check_decode(B, dt, 16, 4, 64, list(np.random.default_rng(5).integers(0, 400, 300)), seed=5, hide=False)
+    check_decode(B, dt, 34, 1, 64, list(np.random.default_rng(6).integers(0, 300, 70)), seed=6, hide=False)
+    check_decode(B, dt, 1, 1, 64, [0, 700] * 20 + list(np.random.default_rng(7).integers(0, 30, 5000)) + [900], seed=7, hide=False)
 
 
 def test_decode_scores_of_any_size(B):
@@ -368,6 +372,38 @@ def test_decode_scores_of_any_size(B):
                 got = run_decode(B, gs, q.cuda(), k, vp, table.cuda(), ints([512]), 0, 0)
                 want, bound = R.decode_batch(q, k.cpu(), vp.cpu(), table, [512], 0, 0, 2)
                 R.assert_within(got, want, torch.finfo(DT[dt]).eps / 2 * want.abs() * 1.01 + bound, "sign %g peak %s" % (sign, peak))
+
+
+def test_decode_queries_that_are_not_numbers_stay_by_themselves(B):
+    for dt, d in (("bf16", 128), ("f32", 64)):
+        table, n_pages = tables(np.random.default_rng(2), [300, 90], 16)
+        kp, vp = make_pool(n_pages, 16, 2, d, DT[dt], "rows", 3)
+        q = randn(2, 8, d, seed=5, dtype=DT[dt])
+        gs = B.make_shape(8, 2, d, dt, 1e4)
+        clean = run_decode(B, gs, q.cuda(), kp, vp, ints(table), ints([300, 90]), 0, 0)
+        q[0, 3, 7], q[1, 4] = float("nan"), float("inf")
+        got = run_decode(B, gs, q.cuda(), kp, vp, ints(table), ints([300, 90]), 0, 0)
+        assert torch.isnan(got[0, 3]).all() and torch.isnan(got[1, 4]).all()
+        got[0, 3], got[1, 4] = clean[0, 3], clean[1, 4]
+        assert torch.equal(got, clean)
+        kp[int(table[1, 1]), 3, 1, 5] = float("nan")      # a visible key of one request and head
+        got = run_decode(B, gs, q.cuda(), kp, vp, ints(table), ints([300, 90]), 0, 0)
+        assert torch.isnan(got[1, 4:]).all() and not torch.isnan(got[1, :4]).any()
+        got[0, 3], got[1, 4:] = clean[0, 3], clean[1, 4:]
+        assert torch.equal(got, clean)
+
+
+def test_decode_into_its_own_queries(B):
+    for dt, d in (("bf16", 128), ("f32", 64)):
+        lens = [5000, 3, 0, 200]
+        table, n_pages = tables(np.random.default_rng(2), lens, 16)
+        kp, vp = make_pool(n_pages, 16, 2, d, DT[dt], "rows", 3)
+        q = randn(4, 8, d, seed=5, dtype=DT[dt]).cuda()
+        gs = B.make_shape(8, 2, d, dt, 1e4)
+        want = run_decode(B, gs, q, kp, vp, ints(table), ints(lens), 0, 0)
+        B.tr_paged_decode_attn(gs, q, B.make_pages(kp, vp), ints(table), ints(lens), 0, 0, q,
+                               B.workspace(B.tr_paged_decode_attn_workspace_size(gs, 4, table.shape[1], 16)))
+        assert torch.equal(q, want)
 
 
 def test_decode_pages_that_are_none(B):

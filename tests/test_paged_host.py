@@ -155,6 +155,7 @@ def rotary(**kw):
     (dict(eps=0.0), -1), (dict(eps=-1.0), -1), (dict(eps=math.nan), -1), (dict(eps=math.inf), -1), (dict(eps=1e-60), -1), (dict(eps=1e300), -1),
     (dict(q=FAKE[0] + 2), -1), (dict(k=FAKE[1] + 8), -1), (dict(v=FAKE[2] + 8), -1), (dict(out=FAKE[7] + 8), -1), (dict(qn=FAKE[3] + 2), -1),
     (dict(kn=FAKE[4] + 2), -1), (dict(qs=28 * 128 + 4), -1), (dict(ks=516), -1), (dict(vs=517), -1), (dict(qs=-3584), -1), (dict(ks=2 ** 62), -1),
+    (dict(out=FAKE[5]), -1), (dict(out=FAKE[6] + 16), -1), (dict(out=FAKE[3]), -1), (dict(out=FAKE[4] + 240), -1), (dict(slots=FAKE[11] + 32), -1),
     (dict(out=FAKE[0] + 256), -1), (dict(out=FAKE[0], qs=28 * 128 + 8), -1), (dict(out=FAKE[1]), -1), (dict(out=FAKE[2] + 4096), -1),
     (dict(k=FAKE[10] + 1024), -1), (dict(out=FAKE[11]), -1), (dict(q=FAKE[11] + 99 * 16384 + 15 * 1024 + 768, qs=0), -1),
     (dict(pages=pages(page_size=12)), -1), (dict(pages=pages(page_size=4)), -1), (dict(pages=pages(n_pages=0)), -1), (dict(pages=pages(n_pages=2 ** 27)), -1),
@@ -191,7 +192,10 @@ def decode(L, **kw):
     (dict(pages="none"), -1), (dict(q=0), -1), (dict(table=0), -1), (dict(lens=0), -1), (dict(out=0), -1), (dict(n=-1), -1), (dict(blocks=-1), -1),
     (dict(window=-1), -1), (dict(sinks=-1), -1), (dict(q=FAKE[0] + 4), -1), (dict(out=FAKE[3] + 8), -1), (dict(blocks=2 ** 28), -1),
     (dict(pages=pages(page_size=0)), -1), (dict(pages=pages(k=0)), -1), (dict(pages=pages(page_stride=4)), -1),
-    (dict(n=65537), B.TR_ERR_UNSUPPORTED), (dict(pages=pages(row_stride=2 ** 26)), B.TR_ERR_UNSUPPORTED)])
+    (dict(out=FAKE[0] + 256), -1), (dict(out=FAKE[1] + 16), -1), (dict(out=FAKE[2]), -1), (dict(out=FAKE[10]), -1), (dict(out=FAKE[11] + 4096), -1),
+    (dict(ws=0), B.TR_ERR_WORKSPACE), (dict(ws=FAKE[4] + 16), B.TR_ERR_WORKSPACE), (dict(bytes=1000), B.TR_ERR_WORKSPACE),
+    (dict(n=65537), B.TR_ERR_UNSUPPORTED), (dict(n=4096, blocks=2 ** 18), B.TR_ERR_UNSUPPORTED), (dict(pages=pages(row_stride=2 ** 26)), B.TR_ERR_UNSUPPORTED),
+    (dict(n=60000, shape=shape(hq=1024, hkv=512), pages=pages(n_kv_heads=512, row_stride=512 * 128, page_stride=2 ** 20)), B.TR_ERR_UNSUPPORTED)])
 def test_decode_refusals(L, kw, code):
     assert decode(L, **kw) == code and L.tr_last_error()
 
