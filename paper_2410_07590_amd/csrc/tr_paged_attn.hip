@@ -1,23 +1,32 @@
 // Decode attention over a paged cache: one new token per request, lengths and page ids known on the GPU only.
 //
-// Bound by the stream of keys and values (4 g flops per 4 bytes for g query heads to a KV head), so the design is about
+// Bound by the stream of keys and values (4 g flops per 4 bytes of bf16 for g query heads to a KV head), so the design is about
 // keeping requests for memory on their way on every compute unit, whatever the lengths are:
 //
-// Work.  An item is a (request, KV head, block of at most 16 NT query heads).  Its visible keys are walked in units of 32 by
-// single waves that share nothing.  The host does not know the lengths, so the launch is a fixed number of waves, each of which
-// takes an equal share of all units of the batch, in order of items: it works out the batch's sum from kv_lens and finds its own
-// range in it.  No share is longer than another by more than a unit, whatever the mix of lengths, and at most the first and the
-// last item of a share are cut.  Pieces of cut items go to the workspace and a second, small launch joins them.
+// Work.  An item is a (request, KV head, block of at most 16 NT query heads).  Its visible keys are walked in units (32 of bf16,
+// 16 of fp32) by single waves that share nothing.  The host does not know the lengths, so the launch is a fixed number of waves,
+// four per compute unit, each of which takes an equal share of all units of the batch, in order of items: it works out the batch's
+// sum from kv_lens and finds its own range in it.  No share is longer than another by more than a unit, whatever the mix of
+// lengths, and at most the first and the last item of a share are cut.  Pieces of cut items go to the workspace and a second,
+// small launch joins them.  (Workgroups of four waves that walked an item's keys together and joined them in LDS took 94.3 us for 64 x
+// 4096 rows where this takes 91.0, 97.5 for one request of 131071 rows (90.0), 104 for 200 requests of 50 to 1200 rows (99.5):
+// their waves wait for one another at the end of each item.)
 //
-// Products.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16, keys and values as the A operands from LDS (V through
-// the transposing read), so that a lane owns one query column: its maximum and denominator are scalars, and its share of S^T
-// is, up to the order of the keys, its B operand of the second product.  The weights go into it as two bf16 parts, which
-// keeps 16 bits of them: the matrix unit is idle most of the time, and the result is as exact as fp32 weights would give.
+// Products.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16 (fp32: 16x16x4), keys and values as the A operands from
+// LDS (bf16 V through the transposing read), so that a lane owns one query column: its maximum and denominator are scalars, and
+// its share of S^T is, up to the order of the keys, its B operand of the second product.  A bf16 product takes the weights as
+// two bf16 parts, which keeps 16 bits of them: the matrix unit is idle most of the time (64 x 4096 rows: 91.1 us, 90.9 with one
+// part), and the error against 64 bits is then that of rounding the result, 1.667e-3 of its norm (2.270e-3 with one part).
 //
-// Data movement.  A wave has room for one unit of K and of V and refills them as soon as their operands are read, straight
-// from memory to LDS, counted waits instead of barriers; the first unit of its next item is on its way before it is done with
-// the last one of this.  A page id is needed for every 8 rows at the most: a wave keeps the ids of its next units in one
-// register, a lane each, and takes them out as scalars.
+// Data movement.  A wave has room for one unit of K and of V (8 KB each at 128 channels) and refills them as soon as their
+// operands are read, straight from memory to LDS, counted waits instead of barriers; the first unit of its next item is on its
+// way before it is done with the last one of this.  A page id is needed for every 8 rows at the most: a wave keeps the ids of
+// its next units in one register, a lane each, and takes them out as scalars.
+//
+// Heads of 128 channels, bf16, fresh pools every pass, us of the whole call (replayed graph): 64 requests of 4096 rows, 28 / 4 heads,
+// pages of 64: 91 (538 MB: 5.9 TB/s; the first kernel alone 80 to 82, 6.6 TB/s); one of 131071, 32 / 8 heads, pages of 16: 90;
+// 32 of up to 32000 rows through a window of 4000 and 4 first tokens: 85 (489 MB); five of 300 to 3000 rows: 13.4; one of 700: 8.4,
+// which is two launches and, in the first, four dependent trips to memory (lengths, page ids, keys, results).
 #include "tr_device.h"
 #include "tr_internal.h"
 
@@ -34,7 +43,9 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 constexpr float SLACK = 8.0f;        // log2 units by which a score may exceed the reference before it moves
 constexpr float NOTHING = -3.0e38f;  // reference of a row that has seen no key
 constexpr int DMA_STREAM = 2;        // non-temporal: every key is read once
-constexpr int FLIGHT = 6;            // loads of 1 KB that a wave has on their way
+// Loads of 1 KB that a wave has on their way.  us with 5 / 6 / 7 / 8: 64 x 4096 rows 94.1 / 91.4 / 92.6 / 96.5, one request of 131071 92.9 /
+// 90.2 / 90.4 / 92.9, windows over 32 requests 87.6 / 85.5 / 86.8 / 90.9, 200 requests of 50 to 1200 105.0 / 103.2 / 103.1 / 103.2.
+constexpr int FLIGHT = 6;
 
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
@@ -232,8 +243,9 @@ template <int DTYPE, int D> struct Stream {
 };
 
 // A wave's walk over its units of piece p, the first of which is on its way; at its end the keys of the first unit of piece `then`
-// are, whose page ids and queries it leaves in ids and in LDS.  Loads return in order, so the counts below say which of them have: a unit's keys once no more
-// than the loads of its values are left, its values once no more than those of the next unit's keys are.
+// are, whose page ids and queries it leaves in ids and in LDS.  Loads return in order, so the counts below say which of them
+// have: a unit's keys once no more than the loads of its values are left, its values once no more than those of the next
+// unit's keys are.
 // A function of its own with restricted pointers, LDS by whole addresses: the compiler otherwise takes the reads of LDS to
 // depend on every load on its way to it.
 template <int DTYPE, int D, int NT>
@@ -262,7 +274,8 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
     for (int t = 0; t < p.n; ++t) {
         UnitRef next;
         const bool last = t + 1 == p.n, more = !last || then.n > 0;
-        // K(t).  Behind the keys of a piece that is not the first there are, besides its values, the results of the last one.
+        // K(t).  Behind the keys of a piece that is not the first there are, besides its values, the results of the last one: at least
+        // D / 16 stores of a lane, none of which touches another and could become one with it.
         if (t == 0 && !first) wait_vm<LPU + D / 16>();
         else wait_vm<LPU>();
         if (t == 0) { // in front of K(1), so that whoever waits for that has them
@@ -447,12 +460,13 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
             before += here;
             r0 += 64;
         }
-        at = __builtin_ctzll(__ballot(before + sums > unit));
+        const uint64_t here = __ballot(before + sums > unit);
+        at = here ? __builtin_ctzll(here) : 63; // never none, unless the lengths are written meanwhile
         before += __builtin_amdgcn_readlane(sums, at) - __builtin_amdgcn_readlane(own, at);
     }
 
     P p;
-    p.r = r0 + at;
+    p.r = min(r0 + at, a.n_req - 1);
     p.w = walk_of<R::UNIT>(a, __builtin_amdgcn_readlane(lens, at));
     const int local = begin - before * per_req;
     p.item = uniform(local / p.w.units);

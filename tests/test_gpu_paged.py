@@ -351,6 +351,22 @@ def test_decode_long_and_many(B, dt):
     check_decode(B, dt, 1, 1, 64, [0, 700] * 20 + list(np.random.default_rng(7).integers(0, 30, 5000)) + [900], seed=7, hide=False)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [8, 16])
+def test_decode_shares_longer_than_a_register_of_page_ids(B, dt, page):
+    """Requests that share pages: 64 rows of 9000 keys over a pool of 500 pages, so every wave walks many units."""
+    rng = np.random.default_rng(page)
+    n, d, n_pages = 64, 64, 500
+    lens = rng.integers(8800, 9200, n)
+    table = rng.integers(0, n_pages, (n, -(-9200 // page)))
+    table[rng.random(table.shape) < 0.02] = -1
+    kp, vp = make_pool(n_pages, page, 1, d, DT[dt], "rows", 3)
+    q = randn(n, 2, d, seed=5, dtype=DT[dt], scale=2.0)
+    got = run_decode(B, B.make_shape(2, 1, d, dt, 1e4), q.cuda(), kp, vp, ints(table), ints(lens), 0, 0)
+    want, bound = R.decode_batch(q, kp.cpu(), vp.cpu(), torch.from_numpy(table), lens, 0, 0, 2)
+    R.assert_within(got, want, torch.finfo(DT[dt]).eps / 2 * want.abs() * 1.01 + bound, "shared pages")
+
+
 def test_decode_scores_of_any_size(B):
     """One key that outweighs all others, at either end of a long row; scores far from zero on either side."""
     for dt, d in (("bf16", 128), ("f32", 64)):
