@@ -34,6 +34,7 @@ PyObject* current_device = nullptr; // torch._C._cuda_getDevice
 PyObject* current_stream = nullptr; // torch._C._cuda_getCurrentRawStream
 PyObject* str_handle = nullptr;
 PyObject* str_cuda_stream = nullptr;
+PyObject* str_tensors = nullptr;
 
 struct Failed {}; // a Python error is set
 
@@ -466,10 +467,22 @@ void has_type(const at::Tensor& t, const tr_shape& s)
 {
     if (t.scalar_type() != (s.dtype == TR_F32 ? at::kFloat : at::kBFloat16)) fail(PyExc_AssertionError, "a tensor has another type than the shape");
 }
-tr_pages pool(PyObject* o)
+tr_pages pool(PyObject* o, Place& at) // of make_pages(), which keeps the tensors beside it, or filled in by hand
 {
     tr_pages p;
     read_buffer(o, &p, sizeof p);
+    PyObject* t = PyObject_GetAttr(o, str_tensors);
+    if (!t) {
+        PyErr_Clear();
+        return p;
+    }
+    try {
+        if (PyTuple_Check(t) && PyTuple_GET_SIZE(t) == 2) at.on(PyTuple_GET_ITEM(t, 0), false), at.on(PyTuple_GET_ITEM(t, 1), false);
+    } catch (const Failed&) {
+        Py_DECREF(t);
+        throw;
+    }
+    Py_DECREF(t);
     return p;
 }
 
@@ -526,7 +539,7 @@ PyObject* paged_append(Args a) // shape, rotary, q, k, v, q_norm, k_norm, eps, p
     const int32_t* pos = a[8] == Py_None ? nullptr : at.ints_of(a[8], n);
     const int32_t* slots = a[9] == Py_None ? nullptr : at.ints_of(a[9], n);
     tr_pages pg;
-    if (a[11] != Py_None) pg = pool(a[11]);
+    if (a[11] != Py_None) pg = pool(a[11], at);
     const int32_t tokens = small(n);
     void* s = at.stream_of(a[12]);
     return run([&] {
@@ -542,7 +555,7 @@ PyObject* paged_decode(Args a) // shape, q, pages, block_table, kv_lens, window,
     const at::Tensor &q = at.on(a[1]), &out = at.on(a[7]);
     has_type(q, sh);
     has_type(out, sh);
-    const tr_pages pg = pool(a[2]);
+    const tr_pages pg = pool(a[2], at);
     int32_t* table = at.ints(a[3]);
     const at::Tensor& t = tensor(a[3]);
     int64_t n;
@@ -616,6 +629,7 @@ PyMODINIT_FUNC PyInit__tr_host(void)
     import_array();
     str_handle = PyUnicode_InternFromString("handle");
     str_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    if (!str_handle || !str_cuda_stream) return nullptr;
+    str_tensors = PyUnicode_InternFromString("tensors");
+    if (!str_handle || !str_cuda_stream || !str_tensors) return nullptr;
     return PyModule_Create(&module);
 }

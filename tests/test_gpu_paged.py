@@ -190,6 +190,20 @@ def test_append_into_pools_of_any_strides(B, pool, dt):
     check_append(B, dt, 8, 1, 128, 50, 32, 0, pool=pool, page=8, packed=True, seed=4)
 
 
+def test_append_with_the_norm_of_one_side(B):
+    for which in (0, 1):
+        gs = B.make_shape(4, 2, 128, "bf16", 1e4, 1)
+        q, k, v = (randn(11, h, 128, seed=h, dtype=torch.bfloat16) for h in (4, 2, 2))
+        w, p = randn(128, seed=9, dtype=torch.bfloat16), torch.arange(11) * 7
+        kp, vp = make_pool(2, 16, 2, 128, torch.bfloat16, "rows", 3)
+        out = torch.empty_like(q).cuda()
+        B.tr_paged_append(gs, None, q.cuda(), k.cuda(), v.cuda(), w.cuda() if which == 0 else None, w.cuda() if which == 1 else None, EPS, ints(p),
+                          ints(np.arange(11)), out, B.make_pages(kp, vp))
+        for got, x, weight in ((out, q, w if which == 0 else None), (kp.flatten(0, 1)[:11], k, w if which == 1 else None)):
+            want, size = R.heads(x, weight, EPS, p, R.frequencies(128, 1e4), 1)
+            R.assert_within(got, want, R.heads_bound(want, size, torch.bfloat16), "norm of side %d" % which)
+
+
 def test_append_many_tokens(B):
     check_append(B, "bf16", 5, 1, 64, 3001, 64, 1, packed=True, seed=9, page=64)
 
@@ -349,6 +363,27 @@ def test_decode_long_and_many(B, dt):
     check_decode(B, dt, 16, 4, 64, list(np.random.default_rng(5).integers(0, 400, 300)), seed=5, hide=False)
     check_decode(B, dt, 34, 1, 64, list(np.random.default_rng(6).integers(0, 300, 70)), seed=6, hide=False)
     check_decode(B, dt, 1, 1, 64, [0, 700] * 20 + list(np.random.default_rng(7).integers(0, 30, 5000)) + [900], seed=7, hide=False)
+
+
+def test_decode_many_requests_of_many_heads(B):
+    """Rows of two blocks of query heads, joined by the waves that begin them."""
+    check_decode(B, "bf16", 40, 1, 64, list(np.random.default_rng(8).integers(20, 90, 830)), seed=8, hide=False)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_decode_as_many_requests_as_there_may_be(B, dt):
+    """65536 requests of no key or of one, whose value is the result."""
+    n, page = 65536, 8
+    lens = torch.randint(0, 2, (n,), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    kp, vp = make_pool(4096, page, 1, 64, DT[dt], "rows", 3)
+    table = torch.randint(0, 4096, (n, 5), generator=torch.Generator().manual_seed(2), dtype=torch.int32)
+    q = randn(n, 2, 64, seed=5, dtype=DT[dt])
+    got = run_decode(B, B.make_shape(2, 1, 64, dt, 1e4), q.cuda(), kp, vp, table.cuda(), lens.cuda(), 0, 0)
+    want = (vp[table[:, 0].long().cuda(), 0] * lens.cuda()[:, None, None]).expand(n, 2, 64)
+    if dt == "bf16":   # the weight p is off by 2^-16 at most, which rounding to bf16 takes away
+        assert torch.equal(got, want)
+    else:              # p v (1 + e1), e1 of up to two steps of the matrix unit, times 1 / p (1 + e2), (1 + e3): four steps of 2^-24
+        assert ((got.double() - want.double()).abs() <= 4.01 * 2.0 ** -24 * want.double().abs()).all()
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
