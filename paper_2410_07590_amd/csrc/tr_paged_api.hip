@@ -318,9 +318,10 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     }
     a.ws_rows = plan.ws_rows;
     const int64_t workers = std::min<int64_t>((plan.bound + TR_PAGED_MIN_UNITS - 1) / TR_PAGED_MIN_UNITS, TR_PAGED_WORKERS);
-    // The join's workgroups, most of which find nothing to do, are what it costs (some 1 600 a microsecond): it looks at the rows
-    // of the result or at those that each wave may have cut, whichever are fewer.  us of the whole call by row / by wave: 512 requests
-    // of 256 rows, 32 / 8 heads (16384 rows or 4096) 106.4 / 97.4; 200 of 50 to 1200 (6400 or 4096) 101.0 / 99.2.
+    // The join's workgroups, most of which find nothing to do, are what it costs: it looks at the rows of the result or at those
+    // that each wave may have cut, whichever are fewer.  us of the whole call by row / by wave: 200 requests of 50 to 1200 rows, 32 / 8
+    // heads (6400 rows or 4096) 95.9 / 95.1, 512 of 256 (16384 or 4096) 95.0 / 92.2, 4096 of 10 to 60, 16 / 4 heads of 64 (65536 or 4096)
+    // 90.6 / 76.3.
     if (plan.bytes) a.cut = (int64_t)n_req * shape->n_q_heads <= workers * plan.ws_rows ? TR_PAGED_JOIN_BY_ROW : TR_PAGED_JOIN_BY_WAVE;
     return tr_launch_paged_decode(a, shape->dtype, shape->head_dim, (int)workers, (hipStream_t)stream);
     });

@@ -9,7 +9,7 @@
 // sum from kv_lens and finds its own range in it.  No share is longer than another by more than a unit, whatever the mix of
 // lengths, and at most the first and the last item of a share are cut.  Pieces of cut items go to the workspace and a second,
 // small launch joins them.  (Workgroups of four waves that walked an item's keys together and joined them in LDS took 94.3 us for 64 x
-// 4096 rows where this takes 91.0, 97.5 for one request of 131071 rows (90.0), 104 for 200 requests of 50 to 1200 rows (99.5):
+// 4096 rows where this takes 90.3, 97.5 for one request of 131071 rows (90.2), 104 for 200 requests of 50 to 1200 rows (95.1):
 // their waves wait for one another at the end of each item.)
 //
 // Products.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16 (fp32: 16x16x4), keys and values as the A operands from
@@ -24,8 +24,8 @@
 // its next units in one register, a lane each, and takes them out as scalars.
 //
 // Heads of 128 channels, bf16, fresh pools every pass, us of the whole call (replayed graph): 64 requests of 4096 rows, 28 / 4 heads,
-// pages of 64: 91 (538 MB: 5.9 TB/s; the first kernel alone 80 to 82, 6.6 TB/s); one of 131071, 32 / 8 heads, pages of 16: 90;
-// 32 of up to 32000 rows through a window of 4000 and 4 first tokens: 85 (489 MB); five of 300 to 3000 rows: 13.4; one of 700: 8.4,
+// pages of 64: 90 (538 MB: 6.0 TB/s; the first kernel alone 80 to 82, 6.6 TB/s); one of 131071, 32 / 8 heads, pages of 16: 90;
+// 32 of up to 32000 rows through a window of 4000 and 4 first tokens: 84 (489 MB); five of 300 to 3000 rows: 13.3; one of 700: 8.3,
 // which is two launches and, in the first, four dependent trips to memory (lengths, page ids, keys, results).
 #include "tr_device.h"
 #include "tr_internal.h"
@@ -569,10 +569,10 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
 // Joins the pieces of cut items: out = sum_p f_p O_p / sum_p f_p l_p with f_p = 2^(m_p - max m).  One workgroup per row of the
 // result, or per row of the item that a wave of the first launch begins; groups of D / 4 lanes take every GROUPS-th piece and
 // are joined through LDS.
-template <int DTYPE, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs a, int rows_per_tile)
+template <int DTYPE, int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void paged_join_kernel(const TrPagedDecodeArgs a, int rows_per_tile)
 {
-    constexpr int LPR = D / 4, GROUPS = 256 / LPR;
+    constexpr int LPR = D / 4, GROUPS = THREADS / LPR;
     __shared__ f32x4 os[GROUPS][LPR];
     __shared__ float2 mls[GROUPS];
     const int tid = threadIdx.x, grp = tid / LPR, piece = tid % LPR;
@@ -598,17 +598,19 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const TrPagedDecodeArgs
     if (item.y <= 1) return;
     float M = NOTHING, L = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int AHEAD = 4; // with eight, 64 x 4096 rows take 94.4 us (90.9): most rows have fewer pieces
+    constexpr int AHEAD = 1024 / THREADS < 8 ? 1024 / THREADS : 8;
     for (int p0 = grp; p0 < item.y; p0 += GROUPS * AHEAD) {
         f32x4 x[AHEAD];
         float2 ml[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int p = p0 + GROUPS * i;
-            const int64_t slot = (int64_t)(2 * (item.x + min(p, item.y - 1)) + (p == 0)) * a.ws_rows + row;
-            x[i] = *(const f32x4*)(a.ws_o + slot * D + 4 * piece);
-            ml[i] = *(const float2*)(a.ws_ml + slot * 2);
-            if (p >= item.y) ml[i] = make_float2(NOTHING, 0.0f), x[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            const int64_t slot = (int64_t)(2 * (item.x + p) + (p == 0)) * a.ws_rows + row;
+            ml[i] = make_float2(NOTHING, 0.0f), x[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (p < item.y) {
+                x[i] = *(const f32x4*)(a.ws_o + slot * D + 4 * piece);
+                ml[i] = *(const float2*)(a.ws_ml + slot * 2);
+            }
         }
         float top = M;
 #pragma unroll
@@ -653,10 +655,15 @@ template <int DTYPE, int D, int NT> int launch_decode(const TrPagedDecodeArgs& a
     static_assert(lds >= 2 * Rows<DTYPE, D>::BYTES + 256 + 16 * NT * Rows<DTYPE, D>::ROW && lds <= 64 * 1024, "");
     paged_decode_kernel<DTYPE, D, NT><<<dim3(grid), dim3(64), lds, s>>>(a);
     TR_HIP(hipGetLastError());
-    if (a.cut) {
-        paged_join_kernel<DTYPE, D><<<dim3(a.cut == TR_PAGED_JOIN_BY_WAVE ? grid * a.ws_rows : a.n_req * a.n_q_heads), dim3(256), 0, s>>>(a, 16 * NT);
-        TR_HIP(hipGetLastError());
-    }
+    if (!a.cut) return TR_OK;
+    // Items have 1 + (waves / items) pieces on average.  Where there are few items, and many pieces of each, more threads read
+    // them sooner; else most of a workgroup has nothing to read, and starting it is what the join costs.  us of the whole call with 256 / 64
+    // threads: one request of 5000 rows (8 items) 12.6 / 14.3, five of 300 to 3000 (40) 13.3 / 14.1, 16 of 2000 (64) 19.2 / 19.4, 24 of up to 9000
+    // (96) 23.4 / 23.0, 64 of 4096 (256) 90.7 / 90.0, 256 of 20 to 400 (1024) 25.6 / 22.9, 200 of 50 to 1200 (1600) 99.3 / 95.0.
+    const dim3 rows(a.cut == TR_PAGED_JOIN_BY_WAVE ? grid * a.ws_rows : a.n_req * a.n_q_heads);
+    if ((int64_t)a.n_req * a.n_kv_heads < 96) paged_join_kernel<DTYPE, D, 256><<<rows, dim3(256), 0, s>>>(a, 16 * NT);
+    else paged_join_kernel<DTYPE, D, 64><<<rows, dim3(64), 0, s>>>(a, 16 * NT);
+    TR_HIP(hipGetLastError());
     return TR_OK;
 }
 template <int DTYPE> int launch_decode(const TrPagedDecodeArgs& a, int head_dim, int grid, hipStream_t s)
