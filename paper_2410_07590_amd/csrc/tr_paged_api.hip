@@ -186,6 +186,7 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     const int64_t e = tr_elem_bytes(shape), q_row = (int64_t)shape->n_q_heads * shape->head_dim, kv_row = (int64_t)shape->n_kv_heads * shape->head_dim;
     if (pages) {
         if (int rc = pool_of(who, shape, pages, &a.pool)) return rc;
+        if (pages->k == pages->v) return tr_fail(TR_ERR_INVALID_ARG, "%s: k and v of the pages are the same rows", who);
     }
     if (n_tokens == 0 || (!q && !k)) return TR_OK;
     if (a.rotary_dim && !pos) return tr_fail(TR_ERR_INVALID_ARG, "%s: pos is NULL", who);

@@ -159,7 +159,7 @@ def rotary(**kw):
     (dict(out=FAKE[0] + 256), -1), (dict(out=FAKE[0], qs=28 * 128 + 8), -1), (dict(out=FAKE[1]), -1), (dict(out=FAKE[2] + 4096), -1),
     (dict(k=FAKE[10] + 1024), -1), (dict(out=FAKE[11]), -1), (dict(q=FAKE[11] + 99 * 16384 + 15 * 1024 + 768, qs=0), -1),
     (dict(pages=pages(page_size=12)), -1), (dict(pages=pages(page_size=4)), -1), (dict(pages=pages(n_pages=0)), -1), (dict(pages=pages(n_pages=2 ** 27)), -1),
-    (dict(pages=pages(reserved=1)), -1), (dict(pages=pages(k=0)), -1), (dict(pages=pages(v=FAKE[11] + 8)), -1), (dict(pages=pages(row_stride=64)), -1),
+    (dict(pages=pages(reserved=1)), -1), (dict(pages=pages(k=0)), -1), (dict(pages=pages(v=FAKE[11] + 8)), -1), (dict(pages=pages(v=FAKE[10])), -1), (dict(pages=pages(row_stride=64)), -1),
     (dict(pages=pages(row_stride=516)), -1), (dict(pages=pages(head_stride=0)), -1), (dict(pages=pages(page_stride=-8192)), -1),
     (dict(pages=pages(page_stride=2 ** 60)), B.TR_ERR_UNSUPPORTED), (dict(pages=pages(page_stride=2 ** 31)), B.TR_ERR_UNSUPPORTED),
     (dict(pages=pages(row_stride=2 ** 26)), B.TR_ERR_UNSUPPORTED)])
