@@ -138,10 +138,20 @@ __global__ __launch_bounds__(256) void page_map_kernel(const TrPageMapArgs a)
             for (int i = 0; i < 4 && t0 + i < a.n_slots; ++i) a.slots[t0 + i] = slot[i], a.pos[t0 + i] = pos[i];
         }
     }
-    for (int64_t p = (int64_t)blockIdx.x * 256 + tid; p < n_pag; p += (int64_t)gridDim.x * 256) {
+    const int64_t step = (int64_t)gridDim.x * 256;
+    for (int64_t p = (int64_t)blockIdx.x * 256 + tid; p < n_pag; p += step) {
         const int r = owner(pg, a.n_req, (int)p);
         const int64_t blk = pages((uint32_t)held[r]) + p - pg[r];
         if (blk < a.max_blocks) a.table[(int64_t)r * a.max_blocks + blk] = free_page(p);
+        else p += (pg[r + 1] - 1 - p) / step * step; // nor do the request's other pages have an entry
+    }
+    if (n_pag != INT32_MAX) return;
+    for (int r = 0; r < a.n_req; ++r) { // entries of pages behind the cut sum
+        if (pg[r + 1] != INT32_MAX) continue;
+        const Lens l = lens(r);
+        const int64_t need = min((int64_t)pages(l.c + l.f), (int64_t)a.max_blocks);
+        for (int64_t blk = (int64_t)pages(l.c) + (INT32_MAX - pg[r]) + (int64_t)blockIdx.x * 256 + tid; blk < need; blk += step)
+            a.table[(int64_t)r * a.max_blocks + blk] = -1;
     }
 }
 

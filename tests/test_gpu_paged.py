@@ -95,6 +95,18 @@ def test_map_where_pages_or_columns_run_out_and_lengths_are_absurd(B):
     check_map(B, cached, new, None, 16, free, table, 3000)
 
 
+@pytest.mark.parametrize("page", [8, 16])
+def test_map_of_more_pages_than_can_be_counted(B, page):
+    # the sum of pages is cut within the ninth (17th) request: what is behind it gets no page, and no entry keeps its old one
+    huge = 2 ** 31 - 1
+    cached = np.array([3] + [0, 5, huge] * 12 + [4, page, 0])
+    new = np.array([9] + [huge, huge, 7] * 12 + [30, 2 * page, 1])
+    free, table = np.arange(50, 110), np.full((len(cached), 9), 3)
+    check_map(B, cached, new, None, page, free, table, 2000)
+    check_map(B, cached[::-1].copy(), new[::-1].copy(), None, page, free, table, 2000)
+    check_map(B, np.zeros(4096, int), np.full(4096, huge), None, page, free, np.full((4096, 3), 3), 10)
+
+
 # ---- heads into pages ------------------------------------------------------------------------------------------------------------
 
 
