@@ -363,7 +363,7 @@ int tr_rotary_init(int32_t layout, int32_t rotary_dim, double base, int32_t scal
  *   pos: device int32 [n_tokens] (NULL with a rotary of no channels), slots: device int32 [n_tokens], -1 or pairwise different
  *   (of two tokens with one slot either may be the one that is kept, in parts).
  * The sum of squares, the angle (64 bits) and all products are fp32 or wider.  Pointers and strides 16-byte aligned, outputs apart
- * from all other tensors, else TR_ERR_INVALID_ARG.  n_tokens == 0 is a no-op. */
+ * from all other tensors, else TR_ERR_INVALID_ARG.  n_q_heads <= 2^20 (else TR_ERR_UNSUPPORTED).  n_tokens == 0 is a no-op. */
 int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* q, int64_t q_stride, const void* k,
                     int64_t k_stride, const void* v, int64_t v_stride, const void* q_norm, const void* k_norm, double eps,
                     const int32_t* pos, const int32_t* slots, int32_t n_tokens, void* q_out, const tr_pages* pages, void* stream);
@@ -380,7 +380,7 @@ int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* 
  * value that is infinite makes NaN of its channel).  The bits of a result depend on the batch's lengths, window and sinks, which
  * decide how it is shared out, not on the table's width or the order of pages.
  * workspace: tr_paged_decode_attn_workspace_size() bytes, 256-byte aligned, else TR_ERR_WORKSPACE; it depends on the arguments
- * of the query alone, not on the lengths; calls that may overlap in time need one each.  q, out and pages 16-byte aligned.
+ * of the query alone, not on the lengths (0 for sizes that the call refuses); calls that may overlap in time need one each.  q, out and pages 16-byte aligned.
  * max_blocks * page_size <= 2^30; n_req <= 65536, n_req * n_q_heads < 2^24 and
  * n_req * n_q_heads * max_blocks * page_size < 2^33 (else TR_ERR_UNSUPPORTED); n_req == 0 is a no-op. */
 size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size);

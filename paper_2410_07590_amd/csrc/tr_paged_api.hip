@@ -9,6 +9,10 @@
 namespace {
 
 const int64_t INT_LIMIT = ((int64_t)1 << 31) - 1;
+const int32_t MOST_HEADS = 1 << 20;     // with 2^31 tokens of them, counts of bytes stay below 2^62
+const int32_t MOST_REQUESTS = 65536;    // of a decode step
+const int64_t MOST_KEYS = 1ll << 30;    // that a row of the table has room for
+const int64_t MOST_UNITS = 1ll << 30;   // of a batch: the kernel counts them in 32 bits
 
 int page_shift(int32_t page_size)
 {
@@ -159,6 +163,7 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     const char* const who = "tr_paged_append";
     if (int rc = tr_check_shape(shape)) return rc;
     if (n_tokens < 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: n_tokens < 0", who);
+    if (shape->n_q_heads > MOST_HEADS) return tr_fail(TR_ERR_UNSUPPORTED, "%s: %d heads, at most 2^20", who, shape->n_q_heads);
     if ((q != nullptr) != (q_out != nullptr)) return tr_fail(TR_ERR_INVALID_ARG, "%s: q and q_out go together", who);
     const int given = (k != nullptr) + (v != nullptr) + (slots != nullptr) + (pages != nullptr);
     if (n_tokens > 0 && given != 0 && given != 4) return tr_fail(TR_ERR_INVALID_ARG, "%s: k, v, slots and pages go together", who);
@@ -228,7 +233,7 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     // A workgroup takes as many tokens as give its threads eight units each, if there are workgroups enough then.  us for 1 token /
     // this: 24000 rows of 4 KV heads of 128 51.2 / 23.8, 16000 tokens of 16 + 4 heads of 64 50.0 / 23.3, 16001 of 32 + 8 of 128 88.6 / 83.0
     // (twice as many: 84.9).
-    const int64_t units = (a.n_q_heads + 2 * a.n_kv_heads) * shape->head_dim * e / 16; // of a token
+    const int64_t units = (int64_t)(a.n_q_heads + 2 * a.n_kv_heads) * shape->head_dim * e / 16; // of a token
     while ((2 << a.tile_shift) <= TR_PAGED_APPEND_TOKENS && (units << a.tile_shift) * 2 <= 2048 && n_tokens >= 2048ll << a.tile_shift) ++a.tile_shift;
     // Streamed stores make the call itself faster at any size, and what reads its results next slower where the caches still
     // hold them: us of the call and a pass over all it wrote, ordinary / streamed, by MB written: 12 MB 18.6 / 17.9, 25 MB 27.9 / 29.4, 49 MB
@@ -268,7 +273,9 @@ extern "C" size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int
     return tr_guard_size([&]() -> size_t {
     tr_clear_error();
     if (tr_check_shape(shape) || n_req < 1 || max_blocks < 1 || page_shift(page_size) < 0) return 0;
-    return decode_plan(shape, n_req, (int64_t)max_blocks * page_size).bytes;
+    if (n_req > MOST_REQUESTS || (int64_t)n_req * shape->n_q_heads > TR_MAX_BLOCKS_256 || (int64_t)max_blocks * page_size > MOST_KEYS) return 0; // refused
+    const DecodePlan plan = decode_plan(shape, n_req, (int64_t)max_blocks * page_size);
+    return plan.bound > MOST_UNITS ? 0 : plan.bytes;
     });
 }
 
@@ -281,12 +288,12 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     const char* const who = "tr_paged_decode_attn";
     if (int rc = tr_check_shape(shape)) return rc;
     if (n_req < 0 || max_blocks < 0 || window < 0 || n_sink < 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: a count is negative", who);
-    if (n_req > 65536) return tr_fail(TR_ERR_UNSUPPORTED, "%s: %d requests, at most 65536", who, n_req);
+    if (n_req > MOST_REQUESTS) return tr_fail(TR_ERR_UNSUPPORTED, "%s: %d requests, at most %d", who, n_req, MOST_REQUESTS);
     if (!pages) return tr_fail(TR_ERR_INVALID_ARG, "%s: pages is NULL", who);
     TrPagedDecodeArgs a;
     memset(&a, 0, sizeof a);
     if (int rc = pool_of(who, shape, pages, &a.pool)) return rc;
-    if ((int64_t)max_blocks * pages->page_size > ((int64_t)1 << 30)) return tr_fail(TR_ERR_INVALID_ARG, "%s: max_blocks %d", who, max_blocks);
+    if ((int64_t)max_blocks * pages->page_size > MOST_KEYS) return tr_fail(TR_ERR_INVALID_ARG, "%s: max_blocks %d", who, max_blocks);
     if ((int64_t)n_req * shape->n_q_heads > TR_MAX_BLOCKS_256) return tr_fail(TR_ERR_UNSUPPORTED, "%s: more than 2^24 (request, head) pairs", who);
     if (n_req == 0) return TR_OK;
     if (!q || !out || !kv_lens || (max_blocks > 0 && !block_table)) return tr_fail(TR_ERR_INVALID_ARG, "%s: an array is NULL", who);
@@ -309,7 +316,7 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     a.group = shape->n_q_heads / shape->n_kv_heads;
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)shape->head_dim));
     const DecodePlan plan = decode_plan(shape, n_req, (int64_t)max_blocks * pages->page_size);
-    if (plan.bound > ((int64_t)1 << 30)) return tr_fail(TR_ERR_UNSUPPORTED, "%s: the table has room for more than 2^30 units of 32 (fp32: 16) keys", who);
+    if (plan.bound > MOST_UNITS) return tr_fail(TR_ERR_UNSUPPORTED, "%s: the table has room for more than 2^30 units of 32 (fp32: 16) keys", who);
     if (plan.bytes) {
         if (!workspace || ((uintptr_t)workspace & 255)) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace missing or not 256-byte aligned", who);
         if (workspace_bytes < plan.bytes) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace holds %zu bytes, %zu needed", who, workspace_bytes, plan.bytes);

@@ -210,6 +210,20 @@ def test_workspace_queries_that_make_no_sense_are_zero(L):
         assert B.tr_paged_decode_attn_workspace_size(*args) == 0
 
 
+def test_workspace_queries_of_sizes_that_are_refused_are_zero(L):
+    most = 2 ** 31 - 1
+    for args in ((shape(), 65537, 1, 16), (shape(), most, most, 1024), (shape(hq=most, hkv=most), most, most, 1024), (shape(hq=4096, hkv=4096), 4096, 9, 16),
+                 (shape(), 1, 2 ** 20 + 1, 1024), (shape(), 4096, 2 ** 18, 16)):
+        assert B.tr_paged_decode_attn_workspace_size(*args) == 0
+    assert B.tr_paged_decode_attn_workspace_size(shape(), 65536, 9, 16) > 0
+    assert B.tr_paged_decode_attn_workspace_size(shape(), 1, 2 ** 20, 1024) > 0
+
+
+def test_append_of_too_many_heads(L):
+    big = shape(hq=2 ** 20 + 1, hkv=2 ** 20 + 1)
+    assert append(L, shape=big, pages=pages(n_kv_heads=2 ** 20 + 1)) == B.TR_ERR_UNSUPPORTED
+
+
 # ---- the binding ------------------------------------------------------------------------------------------------------------------
 
 def fake(*size, dtype=torch.int32):
