@@ -549,6 +549,26 @@ def test_decode_repeats_bit_for_bit_and_on_another_stream(B):
     assert torch.equal(first, again) and torch.equal(first, wider) and torch.equal(first, handed)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_decodes_that_overlap_on_two_streams(B, dt):
+    rng = np.random.default_rng(2)
+    jobs = []
+    for lens, page, hq, hk in (([4000, 30, 900], 16, 8, 2), ([20] * 200 + [3000], 64, 20, 1)):   # the second with two blocks of heads
+        table, n_pages = tables(rng, lens, page)
+        kp, vp = make_pool(n_pages, page, hk, 128, DT[dt], "rows", page)
+        q, gs = randn(len(lens), hq, 128, seed=5, dtype=DT[dt]).cuda(), B.make_shape(hq, hk, 128, dt, 1e4)
+        need = B.tr_paged_decode_attn_workspace_size(gs, len(lens), table.shape[1], page)
+        alone = run_decode(B, gs, q, kp, vp, ints(table), ints(lens), 700, 3)
+        jobs.append((gs, q, B.make_pages(kp, vp), ints(table), ints(lens), B.workspace(need), alone, [torch.empty_like(q) for _ in range(8)], torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for i in range(8):
+        for gs, q, pool, table, lens, ws, _, outs, s in jobs:
+            B.tr_paged_decode_attn(gs, q, pool, table, lens, 700, 3, outs[i], ws, s)
+    torch.cuda.synchronize()
+    for job in jobs:
+        assert all(torch.equal(job[6], out) for out in job[7])
+
+
 # ---- together --------------------------------------------------------------------------------------------------------------------
 
 
