@@ -15,8 +15,8 @@
 // Products.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16 (fp32: 16x16x4), keys and values as the A operands from
 // LDS (bf16 V through the transposing read), so that a lane owns one query column: its maximum and denominator are scalars, and
 // its share of S^T is, up to the order of the keys, its B operand of the second product.  A bf16 product takes the weights as
-// two bf16 parts, which keeps 16 bits of them: the matrix unit is idle most of the time (64 x 4096 rows: 91.1 us, 90.9 with one
-// part), and the error against 64 bits is then that of rounding the result, 1.667e-3 of its norm (2.270e-3 with one part).
+// three bf16 parts, which together are the fp32 weight: the matrix unit is idle most of the time, and the error against 64 bits is
+// then that of rounding the result, 1.667e-3 of its norm (2.270e-3 with one part), also where values cancel.
 //
 // Data movement.  A wave has room for one unit of K and of V (8 KB each at 128 channels) and refills them as soon as their
 // operands are read, straight from memory to LDS, counted waits instead of barriers; the first unit of its next item is on its
@@ -335,7 +335,6 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
                     for (int e = 0; e < 4; ++e)
                         if (!(mine & (1u << (16 * kb + e)))) s[n][kb][e] = -INFINITY;
         }
-        bf16x8 hi[NT], lo[NT]; // fp32: the weights stay in s
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float top = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3]));
@@ -356,12 +355,7 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             for (int i = 0; i < 4 * KB; ++i) {
                 const float w = __builtin_amdgcn_exp2f(fmaf(s[n][i >> 2][i & 3], scale, -acc.m[n]));
                 sum += w;
-                if constexpr (BF16) {
-                    hi[n][i] = (__bf16)w;
-                    lo[n][i] = (__bf16)(w - (float)hi[n][i]);
-                } else {
-                    s[n][0][i] = w;
-                }
+                s[n][i >> 2][i & 3] = w;
             }
             acc.l[n] += sum;
         }
@@ -381,6 +375,20 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
         }
         wait_lds(); // the unit's values are read
         if (!last) st.template issue<true, true>(v, next, ids);
+        bf16x8 parts[NT][3]; // of the weights; fp32: they stay in s.  Not sooner: the next values are on their way meanwhile
+        if constexpr (BF16) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4 * KB; ++i) {
+                    float rest = s[n][i >> 2][i & 3];
+#pragma unroll
+                    for (int j = 0; j < 3; ++j) {
+                        parts[n][j][i] = (__bf16)rest;
+                        rest -= (float)parts[n][j][i];
+                    }
+                }
+        }
         if (cur.seen != ALL) { // what is not seen may be anything, and even a weight of zero would make NaN of NaN
             u32x4 keep; // bf16: element j of an operand is key 16 (j >> 2) + 4 quad + (j & 3)
 #pragma unroll
@@ -399,8 +407,8 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
 #pragma unroll
             for (int cb = 0; cb < D / 16; ++cb) {
                 if constexpr (BF16) {
-                    acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], hi[n], acc.o[n][cb], 0, 0, 0);
-                    acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], lo[n], acc.o[n][cb], 0, 0, 0);
+#pragma unroll
+                    for (int j = 0; j < 3; ++j) acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], parts[n][j], acc.o[n][cb], 0, 0, 0);
                 } else { // operand cb holds key cb % 4 of the four; its channel i goes to block 4 (cb / 4) + i
 #pragma unroll
                     for (int i = 0; i < 4; ++i)

@@ -1,0 +1,60 @@
+"""Paged decode attention where the values of its inputs are hard: weights that cancel, scores far from zero, infinite values and
+values near the largest, each against the definition in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import paged_bounds as P
+from tests.test_gpu_paged import B, DT, ints, make_pool, randn, run_decode, tables  # noqa: F401  (B: the fixture)
+
+pytestmark = pytest.mark.gpu
+BOTH = pytest.mark.parametrize("dt", ["bf16", "f32"])
+
+
+# ---- weights -------------------------------------------------------------------------------------------------------------------
+
+
+@BOTH
+@pytest.mark.parametrize("d", [64, 128])
+def test_weights_keep_the_bits_of_fp32(B, dt, d):
+    """Three keys of weights 1, w and about 1 - w with values 1, -1 and -1: what is left is what the weights lost.
+
+    Scores of one product of powers of two and sums of two exact ones, all exact.  A weight is off by its argument (|x| <= 4.4 log2
+    units, three roundings: 3 * 4.4 * ln 2 = 9.2 steps of 2^-24) and its exponential (2 steps); the weighted sum by at most 9 additions
+    of two steps each, on something of size 1; the sum of weights is 2: (11.2 * 1 + 18) / 2 = 14.6 steps, and one rounding of the result."""
+    n = 64
+    w = torch.linspace(0.05, 0.95, n).double()
+    q = torch.zeros(n, 2, d, dtype=DT[dt])
+    q[..., 0] = q[..., 5] = 1.0
+    kp = torch.zeros(n, 8, 1, d, dtype=DT[dt])
+    for j, x in ((1, w), (2, 1 - w)):
+        s = math.sqrt(d) * torch.log(x)
+        kp[:, j, 0, 0] = s.to(torch.bfloat16).to(DT[dt])
+        kp[:, j, 0, 5] = (s - kp[:, j, 0, 0].double()).to(torch.bfloat16).to(DT[dt])
+    vp = torch.ones(n, 8, 1, d, dtype=DT[dt])
+    vp[:, 1:] = -1.0
+    got = run_decode(B, B.make_shape(2, 1, d, dt, 1e4), q.cuda(), kp.cuda(), vp.cuda(), ints(np.arange(n)[:, None]), ints([3] * n), 0, 0).cpu().double()
+    s = (kp[:, :3, 0, 0].double() + kp[:, :3, 0, 5].double()) / math.sqrt(d)
+    p = torch.softmax(s, 1)
+    want = (p[:, 0] - p[:, 1] - p[:, 2])[:, None, None].expand_as(got)
+    assert want.abs().max() < 2.0 ** -7
+    err = (got - want).abs() - torch.finfo(DT[dt]).eps / 2 * want.abs() * 1.01
+    assert float(err.max()) <= 14.6 * 2.0 ** -24, float(err.max()) * 2.0 ** 24
+
+
+@BOTH
+@pytest.mark.parametrize("d,hq,hk,page", [(64, 8, 2, 16), (128, 8, 2, 8), (128, 20, 1, 64), (64, 40, 1, 32), (128, 4, 4, 256)])
+def test_errors_are_those_of_single_precision(B, dt, d, hq, hk, page):
+    """The norm of the error and every element of it, for data whose roundings are independent (tests/test_paged_bounds.py shows
+    that operands or weights of 16 bits would be noticed)."""
+    lens = [7, 60, 513, 33, 300]
+    table, n_pages = tables(np.random.default_rng(d + hq), lens, page)
+    kp, vp = make_pool(n_pages, page, hk, d, DT[dt], "rows", hq)
+    q = randn(len(lens), hq, d, seed=d, dtype=DT[dt], scale=0.5)
+    got = run_decode(B, B.make_shape(hq, hk, d, dt, 1e4), q.cuda(), kp, vp, ints(table), ints(lens), 0, 0)
+    want, dev = P.decode_batch(q, kp.cpu(), vp.cpu(), table, [range(n) for n in lens], hq // hk)
+    for r, n in enumerate(lens):
+        norm, element = P.excess(got[r], want[r], dev[r], DT[dt])
+        assert norm <= 1 and element <= 1, (n, norm, element)
