@@ -446,7 +446,7 @@ struct TrPagedDecodeArgs {
     int32_t cut;       // 0: no item can be cut; else a second launch joins their pieces: TR_PAGED_JOIN_BY_ROW, _BY_WAVE
     int32_t ws_rows;   // rows of a piece
     float* ws_o;       // [2 workers][ws_rows][head_dim] sums of a piece: 2 w of the item that worker w continues, 2 w + 1 of the one it begins
-    float* ws_ml;      // [2 workers][ws_rows][2] reference maximum (log2 domain) and denominator
+    float* ws_ml;      // [2 workers][ws_rows][2] reference maximum (an unscaled score) and denominator
     int32_t* ws_items; // by row: [items][2] wave that begins an item, number of its pieces; by wave: [waves][2] item it begins and cuts, number of pieces
 };
 int tr_launch_page_map(const TrPageMapArgs& a, hipStream_t s);

@@ -40,9 +40,9 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 #define CONST_AS __attribute__((address_space(4)))
 
-constexpr float SLACK = 8.0f;        // log2 units by which a score may exceed the reference before it moves
-constexpr float NOTHING = -3.0e38f;  // reference of a row that has seen no key
-constexpr int DMA_STREAM = 2;        // non-temporal: every key is read once
+constexpr float SLACK = 8.0f;                 // log2 units by which a score may exceed the reference before it moves
+constexpr float NOTHING = -__FLT_MAX__;       // reference of a row that has seen no key
+constexpr int DMA_STREAM = 2;                 // non-temporal: every key is read once
 // Loads of 1 KB that a wave has on their way.  us with 5 / 6 / 7 / 8: 64 x 4096 rows 94.1 / 91.4 / 92.6 / 96.5, one request of 131071 92.9 /
 // 90.2 / 90.4 / 92.9, windows over 32 requests 87.6 / 85.5 / 86.8 / 90.9, 200 requests of 50 to 1200 105.0 / 103.2 / 103.1 / 103.2.
 constexpr int FLIGHT = 6;
@@ -129,7 +129,7 @@ template <int UNIT> struct Piece {
 };
 
 // What one wave accumulates: O^T of query column lane % 16 (bf16: element e of block b is channel 16 b + 4 (lane / 16) + e; fp32:
-// channel 64 (b / 4) + 16 (lane / 16) + 4 e + b % 4), reference maximum (log2 domain) and this lane's share of the denominator.
+// channel 64 (b / 4) + 16 (lane / 16) + 4 e + b % 4), reference maximum (a score, not yet scaled) and this lane's share of the denominator.
 template <int D, int NT> struct Acc {
     f32x4 o[NT][D / 16];
     float m[NT], l[NT];
@@ -339,10 +339,10 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
         for (int n = 0; n < NT; ++n) {
             float top = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3]));
             if (KB == 2) top = fmaxf(top, fmaxf(fmaxf(s[n][KB - 1][0], s[n][KB - 1][1]), fmaxf(s[n][KB - 1][2], s[n][KB - 1][3])));
-            top *= scale;
-            // the reference is exact wherever it is: it only has to stay near enough for the exponential's range
-            if (__any(top > acc.m[n] + SLACK)) {
-                const float to = fmaxf(acc.m[n], column_reduce<true>(top)), alpha = __builtin_amdgcn_exp2f(acc.m[n] - to);
+            // A weight is 2^((s - m) scale), the difference first: it is exact or nearly so however large the scores are, where that of
+            // two products with the scale would be off by their roundings.  The reference only has to stay near enough for the exponential's range.
+            if (__any((top - acc.m[n]) * scale > SLACK)) {
+                const float to = fmaxf(acc.m[n], column_reduce<true>(top)), alpha = __builtin_amdgcn_exp2f((acc.m[n] - to) * scale);
                 acc.m[n] = to;
                 acc.l[n] *= alpha;
 #pragma unroll
@@ -353,7 +353,7 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < 4 * KB; ++i) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(s[n][i >> 2][i & 3], scale, -acc.m[n]));
+                const float w = __builtin_amdgcn_exp2f((s[n][i >> 2][i & 3] - acc.m[n]) * scale);
                 sum += w;
                 s[n][i >> 2][i & 3] = w;
             }
@@ -574,7 +574,7 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
     }
 }
 
-// Joins the pieces of cut items: out = sum_p f_p O_p / sum_p f_p l_p with f_p = 2^(m_p - max m).  One workgroup per row of the
+// Joins the pieces of cut items: out = sum_p f_p O_p / sum_p f_p l_p with f_p = 2^((m_p - max m) scale).  One workgroup per row of the
 // result, or per row of the item that a wave of the first launch begins; groups of D / 4 lanes take every GROUPS-th piece and
 // are joined through LDS.
 template <int DTYPE, int D, int THREADS>
@@ -623,12 +623,12 @@ __global__ __launch_bounds__(THREADS) void paged_join_kernel(const TrPagedDecode
         float top = M;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, ml[i].x);
-        const float old = __builtin_amdgcn_exp2f(M - top);
+        const float old = __builtin_amdgcn_exp2f((M - top) * a.scale_log2e);
         L *= old;
         o *= old;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const float f = __builtin_amdgcn_exp2f(ml[i].x - top);
+            const float f = __builtin_amdgcn_exp2f((ml[i].x - top) * a.scale_log2e);
             L = fmaf(f, ml[i].y, L);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[i][e], o[e]);
@@ -645,7 +645,7 @@ __global__ __launch_bounds__(THREADS) void paged_join_kernel(const TrPagedDecode
     for (int g = 0; g < GROUPS; ++g) top = fmaxf(top, mls[g].x);
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-        const float f = __builtin_amdgcn_exp2f(mls[g].x - top);
+        const float f = __builtin_amdgcn_exp2f((mls[g].x - top) * a.scale_log2e);
         total = fmaf(f, mls[g].y, total);
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = fmaf(f, os[g][piece][e], y[e]);

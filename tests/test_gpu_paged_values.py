@@ -58,3 +58,52 @@ def test_errors_are_those_of_single_precision(B, dt, d, hq, hk, page):
     for r, n in enumerate(lens):
         norm, element = P.excess(got[r], want[r], dev[r], DT[dt])
         assert norm <= 1 and element <= 1, (n, norm, element)
+
+
+# ---- scores far from zero ----------------------------------------------------------------------------------------------------------
+
+
+@BOTH
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_only_key_has_weight_one_whatever_its_score(B, dt, d):
+    """One visible row per request: its value is the result, bit for bit (a weight that is a power of two, divided by itself).  Scores of
+    either sign up to d * 2^118, also one whose product with the scale is far from an fp32 number: 39936^2 * d."""
+    sizes = [0.0, 2.0 ** -60, 1.0, 39936.0, 3.0 * 2 ** 20, 1.7e9, 2.0 ** 40, 1.1e15, 5.0e17]
+    sizes = [x for x in sizes for _ in (0, 1)]
+    n = len(sizes)
+    size = torch.tensor(sizes)
+    sign = torch.tensor([1.0, -1.0] * (n // 2))
+    noise = 1 + torch.rand(n, 1, d, generator=torch.Generator().manual_seed(d)) / 8
+    noise[6:8] = 1.0   # as it stands
+    q = (size[:, None, None] * noise).to(DT[dt]).expand(n, 4, d).contiguous()
+    for page in (8, 64):
+        kp, vp = make_pool(n, page, 1, d, DT[dt], "rows", page)
+        kp[:, 0, 0] = (size * sign).cuda().to(DT[dt])[:, None]
+        got = run_decode(B, B.make_shape(4, 1, d, dt, 1e4), q.cuda(), kp, vp, ints(np.arange(n)[:, None]), ints([1] * n), 0, 0)
+        assert torch.equal(got, vp[:, 0].expand(n, 4, d))
+
+
+@BOTH
+@pytest.mark.parametrize("lens", [[5], [40, 3, 700], [40000], [900] * 60], ids=str)
+def test_equal_keys_share_the_weight_whatever_their_score(B, dt, lens):
+    """Every third key equal and the others with half its score, which gives them no weight, or twice it where scores are negative: the
+    mean of the values, over shares of several units and joined pieces.  Sums: as in tests/paged_reference.py."""
+    d, page = 64, 16
+    table, n_pages = tables(np.random.default_rng(1), lens, page)
+    kp, vp = make_pool(n_pages, page, 1, d, DT[dt], "rows", 3)
+    for size, sign in ((39936.0, 1.0), (39936.0, -1.0), (1.1e15, 1.0), (1.1e15, -1.0)):
+        q = torch.full((len(lens), 2, d), size, dtype=DT[dt])
+        low = 0.5 if sign > 0 else 2.0
+        k = torch.full((n_pages * page, 1, d), size * sign * low, dtype=DT[dt])
+        top = []
+        for r, n in enumerate(lens):
+            rows = torch.as_tensor(table[r][np.arange(0, n, 3) // page] * page + np.arange(0, n, 3) % page)
+            k[rows] = size * sign
+            top.append(rows)
+        kp.copy_(k.view_as(kp))
+        got = run_decode(B, B.make_shape(2, 1, d, dt, 1e4), q.cuda(), kp, vp, ints(table), ints(lens), 0, 0).cpu().double()
+        v = vp.cpu().double().view(-1, d)
+        for r, rows in enumerate(top):
+            want, n = v[rows].mean(0), lens[r]
+            bound = torch.finfo(DT[dt]).eps / 2 * want.abs() * 1.01 + 2 * (n / 16 + 64) * 2.0 ** -24 * v[rows].abs().mean(0)
+            assert bool(((got[r] - want).abs() <= bound).all()), (size, sign, r)
