@@ -40,9 +40,8 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 #define CONST_AS __attribute__((address_space(4)))
 
-constexpr float SLACK = 8.0f;                 // log2 units by which a score may exceed the reference before it moves
-constexpr float NOTHING = -__FLT_MAX__;       // reference of a row that has seen no key
-constexpr int DMA_STREAM = 2;                 // non-temporal: every key is read once
+constexpr float NOTHING = -__FLT_MAX__; // reference of a row that has seen no key
+constexpr int DMA_STREAM = 2;           // non-temporal: every key is read once
 // Loads of 1 KB that a wave has on their way.  us with 5 / 6 / 7 / 8: 64 x 4096 rows 94.1 / 91.4 / 92.6 / 96.5, one request of 131071 92.9 /
 // 90.2 / 90.4 / 92.9, windows over 32 requests 87.6 / 85.5 / 86.8 / 90.9, 200 requests of 50 to 1200 105.0 / 103.2 / 103.1 / 103.2.
 constexpr int FLIGHT = 6;
@@ -340,8 +339,8 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             float top = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3]));
             if (KB == 2) top = fmaxf(top, fmaxf(fmaxf(s[n][KB - 1][0], s[n][KB - 1][1]), fmaxf(s[n][KB - 1][2], s[n][KB - 1][3])));
             // A weight is 2^((s - m) scale), the difference first: it is exact or nearly so however large the scores are, where that of
-            // two products with the scale would be off by their roundings.  The reference only has to stay near enough for the exponential's range.
-            if (__any((top - acc.m[n]) * scale > SLACK)) {
+            // two products with the scale would be off by their roundings.  No weight exceeds 1, so that values near the largest do not overflow.
+            if (__any(top > acc.m[n])) {
                 const float to = fmaxf(acc.m[n], column_reduce<true>(top)), alpha = __builtin_amdgcn_exp2f((acc.m[n] - to) * scale);
                 acc.m[n] = to;
                 acc.l[n] *= alpha;

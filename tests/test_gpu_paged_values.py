@@ -107,3 +107,38 @@ def test_equal_keys_share_the_weight_whatever_their_score(B, dt, lens):
             want, n = v[rows].mean(0), lens[r]
             bound = torch.finfo(DT[dt]).eps / 2 * want.abs() * 1.01 + 2 * (n / 16 + 64) * 2.0 ** -24 * v[rows].abs().mean(0)
             assert bool(((got[r] - want).abs() <= bound).all()), (size, sign, r)
+
+
+# ---- values near the largest ---------------------------------------------------------------------------------------------------------
+
+
+@BOTH
+def test_values_near_the_largest_do_not_overflow(B, dt):
+    """One key of each request has a weight 2^7 times that of the others and values of half the largest, and comes when others have
+    been seen already or first of all: weights of at most 1 keep the sums in range.  64 requests of 1024 rows: shares of two units or more."""
+    n, length, d, page = 64, 1024, 64, 64
+    rng = np.random.default_rng(3)
+    table, n_pages = tables(rng, [length] * n, page)
+    kp = torch.zeros(n_pages, page, 1, d, dtype=DT[dt])
+    vp = randn(n_pages, page, 1, d, seed=1, dtype=DT[dt])
+    q = torch.zeros(n, 2, d, dtype=DT[dt])
+    q[..., 0] = 1.0
+    big = torch.full((d,), 1.7e38)
+    big[1::2] *= -1
+    at = [16 * r + 3 for r in range(n)]
+    for r in range(n):
+        kp[table[r, at[r] // page], at[r] % page, 0, 0] = 7 * math.log(2) * math.sqrt(d)
+        vp[table[r, at[r] // page], at[r] % page, 0] = big.to(DT[dt])
+    got = run_decode(B, B.make_shape(2, 1, d, dt, 1e4), q.cuda(), kp.cuda(), vp.cuda(), ints(table), ints([length] * n), 0, 0)
+    want, dev = P.decode_batch(q, kp, vp, table, [range(length)] * n, 2)
+    assert P.excess(got, want, dev, DT[dt])[1] <= 1
+
+
+@BOTH
+def test_a_single_largest_value_is_itself(B, dt):
+    top = torch.finfo(DT[dt]).max
+    kp, vp = make_pool(2, 8, 1, 64, DT[dt], "rows", 1)
+    vp[:] = top
+    q = randn(2, 3, 64, seed=2, dtype=DT[dt])
+    got = run_decode(B, B.make_shape(3, 1, 64, dt, 1e4), q.cuda(), kp, vp, ints([[0], [1]]), ints([1, 1]), 0, 0)
+    assert (got == top).all()
