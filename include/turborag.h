@@ -376,8 +376,8 @@ int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* 
  * (a window of the last `window` rows, and the first n_sink rows that stay visible); scores are scaled by 1/sqrt(head_dim).
  * out [n_req, n_q_heads, head_dim], which may be q itself.  A request that sees no row (length 0, or no page behind any visible row) gets zeros.  Rows
  * that are not visible are not read as values: what they hold (NaN included) does not matter.
- * Scores, softmax and the weighted sum are fp32, whatever the type (bf16: the weights as three bf16 parts of each; a visible
- * value that is infinite makes NaN of its channel).  The bits of a result depend on the batch's lengths, window and sinks, which
+ * Scores, softmax and the weighted sum are fp32, whatever the type.  A visible value that is infinite makes its channel so (NaN
+ * where the channel holds both signs; it may where the weight is less than 2^-96 of the largest).  The bits of a result depend on the batch's lengths, window and sinks, which
  * decide how it is shared out, not on the table's width or the order of pages.
  * workspace: tr_paged_decode_attn_workspace_size() bytes, 256-byte aligned, else TR_ERR_WORKSPACE; it depends on the arguments
  * of the query alone, not on the lengths (0 for sizes that the call refuses); calls that may overlap in time need one each.  q, out and pages 16-byte aligned.

@@ -16,7 +16,8 @@
 // LDS (bf16 V through the transposing read), so that a lane owns one query column: its maximum and denominator are scalars, and
 // its share of S^T is, up to the order of the keys, its B operand of the second product.  A bf16 product takes the weights as
 // three bf16 parts, which together are the fp32 weight: the matrix unit is idle most of the time, and the error against 64 bits is
-// then that of rounding the result, 1.667e-3 of its norm (2.270e-3 with one part), also where values cancel.
+// then that of rounding the result, 1.667e-3 of its norm (2.270e-3 with one part), also where values cancel.  All parts are
+// positive, so that an infinite value stays one.
 //
 // Data movement.  A wave has room for one unit of K and of V (8 KB each at 128 channels) and refills them as soon as their
 // operands are read, straight from memory to LDS, counted waits instead of barriers; the first unit of its next item is on its
@@ -92,6 +93,27 @@ template <bool MAX> __device__ __forceinline__ float column_reduce(float x) // o
     u = __float_as_uint(x);
     const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
     return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+
+// Two weights as three pairs of bf16 that add up to them, by cutting off 8 bits at a time.  Each rest gets 2^-30 of its weight besides, which no
+// sum in fp32 notices, so that no part is zero: infinite values times zero would be NaN.
+struct Split {
+    uint32_t pair[3];
+};
+__device__ __forceinline__ Split split(float x, float y)
+{
+    auto upper = [](float f) { return __uint_as_float(__float_as_uint(f) & 0xffff0000u); };
+    auto both = [](float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); };
+    const float wx = x, wy = y;
+    Split s;
+    s.pair[0] = both(x, y);
+#pragma unroll
+    for (int j = 1; j < 3; ++j) {
+        x = fmaf(wx, 0x1p-30f, x - upper(x));
+        y = fmaf(wy, 0x1p-30f, y - upper(y));
+        s.pair[j] = both(x, y);
+    }
+    return s;
 }
 
 // A unit is 8 KB of K and 8 KB of V for heads of 128 channels (half of that for 64): 32 rows of bf16 or 16 of fp32.
@@ -374,18 +396,15 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
         }
         wait_lds(); // the unit's values are read
         if (!last) st.template issue<true, true>(v, next, ids);
-        bf16x8 parts[NT][3]; // of the weights; fp32: they stay in s.  Not sooner: the next values are on their way meanwhile
+        u32x4 parts[NT][3]; // of the weights, as bf16; fp32: they stay in s.  Not sooner: the next values are on their way meanwhile
         if constexpr (BF16) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i = 0; i < 4 * KB; ++i) {
-                    float rest = s[n][i >> 2][i & 3];
+                for (int i = 0; i < 4 * KB; i += 2) {
+                    const auto w = split(s[n][i >> 2][i & 3], s[n][i >> 2][(i & 3) + 1]);
 #pragma unroll
-                    for (int j = 0; j < 3; ++j) {
-                        parts[n][j][i] = (__bf16)rest;
-                        rest -= (float)parts[n][j][i];
-                    }
+                    for (int j = 0; j < 3; ++j) parts[n][j][i / 2] = w.pair[j];
                 }
         }
         if (cur.seen != ALL) { // what is not seen may be anything, and even a weight of zero would make NaN of NaN
@@ -407,7 +426,8 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             for (int cb = 0; cb < D / 16; ++cb) {
                 if constexpr (BF16) {
 #pragma unroll
-                    for (int j = 0; j < 3; ++j) acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], parts[n][j], acc.o[n][cb], 0, 0, 0);
+                    for (int j = 0; j < 3; ++j)
+                        acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], __builtin_bit_cast(bf16x8, parts[n][j]), acc.o[n][cb], 0, 0, 0);
                 } else { // operand cb holds key cb % 4 of the four; its channel i goes to block 4 (cb / 4) + i
 #pragma unroll
                     for (int i = 0; i < 4; ++i)

@@ -142,3 +142,38 @@ def test_a_single_largest_value_is_itself(B, dt):
     q = randn(2, 3, 64, seed=2, dtype=DT[dt])
     got = run_decode(B, B.make_shape(3, 1, 64, dt, 1e4), q.cuda(), kp, vp, ints([[0], [1]]), ints([1, 1]), 0, 0)
     assert (got == top).all()
+
+
+# ---- infinite values -----------------------------------------------------------------------------------------------------------------
+
+
+@BOTH
+@pytest.mark.parametrize("d,page,lens", [(64, 8, [1, 2, 5, 40]), (128, 16, [700, 33, 1]), (128, 64, [3000, 90]), (64, 32, [900] * 60)], ids=str)
+def test_infinite_values_reach_the_result(B, dt, d, page, lens):
+    """A visible value of +-inf makes its channel +-inf, both signs in one channel make NaN, and the other channels do not notice; weights of any
+    bits, 1 among them.  What is not visible is infinite everywhere."""
+    hq, hk, n = 6, 2, len(lens)
+    table, n_pages = tables(np.random.default_rng(d), lens, page)
+    kp, vp = make_pool(n_pages, page, hk, d, DT[dt], "rows", 3)
+    q = randn(n, hq, d, seed=5, dtype=DT[dt])
+    k, v = kp.cpu(), vp.cpu()
+    seen = torch.zeros(n_pages, page, dtype=torch.bool)
+    for r, length in enumerate(lens):
+        seen[table[r][np.arange(length) // page], np.arange(length) % page] = True
+    finite = v.clone()
+    v[~seen] = float("inf")
+    special = {}
+    rng = np.random.default_rng(9)
+    for r, length in enumerate(lens):
+        for channel, values in ((3, [1]), (d - 2, [-1]), (17, [1, -1]), (40, [-1, -1])):
+            rows = rng.permutation(length)[:len(values)]
+            for j, x in zip(rows, values):
+                v[table[r, j // page], j % page, :, channel] = x * float("inf")
+            special[r, channel] = sum(x * float("inf") for x in values[:len(rows)])
+    got = run_decode(B, B.make_shape(hq, hk, d, dt, 1e4), q.cuda(), kp, v.cuda(), ints(table), ints(lens), 0, 0).cpu().double()
+    want, dev = P.decode_batch(q, k, finite, table, [range(x) for x in lens], hq // hk)
+    for (r, channel), x in special.items():
+        at = got[r, :, channel]
+        assert bool(torch.isnan(at).all()) if math.isnan(x) else bool((at == x).all()), (r, channel, x, at)
+        got[r, :, channel] = want[r, :, channel]
+    assert P.excess(got, want, dev, DT[dt])[1] <= 1
