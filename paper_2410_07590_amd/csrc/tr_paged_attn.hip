@@ -76,8 +76,8 @@ template <int UNIT> __device__ __forceinline__ Walk<UNIT> walk_of(const TrPagedD
 {
     Walk<UNIT> w;
     w.len = min(max(kv_len, 0), a.max_blocks << a.pool.page_shift);
-    w.lo = a.window ? max(w.len - a.window, 0) : 0;
-    w.sink = min(a.n_sink, w.lo);
+    w.lo = a.window ? max(max(kv_len, 0) - a.window, 0) : 0; // may lie behind what the table holds
+    w.sink = min(a.n_sink, min(w.lo, w.len));
     w.su = (w.sink + UNIT - 1) / UNIT;
     w.lu = max(w.lo / UNIT, w.su);
     w.units = max(w.su + max((w.len + UNIT - 1) / UNIT - w.lu, 0), 1);

@@ -97,3 +97,25 @@ def test_windows_over_tables_with_holes(B, dt, page):
 @pytest.mark.parametrize("pool", ["heads", "together", "wide"])
 def test_windows_over_pools_of_any_strides(B, dt, pool):
     check(B, dt, 4, 2, 128, lengths(4, 40, 500, 4000), 16, 1500, 45, 2, pool=pool, seed=4)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [8, 16, 64])
+def test_the_window_of_a_length_beyond_the_table(B, dt, page):
+    """The window's edge is the length's, not the table's: of the rows that the table holds those in front of it are not seen, and where
+    the whole window lies behind them there are only the first tokens, or nothing."""
+    blocks, d = 320 // page, 64
+    rows = blocks * page
+    lens = [rows - 1, rows, rows + 1, rows + 70, rows + 149, rows + 150, rows + 151, 5 * rows, 2 ** 31 - 1]
+    table = np.random.default_rng(page).permutation(len(lens) * blocks).reshape(len(lens), blocks)
+    kp, vp = make_pool(len(lens) * blocks, page, 2, d, DT[dt], "rows", 3)
+    q = randn(len(lens), 4, d, seed=5, dtype=DT[dt])
+    for window, sinks in ((150, 0), (150, 20), (150, 3000), (1, 0), (1, 1), (2 ** 31 - 1, 0), (0, 5)):
+        got = run_decode(B, B.make_shape(4, 2, d, dt, 1e4), q.cuda(), kp, vp, ints(table), ints(lens), window, sinks)
+        keys = [[j for j in range(min(n, rows)) if window == 0 or j >= n - window or j < sinks] for n in lens]
+        want, dev = P.decode_batch(q, kp.cpu(), vp.cpu(), table, keys, 2)
+        for r in range(len(lens)):
+            if keys[r]:
+                assert P.excess(got[r], want[r], dev[r], DT[dt])[1] <= 1, (window, sinks, lens[r])
+            else:
+                assert (got[r] == 0).all(), (window, sinks, lens[r])
