@@ -296,6 +296,8 @@ int tr_linear(const void* x, int32_t M, int32_t K, int32_t n_out, const void* co
  * whose k and v are halves of one allocation, are all described by their strides.  k, v 16-byte aligned, strides multiples of 16
  * bytes, at most 64 MiB for rows and heads and below 4 GiB for pages; page_size a power of two, 8 .. 1024; n_pages * page_size below 2^31; k, v and
  * dtype, n_kv_heads and head_dim have to fit the tr_shape of the call (else TR_ERR_SHAPE).
+ * Where rows are written (tr_paged_append), each of K and of V has bytes of its own, and the strides nest: in order of size, each
+ * is at least what the rows, heads or pages of the smaller ones span (else TR_ERR_INVALID_ARG).
  * A slot is the index page * page_size + row of a row in the pool.  A page id outside [0, n_pages) means "no page": rows of
  * such a page are never read or written, and attention gives their keys no weight. */
 typedef struct tr_pages {

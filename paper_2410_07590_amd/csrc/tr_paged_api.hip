@@ -5,6 +5,7 @@
 #include <math.h>
 #include <string.h>
 #include <algorithm>
+#include <utility>
 
 namespace {
 
@@ -33,7 +34,7 @@ int pool_of(const char* who, const tr_shape* sh, const tr_pages* p, TrPool* out)
     if (p->n_pages < 1 || (int64_t)p->n_pages * p->page_size > INT_LIMIT) return tr_fail(TR_ERR_INVALID_ARG, "%s: n_pages %d", who, p->n_pages);
     if (!p->k || !p->v) return tr_fail(TR_ERR_INVALID_ARG, "%s: k or v of the pages is NULL", who);
     const int64_t e = tr_elem_bytes(sh), widest = (int64_t)64 << 20;
-    // a stride of a single page or head is never applied; the others have to keep rows apart
+    // a stride of a single page or head is never applied; whether the others keep rows apart matters where rows are written
     if (p->row_stride < sh->head_dim || (p->n_kv_heads > 1 && p->head_stride < sh->head_dim) || (p->n_pages > 1 && p->page_stride < sh->head_dim))
         return tr_fail(TR_ERR_INVALID_ARG, "%s: strides of the pages are smaller than a head", who);
     if (p->head_stride < 0 || p->page_stride < 0) // of a single head or page
@@ -69,6 +70,40 @@ Span pool_span(const TrPool& pool, const void* base, const tr_pages* p)
 {
     return {base, (p->n_pages - 1) * (int64_t)pool.page_stride + (p->page_size - 1) * (int64_t)pool.row_stride +
                       (p->n_kv_heads - 1) * (int64_t)pool.head_stride + p->head_dim * (int64_t)(p->dtype == TR_F32 ? 4 : 2)};
+}
+
+// Whether every row of K and V has bytes of its own.  Strides nest: taken by size, each is at least what the ones below it span.
+struct Nest {
+    int64_t stride[3], count[3], span[4]; // span[i]: of the axes below i
+    int axes = 0;
+};
+// Whether two rows of the axes below `axes` meet when one of them is `apart` bytes further on: of an axis only the two differences of
+// indices can make up for that, between which it lies.
+bool rows_meet(const Nest& n, int axes, int64_t apart)
+{
+    if (axes == 0) return apart > -n.span[0] && apart < n.span[0];
+    const int64_t s = n.stride[axes - 1], most = n.count[axes - 1] - 1;
+    const int64_t down = apart >= 0 ? apart / s : -((-apart + s - 1) / s);
+    for (int64_t i : {down, down + 1})
+        if (i >= -most && i <= most && rows_meet(n, axes - 1, apart - i * s)) return true;
+    return false;
+}
+bool rows_apart(const tr_pages* p)
+{
+    const int64_t e = p->dtype == TR_F32 ? 4 : 2;
+    std::pair<int64_t, int64_t> axes[] = {{p->head_stride * e, p->n_kv_heads}, {p->row_stride * e, p->page_size}, {p->page_stride * e, p->n_pages}};
+    std::sort(axes, axes + 3);
+    Nest n;
+    n.span[0] = p->head_dim * e;
+    for (const auto& [stride, count] : axes) {
+        if (count == 1) continue;
+        if (stride < n.span[n.axes]) return false;
+        n.stride[n.axes] = stride;
+        n.count[n.axes] = count;
+        n.span[n.axes + 1] = (count - 1) * stride + n.span[n.axes];
+        ++n.axes;
+    }
+    return !rows_meet(n, n.axes, (int64_t)((intptr_t)p->v - (intptr_t)p->k));
 }
 
 } // namespace
@@ -191,7 +226,7 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     const int64_t e = tr_elem_bytes(shape), q_row = (int64_t)shape->n_q_heads * shape->head_dim, kv_row = (int64_t)shape->n_kv_heads * shape->head_dim;
     if (pages) {
         if (int rc = pool_of(who, shape, pages, &a.pool)) return rc;
-        if (pages->k == pages->v) return tr_fail(TR_ERR_INVALID_ARG, "%s: k and v of the pages are the same rows", who);
+        if (!rows_apart(pages)) return tr_fail(TR_ERR_INVALID_ARG, "%s: rows of the pages use the same bytes", who);
     }
     if (n_tokens == 0 || (!q && !k)) return TR_OK;
     if (a.rotary_dim && !pos) return tr_fail(TR_ERR_INVALID_ARG, "%s: pos is NULL", who);
