@@ -292,10 +292,19 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const TrPagedAppendAr
                 float x[N];
                 V::open(u[i], x);
                 if (normed) {
-                    float ss = 0.0f;
+                    auto mean_square = [&]() {
+                        float ss = 0.0f;
 #pragma unroll
-                    for (int c = 0; c < N; ++c) ss = fmaf(x[c], x[c], ss);
-                    const float r = rsqrtf(lanes_sum<LPH>(ss) * (1.0f / D) + a.eps);
+                        for (int c = 0; c < N; ++c) ss = fmaf(x[c], x[c], ss);
+                        return lanes_sum<LPH>(ss) * (1.0f / D);
+                    };
+                    float under = mean_square() + a.eps;
+                    if (!(under <= __FLT_MAX__)) { // for all lanes of the head: the same of a head 2^70 times smaller
+#pragma unroll
+                        for (int c = 0; c < N; ++c) x[c] *= 0x1p-70f;
+                        under = mean_square() + a.eps * 0x1p-70f * 0x1p-70f;
+                    }
+                    const float r = rsqrtf(under);
 #pragma unroll
                     for (int c = 0; c < N; ++c) x[c] *= r * (hk < 0 ? qw[c] : kw[c]);
                 }
