@@ -306,7 +306,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const TrPagedAppendAr
                     }
                     const float r = rsqrtf(under);
 #pragma unroll
-                    for (int c = 0; c < N; ++c) x[c] *= r * (hk < 0 ? qw[c] : kw[c]);
+                    for (int c = 0; c < N; ++c) x[c] = x[c] * r * (hk < 0 ? qw[c] : kw[c]); // in this order: x r is of size 1
                 }
                 if (HALF) {
                     float y[N];

@@ -52,3 +52,18 @@ def test_infinite_and_nan_heads_stay_by_themselves(B):
     assert (out[1, 2, :77] == 0).all() and (out[1, 2, 78:] == 0).all()
     out[1, 2], out[2, 0] = clean[1, 2], clean[2, 0]
     assert torch.equal(out, clean)
+
+
+@pytest.mark.parametrize("dt,d", [("bf16", 128), ("f32", 64)])
+def test_weights_far_from_one(B, dt, d):
+    """x / rms is of ordinary size, whatever the weight: a weight times 1 / rms need not be a number that fp32 has."""
+    q = randn(6, 2, d, seed=1, dtype=torch.float32)
+    scale = torch.tensor([1e17, 1.0, 1e-3, 1e-10, 0.0, 1e10])
+    q = (q * scale[:, None, None]).to(DT[dt])
+    gs = B.make_shape(2, 1, d, dt, 1e4)
+    for size in (1e-30, 1e30, 2e36):
+        w = (randn(d, seed=3, dtype=torch.float32).clamp(-2, 2) * size).to(DT[dt])
+        out = torch.empty_like(q).cuda()
+        B.tr_paged_append(gs, B.tr_rotary_init(0, 0, 1e4), q.cuda(), None, None, w.cuda(), None, EPS, None, None, out, None)
+        want, mag = R.heads(q, w, EPS, torch.zeros(6), [], 0)
+        R.assert_within(out, want, R.heads_bound(want, mag, DT[dt]), "weight of %g" % size)
