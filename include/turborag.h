@@ -375,7 +375,7 @@ int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* 
  * page block_table[r][j / page_size]; the request has kv_lens[r] rows (device int32; at most max_blocks * page_size are looked
  * at, a negative length is 0), the last of them the new token itself.  It attends row j where
  *   window == 0 or j >= kv_lens[r] - window or j < n_sink
- * (a window of the last `window` rows, and the first n_sink rows that stay visible); scores are scaled by 1/sqrt(head_dim).
+ * (a window of the last `window` rows, of which a table that is too short holds fewer, and the first n_sink rows that stay visible); scores are scaled by 1/sqrt(head_dim).
  * out [n_req, n_q_heads, head_dim], which may be q itself.  A request that sees no row (length 0, or no page behind any visible row) gets zeros.  Rows
  * that are not visible are not read as values: what they hold (NaN included) does not matter.
  * Scores, softmax and the weighted sum are fp32, whatever the type.  A visible value that is infinite makes its channel so (NaN
@@ -383,8 +383,9 @@ int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* 
  * decide how it is shared out, not on the table's width or the order of pages.
  * workspace: tr_paged_decode_attn_workspace_size() bytes, 256-byte aligned, else TR_ERR_WORKSPACE; it depends on the arguments
  * of the query alone, not on the lengths (0 for sizes that the call refuses); calls that may overlap in time need one each.  q, out and pages 16-byte aligned.
- * max_blocks * page_size <= 2^30; n_req <= 65536, n_req * n_q_heads < 2^24 and
- * n_req * n_q_heads * max_blocks * page_size < 2^33 (else TR_ERR_UNSUPPORTED); n_req == 0 is a no-op. */
+ * max_blocks * page_size <= 2^30 (else TR_ERR_INVALID_ARG); n_req <= 65536, n_req * n_q_heads < 2^24, and at most 2^30 units of 32 keys
+ * (fp32: 16), counted for each request, KV head and block of 32 of its query heads over all keys that the table has room for (else
+ * TR_ERR_UNSUPPORTED); n_req == 0 is a no-op. */
 size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size);
 int tr_paged_decode_attn(const tr_shape* shape, const void* q, const tr_pages* pages, const int32_t* block_table /*device*/,
                          int32_t max_blocks, const int32_t* kv_lens /*device*/, int32_t n_req, int32_t window, int32_t n_sink,
