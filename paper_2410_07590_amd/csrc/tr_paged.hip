@@ -1,4 +1,5 @@
-// Kernels of the paged cache: block tables and slots of a batch, append with head norms and rotation, decode attention.
+// Kernels of the paged cache: block tables and slots of a batch, append with head norms and rotation.  Times: us of a call, twelve in
+// a replayed graph over three sets of buffers in turn.
 #include "tr_internal.h"
 
 #include <algorithm>
@@ -14,7 +15,7 @@ typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 // lengths per request, from the caches) and then the slots of its own 1024 tokens, a few pages and, the first, the batch's
 // lengths.  A token finds its request by bisection of the sums in LDS, a thread does it once for four neighbours.
 // Sums are cut at 2^32 - 1 by every addition, which leaves addition associative, and at 2^31 - 1 where they are kept.
-// us: five requests with a new token each 4.5 (an empty launch 3.4), 256 prompts of 193 thousand tokens 6.4 (sums of 64 bits through
+// us: five requests with a new token each 4.4 (an empty launch 3.4), 256 prompts of 193 thousand tokens 6.5 (sums of 64 bits through
 // LDS permutes, two trips to memory for the lengths: 4.9 and 6.9).
 
 __device__ __forceinline__ uint32_t add(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
@@ -221,9 +222,11 @@ template <int LANES> __device__ __forceinline__ float other_half(float x)
 // unit of them: its cosines and sines, weights and the token's row are looked up once (looked up for each unit, 16001 tokens of 32 / 8 heads
 // of 128 took 101 us, 88.6 so: vector instructions were half of the time).  The tokens' angles (a thread per pair, 64 bits) are
 // worked out while the first UNITS loads of every thread are on their way.
-// us: 16384 tokens (padding included) of 32 / 8 heads of 128, norm, all channels turned, 400 MB: 79.9, 5.0 TB/s, what a copy of a GB reaches here;
-// 24000 rows of 4 KV heads, 98 MB: 23.6; 64 tokens of 28 / 4 heads: 4.4, a launch and one chain of position, angle, rotation, store.
-// UNITS: with two, 16001 tokens of 40 heads and values take 81.9 us (three 83.3, four 88.8), 1000 9.2 (9.0) and one 4.40 (4.33).
+// us: 16384 tokens (padding included) of 32 / 8 heads of 128, norm, all channels turned, 400 MB: 78.5, 5.1 TB/s (a copy of as many bytes, one
+// by one on a stream, 74.4; this 72.6); 24000 rows of 4 KV heads, 98 MB: 23.6; 64 tokens of 28 / 4 heads: 4.5, a launch and one chain of
+// position, angle, rotation, store.  The check of the norm's range is 0.1 of that.
+// UNITS two / three / four: 16001 tokens of 40 heads and values 78.6 / 79.0 / 78.2, 1000 9.3 / 9.1 / 9.1, 64 of 28 / 4 heads 4.6 / 4.5 / 4.5, one 4.6 /
+// 4.4 / 4.4, the documents 22.8 / 23.6 / 23.1.
 constexpr int APPEND_UNITS = 3;
 template <int DTYPE, int D, bool HALF, bool STREAM>
 __global__ __launch_bounds__(256) void paged_append_kernel(const TrPagedAppendArgs a)

@@ -266,8 +266,7 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     a.n_kv_heads = k ? shape->n_kv_heads : 0;
     a.eps = (float)eps;
     // A workgroup takes as many tokens as give its threads eight units each, if there are workgroups enough then.  us for 1 token /
-    // this: 24000 rows of 4 KV heads of 128 51.2 / 23.8, 16000 tokens of 16 + 4 heads of 64 50.0 / 23.3, 16001 of 32 + 8 of 128 88.6 / 83.0
-    // (twice as many: 84.9).
+    // this: 24000 rows of 4 KV heads of 128 44.6 / 23.6, 16000 tokens of 16 + 4 heads of 64 47.6 / 23.9, 16001 of 32 + 8 of 128 88.3 / 79.0.
     const int64_t units = (int64_t)(a.n_q_heads + 2 * a.n_kv_heads) * shape->head_dim * e / 16; // of a token
     while ((2 << a.tile_shift) <= TR_PAGED_APPEND_TOKENS && (units << a.tile_shift) * 2 <= 2048 && n_tokens >= 2048ll << a.tile_shift) ++a.tile_shift;
     // Streamed stores make the call itself faster at any size, and what reads its results next slower where the caches still
@@ -363,8 +362,8 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     const int64_t workers = std::min<int64_t>((plan.bound + TR_PAGED_MIN_UNITS - 1) / TR_PAGED_MIN_UNITS, TR_PAGED_WORKERS);
     // The join's workgroups, most of which find nothing to do, are what it costs: it looks at the rows of the result or at those
     // that each wave may have cut, whichever are fewer.  us of the whole call by row / by wave: 200 requests of 50 to 1200 rows, 32 / 8
-    // heads (6400 rows or 4096) 95.9 / 95.1, 512 of 256 (16384 or 4096) 95.0 / 92.2, 4096 of 10 to 60, 16 / 4 heads of 64 (65536 or 4096)
-    // 90.6 / 76.3.
+    // heads (6400 rows or 4096) 102.7 / 101.1, 512 of 256 (16384 or 4096) 96.2 / 93.4, 4096 of 10 to 60, 16 / 4 heads of 64 (65536 or 4096)
+    // 92.7 / 78.7.
     if (plan.bytes) a.cut = (int64_t)n_req * shape->n_q_heads <= workers * plan.ws_rows ? TR_PAGED_JOIN_BY_ROW : TR_PAGED_JOIN_BY_WAVE;
     return tr_launch_paged_decode(a, shape->dtype, shape->head_dim, (int)workers, (hipStream_t)stream);
     });

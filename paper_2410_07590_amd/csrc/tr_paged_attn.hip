@@ -5,29 +5,30 @@
 //
 // Work.  An item is a (request, KV head, block of at most 16 NT query heads).  Its visible keys are walked in units (32 of bf16,
 // 16 of fp32) by single waves that share nothing.  The host does not know the lengths, so the launch is a fixed number of waves,
-// four per compute unit, each of which takes an equal share of all units of the batch, in order of items: it works out the batch's
-// sum from kv_lens and finds its own range in it.  No share is longer than another by more than a unit, whatever the mix of
-// lengths, and at most the first and the last item of a share are cut.  Pieces of cut items go to the workspace and a second,
-// small launch joins them.  (Workgroups of four waves that walked an item's keys together and joined them in LDS took 94.3 us for 64 x
-// 4096 rows where this takes 90.3, 97.5 for one request of 131071 rows (90.2), 104 for 200 requests of 50 to 1200 rows (95.1):
-// their waves wait for one another at the end of each item.)
+// four per compute unit, each of which takes ceil(sum / 1024) of the batch's units, in order of items: it works out the sum from
+// kv_lens and finds its own range in it.  So no share is longer than that, whatever the mix of lengths; the waves at the end have less
+// or nothing (1744 units are 872 shares of two), which matters where shares are few units long.  At most the first and the last item
+// of a share are cut.  Pieces of cut items go to the workspace and a second, small launch joins them.  (Workgroups of four waves that
+// walked an item's keys together and joined them in LDS took 94.3 us for 64 x 4096 rows where single waves took 90.3, 97.5 for one request
+// of 131071 rows (90.2), 104 for 200 requests of 50 to 1200 rows (95.1): their waves wait for one another at the end of each item.)
 //
 // Products.  S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_16x16x32_bf16 (fp32: 16x16x4), keys and values as the A operands from
 // LDS (bf16 V through the transposing read), so that a lane owns one query column: its maximum and denominator are scalars, and
 // its share of S^T is, up to the order of the keys, its B operand of the second product.  A bf16 product takes the weights as
-// three bf16 parts, which together are the fp32 weight: the matrix unit is idle most of the time, and the error against 64 bits is
-// then that of rounding the result, 1.667e-3 of its norm (2.270e-3 with one part), also where values cancel.  All parts are
-// positive, so that an infinite value stays one.
+// three bf16 parts, which together are the fp32 weight: the matrix unit is idle most of the time (64 x 4096 rows: 89.7 us, 89.4 with two
+// parts), and the error against 64 bits is then that of rounding the result, 1.667e-3 of its norm (2.270e-3 with one part), also
+// where values cancel.  All parts are positive, so that an infinite value stays one (90.4 us; with signed parts 90.0).
 //
 // Data movement.  A wave has room for one unit of K and of V (8 KB each at 128 channels) and refills them as soon as their
 // operands are read, straight from memory to LDS, counted waits instead of barriers; the first unit of its next item is on its
 // way before it is done with the last one of this.  A page id is needed for every 8 rows at the most: a wave keeps the ids of
 // its next units in one register, a lane each, and takes them out as scalars.
 //
-// Heads of 128 channels, bf16, fresh pools every pass, us of the whole call (replayed graph): 64 requests of 4096 rows, 28 / 4 heads,
-// pages of 64: 90 (538 MB: 6.0 TB/s; the first kernel alone 80 to 82, 6.6 TB/s); one of 131071, 32 / 8 heads, pages of 16: 90;
-// 32 of up to 32000 rows through a window of 4000 and 4 first tokens: 84 (489 MB); five of 300 to 3000 rows: 13.3; one of 700: 8.3,
-// which is two launches and, in the first, four dependent trips to memory (lengths, page ids, keys, results).
+// Times here and below: us of the whole call, twelve in a replayed graph over three pools in turn (called one by one on a stream
+// the long ones take 5 % less).  Heads of 128 channels, bf16: 64 requests of 4096 rows, 28 / 4 heads, pages of 64: 90.4 (538 MB: 5.9 TB/s; the
+// first kernel alone 83, 6.5 TB/s); one of 131071, 32 / 8 heads, pages of 16: 91.1; 32 of up to 32000 rows through a window of 4000 and
+// 4 first tokens: 85.9 (489 MB); five of 300 to 3000 rows: 13.6; one of 700: 8.4, which is two launches and, in the first, four
+// dependent trips to memory (lengths, page ids, keys, results).
 #include "tr_device.h"
 #include "tr_internal.h"
 
@@ -43,8 +44,8 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float NOTHING = -__FLT_MAX__; // reference of a row that has seen no key
 constexpr int DMA_STREAM = 2;           // non-temporal: every key is read once
-// Loads of 1 KB that a wave has on their way.  us with 5 / 6 / 7 / 8: 64 x 4096 rows 94.1 / 91.4 / 92.6 / 96.5, one request of 131071 92.9 /
-// 90.2 / 90.4 / 92.9, windows over 32 requests 87.6 / 85.5 / 86.8 / 90.9, 200 requests of 50 to 1200 105.0 / 103.2 / 103.1 / 103.2.
+// Loads of 1 KB that a wave has on their way.  us with 5 / 6 / 7 / 8: 64 x 4096 rows 95.5 / 92.7 / 91.8 / 96.2, one request of 131071 95.4 /
+// 92.1 / 91.3 / 94.3, windows over 32 requests 89.1 / 86.0 / 85.6 / 90.4, 200 requests of 50 to 1200 99.1 / 97.0 / 96.4 / 98.2.
 constexpr int FLIGHT = 6;
 
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
@@ -684,9 +685,10 @@ template <int DTYPE, int D, int NT> int launch_decode(const TrPagedDecodeArgs& a
     TR_HIP(hipGetLastError());
     if (!a.cut) return TR_OK;
     // Items have 1 + (waves / items) pieces on average.  Where there are few items, and many pieces of each, more threads read
-    // them sooner; else most of a workgroup has nothing to read, and starting it is what the join costs.  us of the whole call with 256 / 64
-    // threads: one request of 5000 rows (8 items) 12.6 / 14.3, five of 300 to 3000 (40) 13.3 / 14.1, 16 of 2000 (64) 19.2 / 19.4, 24 of up to 9000
-    // (96) 23.4 / 23.0, 64 of 4096 (256) 90.7 / 90.0, 256 of 20 to 400 (1024) 25.6 / 22.9, 200 of 50 to 1200 (1600) 99.3 / 95.0.
+    // them sooner; else most of a workgroup has nothing to read, and starting it is what the join costs.  The rule counts KV heads of all
+    // requests, which are the items unless a KV head has more than 32 query heads; it was measured where it has not.  us with 256 / 64
+    // threads: one request of 5000 rows (8 items) 12.8 / 14.5, five of 300 to 3000 (40) 13.6 / 14.3, 16 of 2000 (64) 19.9 / 20.2, 24 of up to 9000
+    // (96) 24.5 / 24.1, 64 of 4096 (256) 92.7 / 92.6, 256 of 20 to 400 (1024) 26.8 / 23.7, 200 of 50 to 1200 (1600) 103.1 / 98.1.
     const dim3 rows(a.cut == TR_PAGED_JOIN_BY_WAVE ? grid * a.ws_rows : a.n_req * a.n_q_heads);
     if ((int64_t)a.n_req * a.n_kv_heads < 96) paged_join_kernel<DTYPE, D, 256><<<rows, dim3(256), 0, s>>>(a, 16 * NT);
     else paged_join_kernel<DTYPE, D, 64><<<rows, dim3(64), 0, s>>>(a, 16 * NT);
