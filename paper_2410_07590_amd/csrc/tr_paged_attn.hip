@@ -25,9 +25,9 @@
 // its next units in one register, a lane each, and takes them out as scalars.
 //
 // Times here and below: us of the whole call, twelve in a replayed graph over three pools in turn (called one by one on a stream
-// the long ones take 5 % less).  Heads of 128 channels, bf16: 64 requests of 4096 rows, 28 / 4 heads, pages of 64: 90.4 (538 MB: 5.9 TB/s; the
-// first kernel alone 83, 6.5 TB/s); one of 131071, 32 / 8 heads, pages of 16: 91.1; 32 of up to 32000 rows through a window of 4000 and
-// 4 first tokens: 85.9 (489 MB); five of 300 to 3000 rows: 13.6; one of 700: 8.4, which is two launches and, in the first, four
+// the long ones take 5 % less).  Heads of 128 channels, bf16: 64 requests of 4096 rows, 28 / 4 heads, pages of 64: 91.4 (538 MB: 5.9 TB/s; the
+// first kernel alone 83, 6.5 TB/s); one of 131071, 32 / 8 heads, pages of 16: 90.9; 32 of up to 32000 rows through a window of 4000 and
+// 4 first tokens: 85.4 (489 MB); five of 300 to 3000 rows: 13.6; one of 700: 8.5, which is two launches and, in the first, four
 // dependent trips to memory (lengths, page ids, keys, results).
 #include "tr_device.h"
 #include "tr_internal.h"
@@ -44,9 +44,9 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float NOTHING = -__FLT_MAX__; // reference of a row that has seen no key
 constexpr int DMA_STREAM = 2;           // non-temporal: every key is read once
-// Loads of 1 KB that a wave has on their way.  us with 5 / 6 / 7 / 8: 64 x 4096 rows 95.5 / 92.7 / 91.8 / 96.2, one request of 131071 95.4 /
-// 92.1 / 91.3 / 94.3, windows over 32 requests 89.1 / 86.0 / 85.6 / 90.4, 200 requests of 50 to 1200 99.1 / 97.0 / 96.4 / 98.2.
-constexpr int FLIGHT = 6;
+// Loads of 1 KB that a wave has on their way.  us with 5 / 6 / 7 / 8: 64 x 4096 rows 95.5 / 92.6 / 91.7 / 96.2, one request of 131071 95.4 /
+// 92.2 / 91.3 / 94.3, windows over 32 requests 89.1 / 86.0 / 85.5 / 90.4, 200 requests of 50 to 1200 99.1 / 96.9 / 96.2 / 98.2.
+constexpr int FLIGHT = 7;
 
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
