@@ -375,12 +375,14 @@ int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* 
  * page block_table[r][j / page_size]; the request has kv_lens[r] rows (device int32; at most max_blocks * page_size are looked
  * at, a negative length is 0), the last of them the new token itself.  It attends row j where
  *   window == 0 or j >= kv_lens[r] - window or j < n_sink
- * (a window of the last `window` rows, of which a table that is too short holds fewer, and the first n_sink rows that stay visible); scores are scaled by 1/sqrt(head_dim).
+ * (a window of the last `window` rows, of which a table that is too short holds fewer, and the first n_sink rows that stay
+ * visible); scores are scaled by 1/sqrt(head_dim).
  * out [n_req, n_q_heads, head_dim], which may be q itself.  A request that sees no row (length 0, or no page behind any visible row) gets zeros.  Rows
  * that are not visible are not read as values: what they hold (NaN included) does not matter.
- * Scores, softmax and the weighted sum are fp32, whatever the type.  A visible value that is infinite makes its channel so (NaN
- * where the channel holds both signs; it may where the weight is less than 2^-96 of the largest).  The bits of a result depend on the batch's lengths, window and sinks, which
- * decide how it is shared out, not on the table's width or the order of pages.
+ * Scores, softmax and the weighted sum are fp32, whatever the type; scores may be of any size that fp32 has.  A visible value that
+ * is infinite makes its channel so (NaN where the channel holds both signs; it may where the weight is less than 2^-96 of the
+ * largest).  The bits of a result depend on the batch's lengths, window and sinks, which decide how it is shared out, not on the
+ * table's width or the order of pages.
  * workspace: tr_paged_decode_attn_workspace_size() bytes, 256-byte aligned, else TR_ERR_WORKSPACE; it depends on the arguments
  * of the query alone, not on the lengths (0 for sizes that the call refuses); calls that may overlap in time need one each.  q, out and pages 16-byte aligned.
  * max_blocks * page_size <= 2^30 (else TR_ERR_INVALID_ARG); n_req <= 65536, n_req * n_q_heads < 2^24, and at most 2^30 units of 32 keys
