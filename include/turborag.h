@@ -13,6 +13,7 @@
  *   Eq. 1            projections around the attention for the query tokens -> tr_linear
  *   Sec. 3.4 step 7  the same cache in pages, its lengths and block tables on the GPU -> tr_page_map, tr_rotary_init,
  *                                                       tr_paged_append, tr_paged_decode_attn
+ *                  ... and those pages in 8 bits        -> tr_paged_append_q8, tr_paged_read_q8, tr_paged_decode_attn_q8
  *
  * Conventions (all entry points):
  *   - Tensors are token-major, contiguous: [rows, heads, head_dim], element type `tr_shape.dtype`
@@ -392,6 +393,68 @@ size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int32_t n_req,
 int tr_paged_decode_attn(const tr_shape* shape, const void* q, const tr_pages* pages, const int32_t* block_table /*device*/,
                          int32_t max_blocks, const int32_t* kv_lens /*device*/, int32_t n_req, int32_t window, int32_t n_sink,
                          void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- the pages in 8 bits ----------------------------------------------------------------------------------------------------
+ * What bounds a decode step is reading the cache, and what bounds a batch is room for it; a pool in 8 bits halves both.  It takes
+ * the place of tr_pages beside the same block tables, slots and positions (tr_page_map, tr_rotary_init): per step tr_page_map,
+ * tr_paged_append_q8, tr_paged_decode_attn_q8; tr_paged_read_q8 gives rows back for the calls that want a contiguous cache
+ * (tr_prefill_attn of a question behind documents that the pages hold).
+ *
+ * tr_pages_q8: row i of page p of KV head h begins at byte p * page_stride + i * row_stride + h * head_stride of k (and of v) and
+ * is head_dim codes: e4m3 (1 sign, 4 exponent bits of bias 7, 3 mantissa bits; largest 448; 0x7f and 0xff NaN; no infinity).  Each block
+ * of 16 rows of a page has for each head a scale for its keys and one for its values: k_scale, v_scale
+ * [n_pages, n_kv_heads, page_size / 16], bytes s of the meaning 2^(s - 127).  A row is worth code * 2^(s - 127).  The calls write 10 <= s <= 247, with
+ * which every value but NaN is a normal number or zero of fp32 and of bf16; other bytes from 1 to 254 are read for what they mean, as far
+ * as the values are normal numbers or zero, 0 and 255 make the values of the block's rows undefined.
+ * Strides, alignment and limits are those of tr_pages for elements of one byte, except that page_size is 16 .. 1024; the shape's dtype
+ * is that of queries, new keys and values and results.  The scales have no alignment. */
+typedef struct tr_pages_q8 {
+    void* k;
+    void* v;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    int64_t page_stride; /* bytes */
+    int64_t row_stride;
+    int64_t head_stride;
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int64_t reserved; /* must be 0 */
+} tr_pages_q8;
+
+/* tr_paged_append into such a pool: the same arguments, and the same queries.  Keys (normalised and turned in fp32 or wider) and
+ * values x are rounded once, to nearest even:  code = e4m3(x / 2^e),  e = the smallest with |x| <= 448 * 2^e for what the block
+ * holds, -117 <= e <= 120.  NaN and infinite x become NaN and have no part in e (nor have they one in what their block's other channels
+ * hold); |x| beyond 1.875 * 2^127 counts as that.
+ * The rows of a block that a call writes follow one another: its tokens with slots of one block stand side by side, in any order of rows
+ * (as tr_page_map gives them).  Where row 0 is among them, the block starts anew: e is that of the written rows, and the other rows
+ * are not held (they keep their codes).  Where it is not, e is at least what it was; if the new rows need more, the block's other
+ * rows are rounded again to the new scale - a factor that is a power of two, which changes only values below 2^-6 of the scale
+ * before or after it.  So a block filled token by token ends at the scale of one filled at once, and at its codes but for such values.
+ * Slots of one block that repeat or do not stand side by side leave that block's rows and scales undefined, and no others.  The
+ * scales are apart from everything else of the call (TR_ERR_INVALID_ARG). */
+int tr_paged_append_q8(const tr_shape* shape, const tr_rotary* rotary, const void* q, int64_t q_stride, const void* k,
+                       int64_t k_stride, const void* v, int64_t v_stride, const void* q_norm, const void* k_norm, double eps,
+                       const int32_t* pos, const int32_t* slots, int32_t n_tokens, void* q_out, const tr_pages_q8* pages, void* stream);
+
+/* Rows of a batch of requests out of the pages, as they are worth, in the shape's type (exact).  Row j < kv_lens[r] of request r goes to
+ * row row_start[r] + j of out_k and out_v [n_rows, n_kv_heads, head_dim], as far as that is below row_start[r + 1] and n_rows and the
+ * table has an entry for it; rows of a page that is none become zeros, all rows that no request claims stay as they are.  block_table
+ * [n_req, max_blocks], kv_lens [n_req] (negative: 0), row_start [n_req + 1]: device int32, row_start ascending (where it is not, which rows
+ * are written is undefined, not that they are rows of the outputs).  Outputs 16-byte aligned, apart from each other and all inputs.  n_rows == 0 and
+ * n_req == 0 are no-ops.  Limits of n_req and max_blocks as for tr_paged_decode_attn_q8. */
+int tr_paged_read_q8(const tr_shape* shape, const tr_pages_q8* pages, const int32_t* block_table /*device*/, int32_t max_blocks,
+                     const int32_t* kv_lens /*device*/, const int32_t* row_start /*device*/, int32_t n_req, void* out_k, void* out_v,
+                     int32_t n_rows, void* stream);
+
+/* tr_paged_decode_attn over such a pool: the same arguments, masks, guarantees and limits (units of 32 keys for both types).  Keys
+ * and values enter the products as they are worth, exactly; queries, weights, scores and sums are fp32 or what the type holds.  A visible
+ * NaN makes its head's (key) or its channel's (value) results NaN. */
+size_t tr_paged_decode_attn_q8_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size);
+int tr_paged_decode_attn_q8(const tr_shape* shape, const void* q, const tr_pages_q8* pages, const int32_t* block_table /*device*/,
+                            int32_t max_blocks, const int32_t* kv_lens /*device*/, int32_t n_req, int32_t window, int32_t n_sink,
+                            void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- launch-policy override for tests and sweeps -------------------------------------------------------------------------
  * Sets a process-wide override of one value of the launch policy; value 0 restores the default.  Names: "wg_rows"

@@ -32,6 +32,7 @@ EXPORTS = [
     "tr_sequence_plan", "tr_sequence_prefill_attn_workspace_size", "tr_sequence_prefill_attn",
     "tr_linear_workspace_size", "tr_linear", "tr_set_tuning",
     "tr_page_map", "tr_rotary_init", "tr_paged_append", "tr_paged_decode_attn_workspace_size", "tr_paged_decode_attn",
+    "tr_paged_append_q8", "tr_paged_read_q8", "tr_paged_decode_attn_q8_workspace_size", "tr_paged_decode_attn_q8",
     "tr_probe_mfma_loop_sink_bytes", "tr_probe_mfma_loop",
 ]
 
@@ -46,6 +47,12 @@ class tr_pages(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("row_stride", C.c_int64),
                 ("head_stride", C.c_int64), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class tr_pages_q8(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("page_stride", C.c_int64),
+                ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("reserved", C.c_int64)]
 
 
 class tr_rotary(C.Structure):
@@ -78,7 +85,8 @@ def lib():
         for name in ("tr_prefill_attn_workspace_size", "tr_prefill_attn_batched_workspace_size",
                      "tr_prefill_attn_gather_workspace_size", "tr_decode_attn_workspace_size",
                      "tr_chunk_prefill_attn_workspace_size", "tr_sequence_prefill_attn_workspace_size",
-                     "tr_linear_workspace_size", "tr_paged_decode_attn_workspace_size", "tr_prefill_attn_static_scratch_bytes",
+                     "tr_linear_workspace_size", "tr_paged_decode_attn_workspace_size", "tr_paged_decode_attn_q8_workspace_size",
+                     "tr_prefill_attn_static_scratch_bytes",
                      "tr_probe_mfma_loop_sink_bytes"):
             getattr(L, name).restype = C.c_size_t
         _tr_host.bind({name: C.cast(getattr(L, name), C.c_void_p).value for name in EXPORTS}, TurboRagError,
@@ -302,14 +310,19 @@ def tr_linear(x, w, y, workspace=None, stream=None):
     _native().linear(x, ws_, ys_, workspace, stream)
 
 
-def make_pages(k_pages, v_pages):
-    """The pool behind two device tensors [n_pages, page_size, n_kv_heads, head_dim] of equal strides, last one 1: a pool that
-    keeps the rows of a head together ([page, head, row, channel]) is passed as its transpose(1, 2).  Keeps the tensors alive."""
+def _check_pages(k_pages, v_pages):
     assert k_pages.is_cuda and v_pages.is_cuda and k_pages.device == v_pages.device, "pages are device tensors"
     assert k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.stride() == v_pages.stride() and k_pages.dtype == v_pages.dtype
     assert k_pages.stride(3) == 1, "the channels of a row must be contiguous"
     n, size, heads, d = k_pages.shape
     assert max(n, size, heads) < 2 ** 31
+
+
+def make_pages(k_pages, v_pages):
+    """The pool behind two device tensors [n_pages, page_size, n_kv_heads, head_dim] of equal strides, last one 1: a pool that
+    keeps the rows of a head together ([page, head, row, channel]) is passed as its transpose(1, 2).  Keeps the tensors alive."""
+    _check_pages(k_pages, v_pages)
+    n, size, heads, d = k_pages.shape
     p = tr_pages(k_pages.data_ptr(), v_pages.data_ptr(), *k_pages.stride()[:3], n, size, heads, d,
                  {torch.float32: TR_F32, torch.bfloat16: TR_BF16}[k_pages.dtype], 0)
     if n == 1:
@@ -317,6 +330,25 @@ def make_pages(k_pages, v_pages):
     if heads == 1:
         p.head_stride = 0
     p.tensors = (k_pages, v_pages)
+    return p
+
+
+def make_pages_q8(k_pages, v_pages, k_scale, v_scale):
+    """The pool of 8 bits behind two device tensors of codes (torch.float8_e4m3fn or uint8) laid out as for make_pages, and two of
+    scales [n_pages, n_kv_heads, page_size / 16] (torch.float8_e8m0fnu or uint8), contiguous.  Keeps the tensors alive."""
+    _check_pages(k_pages, v_pages)
+    assert k_pages.dtype in (torch.float8_e4m3fn, torch.uint8), "codes are torch.float8_e4m3fn or uint8"
+    n, size, heads, d = k_pages.shape
+    for t in (k_scale, v_scale):
+        assert t.dtype in (torch.float8_e8m0fnu, torch.uint8), "scales are torch.float8_e8m0fnu or uint8"
+        assert t.is_cuda and t.device == k_pages.device and t.is_contiguous(), "scales are contiguous device tensors"
+        assert tuple(t.shape) == (n, heads, size // 16), "scales are [n_pages, n_kv_heads, page_size / 16]"
+    p = tr_pages_q8(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *k_pages.stride()[:3], n, size, heads, d, 0)
+    if n == 1:
+        p.page_stride = 0   # never applied
+    if heads == 1:
+        p.head_stride = 0
+    p.tensors = (k_pages, v_pages, k_scale, v_scale)
     return p
 
 
@@ -345,6 +377,25 @@ def tr_paged_decode_attn_workspace_size(shape, n_req, max_blocks, page_size):
 
 def tr_paged_decode_attn(shape, q, pages, block_table, kv_lens, window, n_sink, out, workspace=None, stream=None):
     _native().paged_decode_attn(shape, q, pages, block_table, kv_lens, window, n_sink, out, workspace, stream)
+
+
+def tr_paged_append_q8(shape, rotary, q, k, v, q_norm, k_norm, eps, pos, slots, q_out, pages, stream=None):
+    """tr_paged_append into the pool of make_pages_q8()."""
+    _native().paged_append_q8(shape, rotary, q, k, v, q_norm, k_norm, eps, pos, slots, q_out, pages, stream)
+
+
+def tr_paged_read_q8(shape, pages, block_table, kv_lens, row_start, out_k, out_v, stream=None):
+    """Rows of requests as what their codes stand for: request r's to rows row_start[r] .. of out_k and out_v [rows, n_kv_heads, head_dim]."""
+    _native().paged_read_q8(shape, pages, block_table, kv_lens, row_start, out_k, out_v, stream)
+
+
+def tr_paged_decode_attn_q8_workspace_size(shape, n_req, max_blocks, page_size):
+    return int(lib().tr_paged_decode_attn_q8_workspace_size(C.byref(shape), C.c_int32(n_req), C.c_int32(max_blocks), C.c_int32(page_size)))
+
+
+def tr_paged_decode_attn_q8(shape, q, pages, block_table, kv_lens, window, n_sink, out, workspace=None, stream=None):
+    """tr_paged_decode_attn over the pool of make_pages_q8()."""
+    _native().paged_decode_attn_q8(shape, q, pages, block_table, kv_lens, window, n_sink, out, workspace, stream)
 
 
 def workspace(nbytes, device="cuda"):

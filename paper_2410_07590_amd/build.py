@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libturborag_hip.so")
 HOST = os.path.join(HERE, "_tr_host.so")
 SOURCES = ["tr_api.hip", "tr_copy.hip", "tr_attn.hip", "tr_attn_f32.hip", "tr_linear.hip", "tr_probe.hip",
-           "tr_paged_api.hip", "tr_paged.hip", "tr_paged_attn.hip"]
+           "tr_paged_api.hip", "tr_paged.hip", "tr_paged_attn.hip", "tr_paged_q8.hip", "tr_paged_q8_attn.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed fp32 VALU forms are kept off for every HIP translation unit

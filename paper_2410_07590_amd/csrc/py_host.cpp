@@ -23,7 +23,8 @@ namespace {
     X(tr_last_error) X(tr_plan) X(tr_kv_assemble) X(tr_kv_assemble_raw) X(tr_kv_assemble_batched) X(tr_kv_append)            \
     X(tr_kv_assemble_append) X(tr_kv_append_batched) X(tr_prefill_attn) X(tr_prefill_attn_static) X(tr_prefill_attn_batched) \
     X(tr_prefill_attn_gather) X(tr_decode_attn) X(tr_chunk_prefill_attn) X(tr_sequence_prefill_attn) X(tr_linear)                \
-    X(tr_page_map) X(tr_paged_append) X(tr_paged_decode_attn)
+    X(tr_page_map) X(tr_paged_append) X(tr_paged_decode_attn) \
+    X(tr_paged_append_q8) X(tr_paged_read_q8) X(tr_paged_decode_attn_q8)
 struct Api {
 #define X(name) decltype(&::name) name;
     TR_CALLS(X)
@@ -467,9 +468,9 @@ void has_type(const at::Tensor& t, const tr_shape& s)
 {
     if (t.scalar_type() != (s.dtype == TR_F32 ? at::kFloat : at::kBFloat16)) fail(PyExc_AssertionError, "a tensor has another type than the shape");
 }
-tr_pages pool(PyObject* o, Place& at) // of make_pages(), which keeps the tensors beside it, or filled in by hand
+template <class POOL> POOL pool(PyObject* o, Place& at) // of make_pages() or make_pages_q8(), which keep the tensors beside it, or filled in by hand
 {
-    tr_pages p;
+    POOL p;
     read_buffer(o, &p, sizeof p);
     PyObject* t = PyObject_GetAttr(o, str_tensors);
     if (!t) {
@@ -477,7 +478,8 @@ tr_pages pool(PyObject* o, Place& at) // of make_pages(), which keeps the tensor
         return p;
     }
     try {
-        if (PyTuple_Check(t) && PyTuple_GET_SIZE(t) == 2) at.on(PyTuple_GET_ITEM(t, 0), false), at.on(PyTuple_GET_ITEM(t, 1), false);
+        if (PyTuple_Check(t))
+            for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(t); ++i) at.on(PyTuple_GET_ITEM(t, i), false);
     } catch (const Failed&) {
         Py_DECREF(t);
         throw;
@@ -502,7 +504,7 @@ PyObject* page_map(Args a) // cached_lens, new_lens, first_pos, page_size, free_
     return run([&] { return api.tr_page_map(cached, fresh, first, req, page, free_pages, n_free_, table, blocks, lens, cu, slots, pos, n_slots_, counts, s); });
 }
 
-PyObject* paged_append(Args a) // shape, rotary, q, k, v, q_norm, k_norm, eps, pos, slots, q_out, pages, stream
+template <class POOL, class Call> PyObject* paged_append_to(Args a, Call call) // shape, rotary, q, k, v, q_norm, k_norm, eps, pos, slots, q_out, pages, stream
 {
     const tr_shape sh = shape(a[0]);
     tr_rotary rot;
@@ -538,24 +540,26 @@ PyObject* paged_append(Args a) // shape, rotary, q, k, v, q_norm, k_norm, eps, p
     if (eps == -1.0 && PyErr_Occurred()) throw Failed();
     const int32_t* pos = a[8] == Py_None ? nullptr : at.ints_of(a[8], n);
     const int32_t* slots = a[9] == Py_None ? nullptr : at.ints_of(a[9], n);
-    tr_pages pg;
-    if (a[11] != Py_None) pg = pool(a[11], at);
+    POOL pg;
+    if (a[11] != Py_None) pg = pool<POOL>(a[11], at);
     const int32_t tokens = small(n);
     void* s = at.stream_of(a[12]);
     return run([&] {
-        return api.tr_paged_append(&sh, a[1] == Py_None ? nullptr : &rot, q.p, q.stride, k.p, k.stride, v.p, v.stride, qw, kw, eps, pos, slots, tokens,
-                                   out.p, a[11] == Py_None ? nullptr : &pg, s);
+        return call(&sh, a[1] == Py_None ? nullptr : &rot, q.p, q.stride, k.p, k.stride, v.p, v.stride, qw, kw, eps, pos, slots, tokens, out.p,
+                    a[11] == Py_None ? nullptr : &pg, s);
     });
 }
+PyObject* paged_append(Args a) { return paged_append_to<tr_pages>(a, api.tr_paged_append); }
+PyObject* paged_append_q8(Args a) { return paged_append_to<tr_pages_q8>(a, api.tr_paged_append_q8); }
 
-PyObject* paged_decode(Args a) // shape, q, pages, block_table, kv_lens, window, n_sink, out, workspace, stream
+template <class POOL, class Call> PyObject* paged_decode_over(Args a, Call call) // shape, q, pages, block_table, kv_lens, window, n_sink, out, workspace, stream
 {
     const tr_shape sh = shape(a[0]);
     Place at;
     const at::Tensor &q = at.on(a[1]), &out = at.on(a[7]);
     has_type(q, sh);
     has_type(out, sh);
-    const tr_pages pg = pool(a[2], at);
+    const POOL pg = pool<POOL>(a[2], at);
     int32_t* table = at.ints(a[3]);
     const at::Tensor& t = tensor(a[3]);
     int64_t n;
@@ -569,7 +573,31 @@ PyObject* paged_decode(Args a) // shape, q, pages, block_table, kv_lens, window,
     if (a[8] != Py_None) at.on(a[8]);
     const Work w(a[8]);
     void* s = at.stream_of(a[9]);
-    return run([&] { return api.tr_paged_decode_attn(&sh, qp, &pg, table, blocks, lens, req, window, sinks, op, w.p, w.bytes, s); });
+    return run([&] { return call(&sh, qp, &pg, table, blocks, lens, req, window, sinks, op, w.p, w.bytes, s); });
+}
+PyObject* paged_decode(Args a) { return paged_decode_over<tr_pages>(a, api.tr_paged_decode_attn); }
+PyObject* paged_decode_q8(Args a) { return paged_decode_over<tr_pages_q8>(a, api.tr_paged_decode_attn_q8); }
+
+PyObject* paged_read_q8(Args a) // shape, pages, block_table, kv_lens, row_start, out_k, out_v, stream
+{
+    const tr_shape sh = shape(a[0]);
+    Place at;
+    const at::Tensor &k = at.on(a[5]), &v = at.on(a[6]);
+    has_type(k, sh);
+    has_type(v, sh);
+    const tr_pages_q8 pg = pool<tr_pages_q8>(a[1], at);
+    int32_t* table = at.ints(a[2]);
+    const at::Tensor& t = tensor(a[2]);
+    int64_t n;
+    const int32_t* lens = at.ints(a[3], &n);
+    if (t.dim() != 2 || t.size(0) != n) fail(PyExc_AssertionError, "block_table is [requests, blocks]");
+    const int32_t* start = at.ints_of(a[4], n + 1);
+    for (const at::Tensor* o : {&k, &v})
+        if (o->dim() != 3 || o->size(0) != k.size(0) || o->size(1) != sh.n_kv_heads || o->size(2) != sh.head_dim)
+            fail(PyExc_AssertionError, "outputs are [rows, heads, head_dim]");
+    const int32_t req = small(n), blocks = small(t.size(1)), rows = small(k.size(0));
+    void *kp = k.data_ptr(), *vp = v.data_ptr(), *s = at.stream_of(a[7]);
+    return run([&] { return api.tr_paged_read_q8(&sh, &pg, table, blocks, lens, start, req, kp, vp, rows, s); });
 }
 
 // addresses: dict name -> address of the library's entry point; error: the exception class for a failed call
@@ -618,6 +646,9 @@ PyMethodDef methods[] = {
     ENTRY("page_map", 12, page_map),
     ENTRY("paged_append", 13, paged_append),
     ENTRY("paged_decode_attn", 10, paged_decode),
+    ENTRY("paged_append_q8", 13, paged_append_q8),
+    ENTRY("paged_read_q8", 8, paged_read_q8),
+    ENTRY("paged_decode_attn_q8", 10, paged_decode_q8),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tr_host", "argument marshalling for binding.py", -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -407,7 +407,10 @@ struct TrPool {
     char* v;
     uint32_t page_stride, row_stride, head_stride;
     int32_t n_pages, page_shift;
+    uint8_t *k_scale, *v_scale; // of a pool in 8 bits
 };
+#define TR_Q8_ROWS 16 // that share a scale
+#define TR_Q8_UNIT 32 // keys that a wave of the decode over 8 bits takes at a time
 #define TR_PAGED_APPEND_TOKENS 8 // at most, of a workgroup
 struct TrPagedAppendArgs {
     const char* q;
@@ -449,6 +452,18 @@ struct TrPagedDecodeArgs {
     float* ws_ml;      // [2 workers][ws_rows][2] reference maximum (an unscaled score) and denominator
     int32_t* ws_items; // by row: [items][2] wave that begins an item, number of its pieces; by wave: [waves][2] item it begins and cuts, number of pieces
 };
+struct TrPagedReadArgs {
+    TrPool pool;
+    const int32_t* table;
+    const int32_t* kv_lens;
+    const int32_t* row_start;
+    char* out_k;
+    char* out_v;
+    int32_t n_req, max_blocks, n_rows, n_kv_heads;
+};
 int tr_launch_page_map(const TrPageMapArgs& a, hipStream_t s);
 int tr_launch_paged_append(const TrPagedAppendArgs& a, int dtype, int head_dim, int layout, hipStream_t s);
 int tr_launch_paged_decode(const TrPagedDecodeArgs& a, int dtype, int head_dim, int grid, hipStream_t s);
+int tr_launch_paged_append_q8(const TrPagedAppendArgs& a, int dtype, int head_dim, int layout, hipStream_t s);
+int tr_launch_paged_read_q8(const TrPagedReadArgs& a, int dtype, int head_dim, hipStream_t s);
+int tr_launch_paged_decode_q8(const TrPagedDecodeArgs& a, int dtype, int head_dim, int grid, hipStream_t s);

@@ -1,13 +1,12 @@
 // Kernels of the paged cache: block tables and slots of a batch, append with head norms and rotation.  Times: us of a call, twelve in
 // a replayed graph over three sets of buffers in turn.
 #include "tr_internal.h"
+#include "tr_paged_heads.h"
 
 #include <algorithm>
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // ---- block tables, slots, position ids ------------------------------------------------------------------------------------
@@ -158,65 +157,6 @@ __global__ __launch_bounds__(256) void page_map_kernel(const TrPageMapArgs a)
 
 // ---- heads: norm, rotation, rows of the pool --------------------------------------------------------------------------------
 
-// A 16-byte unit of a head in fp32: 8 bf16 or 4 fp32 channels.
-template <int DTYPE> struct Vec;
-template <> struct Vec<TR_BF16> {
-    static constexpr int N = 8;
-    static __device__ __forceinline__ void open(u32x4 u, float (&x)[8])
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
-    static __device__ __forceinline__ u32x4 close(const float (&x)[8])
-    {
-        typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-        bf16x8 y;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = (__bf16)x[i];
-        return __builtin_bit_cast(u32x4, y);
-    }
-};
-template <> struct Vec<TR_F32> {
-    static constexpr int N = 4;
-    static __device__ __forceinline__ void open(u32x4 u, float (&x)[4])
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(u[i]);
-    }
-    static __device__ __forceinline__ u32x4 close(const float (&x)[4])
-    {
-        u32x4 u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(x[i]);
-        return u;
-    }
-};
-
-// Sum over LANES neighbouring lanes, within a row of 16 on the vector unit's cross-lane path.
-template <int LANES> __device__ __forceinline__ float lanes_sum(float x)
-{
-    static_assert(LANES == 8 || LANES == 16 || LANES == 32, "");
-    auto bits = [&]() { return __builtin_bit_cast(int, x); };
-    auto add = [&](int y) { x += __builtin_bit_cast(float, y); };
-    add(__builtin_amdgcn_update_dpp(bits(), bits(), 0xB1, 0xf, 0xf, false));                   // quad_perm [1,0,3,2]
-    add(__builtin_amdgcn_update_dpp(bits(), bits(), 0x4E, 0xf, 0xf, false));                   // quad_perm [2,3,0,1]
-    add(__builtin_amdgcn_update_dpp(bits(), bits(), 0x141, 0xf, 0xf, false));                  // row_half_mirror
-    if (LANES >= 16) add(__builtin_amdgcn_update_dpp(bits(), bits(), 0x140, 0xf, 0xf, false)); // row_mirror
-    if (LANES == 32) x += __shfl_xor(x, 16);
-    return x;
-}
-
-// The value of the lane half a head away, where the whole head turns.
-template <int LANES> __device__ __forceinline__ float other_half(float x)
-{
-    const int b = __builtin_bit_cast(int, x);
-    if constexpr (LANES == 16) return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, 0x128, 0xf, 0xf, false)); // row_ror 8
-    else if constexpr (LANES == 8) { // of eight lanes, and of each four: the mirror of the mirror
-        const int m = __builtin_amdgcn_update_dpp(b, b, 0x141, 0xf, 0xf, false);
-        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(m, m, 0x1B, 0xf, 0xf, false));
-    } else return __shfl_xor(x, LANES / 2);
-}
-
 // Bound by memory: a head is read once and written once.  A workgroup owns a few tokens; LPH neighbouring lanes own a head, a
 // 16-byte unit each, so a norm and a rotation stay within a wave.  A thread has part in heads of one token only, always the same
 // unit of them: its cosines and sines, weights and the token's row are looked up once (looked up for each unit, 16001 tokens of 32 / 8 heads
@@ -294,42 +234,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const TrPagedAppendAr
             if (hv < 0 && (pairs || normed)) {
                 float x[N];
                 V::open(u[i], x);
-                if (normed) {
-                    auto mean_square = [&]() {
-                        float ss = 0.0f;
-#pragma unroll
-                        for (int c = 0; c < N; ++c) ss = fmaf(x[c], x[c], ss);
-                        return lanes_sum<LPH>(ss) * (1.0f / D);
-                    };
-                    float under = mean_square() + a.eps;
-                    if (!(under <= __FLT_MAX__)) { // for all lanes of the head: the same of a head 2^70 times smaller
-#pragma unroll
-                        for (int c = 0; c < N; ++c) x[c] *= 0x1p-70f;
-                        under = mean_square() + a.eps * 0x1p-70f * 0x1p-70f;
-                    }
-                    const float r = rsqrtf(under);
-#pragma unroll
-                    for (int c = 0; c < N; ++c) x[c] = x[c] * r * (hk < 0 ? qw[c] : kw[c]); // in this order: x r is of size 1
-                }
-                if (HALF) {
-                    float y[N];
-                    if (full) {
-#pragma unroll
-                        for (int c = 0; c < N; ++c) y[c] = other_half<LPH>(x[c]);
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < N; ++c) y[c] = __shfl(x[c], partner);
-                    }
-#pragma unroll
-                    for (int c = 0; c < N; ++c) x[c] = turns ? x[c] * e[c].x + y[c] * e[c].y : x[c];
-                } else {
-#pragma unroll
-                    for (int c = 0; c < N / 2; ++c) {
-                        const float one = x[2 * c], two = x[2 * c + 1];
-                        x[2 * c] = turns ? one * e[c].x - two * e[c].y : one;
-                        x[2 * c + 1] = turns ? two * e[c].x + one * e[c].y : two;
-                    }
-                }
+                norm_and_turn<N, LPH, HALF>(x, normed, hk < 0 ? qw : kw, a.eps, e, turns, full, partner);
                 if (normed || turns) u[i] = V::close(x);
             }
             char* const to = hk < 0 ? qd + (int64_t)head * HEAD : hv < 0 ? kd + (int64_t)hk * a.pool.head_stride : vd + (int64_t)hv * a.pool.head_stride;

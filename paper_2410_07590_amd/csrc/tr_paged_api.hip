@@ -22,35 +22,71 @@ int page_shift(int32_t page_size)
 }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-// Checks the pool against the shape and gives the form that the kernels address.
+// A pool of either kind, as the checks see it: strides in elements.
+struct Pages {
+    const char *k, *v;
+    int64_t page_stride, row_stride, head_stride;
+    int32_t n_pages, page_size, heads, d;
+    int64_t e; // bytes of an element
+    const uint8_t *k_scale, *v_scale; // NULL: a pool without scales
+};
+Pages pages_of(const tr_pages* p)
+{
+    return {(const char*)p->k, (const char*)p->v, p->page_stride, p->row_stride, p->head_stride, p->n_pages, p->page_size, p->n_kv_heads, p->head_dim,
+            p->dtype == TR_F32 ? 4 : 2, nullptr, nullptr};
+}
+Pages pages_of(const tr_pages_q8* p)
+{
+    return {(const char*)p->k, (const char*)p->v, p->page_stride, p->row_stride, p->head_stride, p->n_pages, p->page_size, p->n_kv_heads, p->head_dim,
+            1, p->k_scale, p->v_scale};
+}
+
+// Gives the form that the kernels address, where it describes a pool.
+int check_pool(const char* who, const Pages& p, int least_page, TrPool* out)
+{
+    const int shift = page_shift(p.page_size);
+    if (shift < 0 || p.page_size < least_page)
+        return tr_fail(TR_ERR_INVALID_ARG, "%s: page_size %d is not a power of two from %d to 1024", who, p.page_size, least_page);
+    if (p.n_pages < 1 || (int64_t)p.n_pages * p.page_size > INT_LIMIT) return tr_fail(TR_ERR_INVALID_ARG, "%s: n_pages %d", who, p.n_pages);
+    if (!p.k || !p.v) return tr_fail(TR_ERR_INVALID_ARG, "%s: k or v of the pages is NULL", who);
+    const int64_t e = p.e, widest = (int64_t)64 << 20;
+    // a stride of a single page or head is never applied; whether the others keep rows apart matters where rows are written
+    if (p.row_stride < p.d || (p.heads > 1 && p.head_stride < p.d) || (p.n_pages > 1 && p.page_stride < p.d))
+        return tr_fail(TR_ERR_INVALID_ARG, "%s: strides of the pages are smaller than a head", who);
+    if (p.head_stride < 0 || p.page_stride < 0) // of a single head or page
+        return tr_fail(TR_ERR_INVALID_ARG, "%s: strides of the pages are out of range", who);
+    if (p.row_stride > widest / e || p.head_stride > widest / e || p.page_stride > (widest * 64 - 1) / e)
+        return tr_fail(TR_ERR_UNSUPPORTED, "%s: rows or heads of the pages are more than 64 MiB apart, or pages 4 GiB", who);
+    if (!aligned16(p.k) || !aligned16(p.v) || p.page_stride * e % 16 || p.row_stride * e % 16 || p.head_stride * e % 16)
+        return tr_fail(TR_ERR_INVALID_ARG, "%s: pages and their strides must be 16-byte aligned", who);
+    out->k = const_cast<char*>(p.k);
+    out->v = const_cast<char*>(p.v);
+    out->page_stride = (uint32_t)(p.page_stride * e);
+    out->row_stride = (uint32_t)(p.row_stride * e);
+    out->head_stride = (uint32_t)(p.head_stride * e);
+    out->n_pages = p.n_pages;
+    out->page_shift = shift;
+    out->k_scale = const_cast<uint8_t*>(p.k_scale);
+    out->v_scale = const_cast<uint8_t*>(p.v_scale);
+    return TR_OK;
+}
+// Checks the pool against the shape, too.
 int pool_of(const char* who, const tr_shape* sh, const tr_pages* p, TrPool* out)
 {
     if (p->reserved != 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: reserved of tr_pages must be 0", who);
     if (p->dtype != sh->dtype || p->n_kv_heads != sh->n_kv_heads || p->head_dim != sh->head_dim)
         return tr_fail(TR_ERR_SHAPE, "%s: pages of type %d with %d heads of %d channels, the shape has type %d, %d heads, %d channels", who, p->dtype,
                        p->n_kv_heads, p->head_dim, sh->dtype, sh->n_kv_heads, sh->head_dim);
-    const int shift = page_shift(p->page_size);
-    if (shift < 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: page_size %d is not a power of two from 8 to 1024", who, p->page_size);
-    if (p->n_pages < 1 || (int64_t)p->n_pages * p->page_size > INT_LIMIT) return tr_fail(TR_ERR_INVALID_ARG, "%s: n_pages %d", who, p->n_pages);
-    if (!p->k || !p->v) return tr_fail(TR_ERR_INVALID_ARG, "%s: k or v of the pages is NULL", who);
-    const int64_t e = tr_elem_bytes(sh), widest = (int64_t)64 << 20;
-    // a stride of a single page or head is never applied; whether the others keep rows apart matters where rows are written
-    if (p->row_stride < sh->head_dim || (p->n_kv_heads > 1 && p->head_stride < sh->head_dim) || (p->n_pages > 1 && p->page_stride < sh->head_dim))
-        return tr_fail(TR_ERR_INVALID_ARG, "%s: strides of the pages are smaller than a head", who);
-    if (p->head_stride < 0 || p->page_stride < 0) // of a single head or page
-        return tr_fail(TR_ERR_INVALID_ARG, "%s: strides of the pages are out of range", who);
-    if (p->row_stride > widest / e || p->head_stride > widest / e || p->page_stride > (widest * 64 - 1) / e)
-        return tr_fail(TR_ERR_UNSUPPORTED, "%s: rows or heads of the pages are more than 64 MiB apart, or pages 4 GiB", who);
-    if (!aligned16(p->k) || !aligned16(p->v) || p->page_stride * e % 16 || p->row_stride * e % 16 || p->head_stride * e % 16)
-        return tr_fail(TR_ERR_INVALID_ARG, "%s: pages and their strides must be 16-byte aligned", who);
-    out->k = (char*)p->k;
-    out->v = (char*)p->v;
-    out->page_stride = (uint32_t)(p->page_stride * e);
-    out->row_stride = (uint32_t)(p->row_stride * e);
-    out->head_stride = (uint32_t)(p->head_stride * e);
-    out->n_pages = p->n_pages;
-    out->page_shift = shift;
-    return TR_OK;
+    return check_pool(who, pages_of(p), 8, out);
+}
+int pool_of(const char* who, const tr_shape* sh, const tr_pages_q8* p, TrPool* out)
+{
+    if (p->reserved != 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: reserved of tr_pages_q8 must be 0", who);
+    if (p->n_kv_heads != sh->n_kv_heads || p->head_dim != sh->head_dim)
+        return tr_fail(TR_ERR_SHAPE, "%s: pages with %d heads of %d channels, the shape has %d heads, %d channels", who, p->n_kv_heads, p->head_dim,
+                       sh->n_kv_heads, sh->head_dim);
+    if (!p->k_scale || !p->v_scale) return tr_fail(TR_ERR_INVALID_ARG, "%s: k_scale or v_scale of the pages is NULL", who);
+    return check_pool(who, pages_of(p), TR_Q8_ROWS, out);
 }
 
 struct Span {
@@ -65,11 +101,18 @@ bool overlap(const Span& a, const Span& b)
 Span ints(const int32_t* p, int64_t n) { return {p, p ? 4 * n : 0}; }
 // n rows of `row` bytes, a stride apart
 Span rows(const void* p, int64_t n, int64_t stride, int64_t row) { return {p, p ? (n - 1) * stride + row : 0}; }
-// all rows of a pool, and what lies between them
-Span pool_span(const TrPool& pool, const void* base, const tr_pages* p)
+// what a pool consists of: all rows of K and of V with what lies between them, and the scales
+struct Spans {
+    Span s[4];
+    int n;
+    const Span* begin() const { return s; }
+    const Span* end() const { return s + n; }
+};
+Spans pool_spans(const Pages& p)
 {
-    return {base, (p->n_pages - 1) * (int64_t)pool.page_stride + (p->page_size - 1) * (int64_t)pool.row_stride +
-                      (p->n_kv_heads - 1) * (int64_t)pool.head_stride + p->head_dim * (int64_t)(p->dtype == TR_F32 ? 4 : 2)};
+    const int64_t bytes = ((p.n_pages - 1) * p.page_stride + (p.page_size - 1) * p.row_stride + (p.heads - 1) * p.head_stride + p.d) * p.e;
+    const int64_t scales = (int64_t)p.n_pages * (p.page_size / TR_Q8_ROWS) * p.heads;
+    return {{{p.k, bytes}, {p.v, bytes}, {p.k_scale, scales}, {p.v_scale, scales}}, p.k_scale ? 4 : 2};
 }
 
 // Whether every row of K and V has bytes of its own.  Strides nest: taken by size, each is at least what the ones below it span.
@@ -88,13 +131,12 @@ bool rows_meet(const Nest& n, int axes, int64_t apart)
         if (i >= -most && i <= most && rows_meet(n, axes - 1, apart - i * s)) return true;
     return false;
 }
-bool rows_apart(const tr_pages* p)
+bool rows_apart(const Pages& p)
 {
-    const int64_t e = p->dtype == TR_F32 ? 4 : 2;
-    std::pair<int64_t, int64_t> axes[] = {{p->head_stride * e, p->n_kv_heads}, {p->row_stride * e, p->page_size}, {p->page_stride * e, p->n_pages}};
+    std::pair<int64_t, int64_t> axes[] = {{p.head_stride * p.e, p.heads}, {p.row_stride * p.e, p.page_size}, {p.page_stride * p.e, p.n_pages}};
     std::sort(axes, axes + 3);
     Nest n;
-    n.span[0] = p->head_dim * e;
+    n.span[0] = p.d * p.e;
     for (const auto& [stride, count] : axes) {
         if (count == 1) continue;
         if (stride < n.span[n.axes]) return false;
@@ -103,7 +145,7 @@ bool rows_apart(const tr_pages* p)
         n.span[n.axes + 1] = (count - 1) * stride + n.span[n.axes];
         ++n.axes;
     }
-    return !rows_meet(n, n.axes, (int64_t)((intptr_t)p->v - (intptr_t)p->k));
+    return !rows_meet(n, n.axes, (int64_t)((intptr_t)p.v - (intptr_t)p.k));
 }
 
 } // namespace
@@ -189,13 +231,14 @@ extern "C" int tr_rotary_init(int32_t layout, int32_t rotary_dim, double base, i
     });
 }
 
-extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
-                               const void* v, int64_t v_stride, const void* q_norm, const void* k_norm, double eps, const int32_t* pos,
-                               const int32_t* slots, int32_t n_tokens, void* q_out, const tr_pages* pages, void* stream)
+namespace {
+// The checks of both calls that append, and their kernels' arguments.  n_tokens stays 0 where there is nothing to do.
+template <class POOL>
+int append_args(const char* who, const tr_shape* shape, const tr_rotary* rotary, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                int64_t v_stride, const void* q_norm, const void* k_norm, double eps, const int32_t* pos, const int32_t* slots, int32_t n_tokens, void* q_out,
+                const POOL* pages, TrPagedAppendArgs& a, int& layout)
 {
-    return tr_guard_int([&]() -> int {
-    tr_clear_error();
-    const char* const who = "tr_paged_append";
+    memset(&a, 0, sizeof a);
     if (int rc = tr_check_shape(shape)) return rc;
     if (n_tokens < 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: n_tokens < 0", who);
     if (shape->n_q_heads > MOST_HEADS) return tr_fail(TR_ERR_UNSUPPORTED, "%s: %d heads, at most 2^20", who, shape->n_q_heads);
@@ -203,9 +246,7 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     const int given = (k != nullptr) + (v != nullptr) + (slots != nullptr) + (pages != nullptr);
     if (n_tokens > 0 && given != 0 && given != 4) return tr_fail(TR_ERR_INVALID_ARG, "%s: k, v, slots and pages go together", who);
     if (!((float)eps >= FLT_MIN) || !isfinite((float)eps)) return tr_fail(TR_ERR_INVALID_ARG, "%s: eps must be finite and a positive normal fp32 value", who);
-    TrPagedAppendArgs a;
-    memset(&a, 0, sizeof a);
-    int layout = shape->rope_layout;
+    layout = shape->rope_layout;
     if (rotary) {
         layout = rotary->layout;
         if (layout != TR_ROPE_INTERLEAVED && layout != TR_ROPE_HALF) return tr_fail(TR_ERR_INVALID_ARG, "%s: layout %d of the rotary", who, layout);
@@ -226,7 +267,11 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     const int64_t e = tr_elem_bytes(shape), q_row = (int64_t)shape->n_q_heads * shape->head_dim, kv_row = (int64_t)shape->n_kv_heads * shape->head_dim;
     if (pages) {
         if (int rc = pool_of(who, shape, pages, &a.pool)) return rc;
-        if (!rows_apart(pages)) return tr_fail(TR_ERR_INVALID_ARG, "%s: rows of the pages use the same bytes", who);
+        if (!rows_apart(pages_of(pages))) return tr_fail(TR_ERR_INVALID_ARG, "%s: rows of the pages use the same bytes", who);
+        const Spans own = pool_spans(pages_of(pages));
+        for (int i = 2; i < own.n; ++i)
+            for (int j = 0; j < i; ++j)
+                if (overlap(own.s[i], own.s[j])) return tr_fail(TR_ERR_INVALID_ARG, "%s: scales of the pages overlap each other or the codes", who);
     }
     if (n_tokens == 0 || (!q && !k)) return TR_OK;
     if (a.rotary_dim && !pos) return tr_fail(TR_ERR_INVALID_ARG, "%s: pos is NULL", who);
@@ -241,7 +286,7 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     for (const Span& s : in)
         if (overlap(outs, s)) return tr_fail(TR_ERR_INVALID_ARG, "%s: q_out overlaps an input", who);
     if (pages) {
-        for (const Span& pool : {pool_span(a.pool, pages->k, pages), pool_span(a.pool, pages->v, pages)}) {
+        for (const Span& pool : pool_spans(pages_of(pages))) {
             for (const Span& s : in)
                 if (overlap(pool, s)) return tr_fail(TR_ERR_INVALID_ARG, "%s: the pages overlap an input", who);
             if (overlap(pool, qs) || overlap(pool, outs)) return tr_fail(TR_ERR_INVALID_ARG, "%s: the pages overlap q or q_out", who);
@@ -265,15 +310,57 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     a.n_q_heads = q ? shape->n_q_heads : 0;
     a.n_kv_heads = k ? shape->n_kv_heads : 0;
     a.eps = (float)eps;
+    return TR_OK;
+}
+void append_tiles(TrPagedAppendArgs& a, const tr_shape* shape)
+{
     // A workgroup takes as many tokens as give its threads eight units each, if there are workgroups enough then.  us for 1 token /
     // this: 24000 rows of 4 KV heads of 128 44.6 / 23.6, 16000 tokens of 16 + 4 heads of 64 47.6 / 23.9, 16001 of 32 + 8 of 128 88.3 / 79.0.
-    const int64_t units = (int64_t)(a.n_q_heads + 2 * a.n_kv_heads) * shape->head_dim * e / 16; // of a token
-    while ((2 << a.tile_shift) <= TR_PAGED_APPEND_TOKENS && (units << a.tile_shift) * 2 <= 2048 && n_tokens >= 2048ll << a.tile_shift) ++a.tile_shift;
+    const int64_t units = (int64_t)(a.n_q_heads + 2 * a.n_kv_heads) * shape->head_dim * tr_elem_bytes(shape) / 16; // of a token
+    while ((2 << a.tile_shift) <= TR_PAGED_APPEND_TOKENS && (units << a.tile_shift) * 2 <= 2048 && a.n_tokens >= 2048ll << a.tile_shift) ++a.tile_shift;
     // Streamed stores make the call itself faster at any size, and what reads its results next slower where the caches still
     // hold them: us of the call and a pass over all it wrote, ordinary / streamed, by MB written: 12 MB 18.6 / 17.9, 25 MB 27.9 / 29.4, 49 MB
     // 45.4 / 46.8, 98 MB 78.4 / 84.1, 197 MB 151.5 / 148.0.
-    a.stream = 16 * units * n_tokens >= 150ll << 20;
+    a.stream = 16 * units * a.n_tokens >= 150ll << 20;
+}
+} // namespace
+
+extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, const void* q_norm, const void* k_norm, double eps, const int32_t* pos,
+                               const int32_t* slots, int32_t n_tokens, void* q_out, const tr_pages* pages, void* stream)
+{
+    return tr_guard_int([&]() -> int {
+    tr_clear_error();
+    TrPagedAppendArgs a;
+    int layout;
+    if (int rc = append_args("tr_paged_append", shape, rotary, q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm, eps, pos, slots, n_tokens, q_out, pages, a, layout))
+        return rc;
+    if (a.n_tokens == 0) return TR_OK;
+    append_tiles(a, shape);
     return tr_launch_paged_append(a, shape->dtype, shape->head_dim, layout, (hipStream_t)stream);
+    });
+}
+
+extern "C" int tr_paged_append_q8(const tr_shape* shape, const tr_rotary* rotary, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                  const void* v, int64_t v_stride, const void* q_norm, const void* k_norm, double eps, const int32_t* pos,
+                                  const int32_t* slots, int32_t n_tokens, void* q_out, const tr_pages_q8* pages, void* stream)
+{
+    return tr_guard_int([&]() -> int {
+    tr_clear_error();
+    TrPagedAppendArgs a;
+    int layout;
+    if (int rc = append_args("tr_paged_append_q8", shape, rotary, q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm, eps, pos, slots, n_tokens, q_out, pages, a, layout))
+        return rc;
+    if (a.n_tokens == 0) return TR_OK;
+    if (a.q) {
+        TrPagedAppendArgs b = a;
+        b.k = b.v = nullptr;
+        b.slots = nullptr;
+        b.n_kv_heads = 0;
+        append_tiles(b, shape);
+        if (int rc = tr_launch_paged_append(b, shape->dtype, shape->head_dim, layout, (hipStream_t)stream)) return rc;
+    }
+    return a.k ? tr_launch_paged_append_q8(a, shape->dtype, shape->head_dim, layout, (hipStream_t)stream) : TR_OK;
     });
 }
 
@@ -285,46 +372,45 @@ struct DecodePlan {
     int32_t ws_rows;
     size_t ml_at, items_at, bytes;
 };
-DecodePlan decode_plan(const tr_shape* sh, int64_t n_req, int64_t keys)
+struct DecodeForm {
+    int unit;       // keys that a wave takes at a time
+    int workers;    // waves of a launch
+    int least_page;
+};
+DecodePlan decode_plan(const tr_shape* sh, int64_t n_req, int64_t keys, const DecodeForm& form)
 {
     DecodePlan p;
     const int group = sh->n_q_heads / sh->n_kv_heads, tile = tr_paged_tile_rows(group);
     p.items = n_req * sh->n_kv_heads * ((group + tile - 1) / tile);
-    const int unit = tr_paged_unit_keys(sh->dtype);
-    const int64_t units = std::max<int64_t>((keys + unit - 1) / unit, 1);
+    const int64_t units = std::max<int64_t>((keys + form.unit - 1) / form.unit, 1);
     p.bound = p.items * units;
     p.ws_rows = std::min(group, tile);
     const bool none = units == 1; // a unit is never cut
-    p.ml_at = tr_align256(2ull * TR_PAGED_WORKERS * p.ws_rows * sh->head_dim * 4);
-    p.items_at = p.ml_at + tr_align256(2ull * TR_PAGED_WORKERS * p.ws_rows * 8);
-    p.bytes = none ? 0 : p.items_at + tr_align256((size_t)std::max<int64_t>(p.items, TR_PAGED_WORKERS) * 8);
+    p.ml_at = tr_align256(2ull * form.workers * p.ws_rows * sh->head_dim * 4);
+    p.items_at = p.ml_at + tr_align256(2ull * form.workers * p.ws_rows * 8);
+    p.bytes = none ? 0 : p.items_at + tr_align256((size_t)std::max<int64_t>(p.items, form.workers) * 8);
     return p;
 }
 } // namespace
 
-extern "C" size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size)
+namespace {
+size_t decode_workspace(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size, const DecodeForm& form)
 {
-    return tr_guard_size([&]() -> size_t {
-    tr_clear_error();
-    if (tr_check_shape(shape) || n_req < 1 || max_blocks < 1 || page_shift(page_size) < 0) return 0;
+    if (tr_check_shape(shape) || n_req < 1 || max_blocks < 1 || page_shift(page_size) < 0 || page_size < form.least_page) return 0;
     if (n_req > MOST_REQUESTS || (int64_t)n_req * shape->n_q_heads > TR_MAX_BLOCKS_256 || (int64_t)max_blocks * page_size > MOST_KEYS) return 0; // refused
-    const DecodePlan plan = decode_plan(shape, n_req, (int64_t)max_blocks * page_size);
+    const DecodePlan plan = decode_plan(shape, n_req, (int64_t)max_blocks * page_size, form);
     return plan.bound > MOST_UNITS ? 0 : plan.bytes;
-    });
 }
-
-extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const tr_pages* pages, const int32_t* block_table, int32_t max_blocks,
-                                    const int32_t* kv_lens, int32_t n_req, int32_t window, int32_t n_sink, void* out, void* workspace,
-                                    size_t workspace_bytes, void* stream)
+// The checks of both calls, and their kernels' arguments.  n_req stays 0 where there is nothing to do.
+template <class POOL>
+int decode_args(const char* who, const tr_shape* shape, const void* q, const POOL* pages, const int32_t* block_table, int32_t max_blocks, const int32_t* kv_lens,
+                int32_t n_req, int32_t window, int32_t n_sink, void* out, void* workspace, size_t workspace_bytes, const DecodeForm& form, TrPagedDecodeArgs& a,
+                int& workers)
 {
-    return tr_guard_int([&]() -> int {
-    tr_clear_error();
-    const char* const who = "tr_paged_decode_attn";
     if (int rc = tr_check_shape(shape)) return rc;
     if (n_req < 0 || max_blocks < 0 || window < 0 || n_sink < 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: a count is negative", who);
     if (n_req > MOST_REQUESTS) return tr_fail(TR_ERR_UNSUPPORTED, "%s: %d requests, at most %d", who, n_req, MOST_REQUESTS);
     if (!pages) return tr_fail(TR_ERR_INVALID_ARG, "%s: pages is NULL", who);
-    TrPagedDecodeArgs a;
     memset(&a, 0, sizeof a);
     if (int rc = pool_of(who, shape, pages, &a.pool)) return rc;
     if ((int64_t)max_blocks * pages->page_size > MOST_KEYS) return tr_fail(TR_ERR_INVALID_ARG, "%s: max_blocks %d", who, max_blocks);
@@ -335,7 +421,9 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     const int64_t row = (int64_t)shape->n_q_heads * shape->head_dim * tr_elem_bytes(shape);
     const Span outs = rows(out, n_req, row, row);
     if (overlap(outs, rows(q, n_req, row, row)) && out != q) return tr_fail(TR_ERR_INVALID_ARG, "%s: out overlaps q without being it", who);
-    for (const Span& s : {pool_span(a.pool, pages->k, pages), pool_span(a.pool, pages->v, pages), ints(block_table, (int64_t)n_req * max_blocks), ints(kv_lens, n_req)})
+    for (const Span& s : pool_spans(pages_of(pages)))
+        if (overlap(outs, s)) return tr_fail(TR_ERR_INVALID_ARG, "%s: out overlaps the pages, the table or the lengths", who);
+    for (const Span& s : {ints(block_table, (int64_t)n_req * max_blocks), ints(kv_lens, n_req)})
         if (overlap(outs, s)) return tr_fail(TR_ERR_INVALID_ARG, "%s: out overlaps the pages, the table or the lengths", who);
     a.q = q;
     a.out = out;
@@ -349,8 +437,8 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
     a.n_kv_heads = shape->n_kv_heads;
     a.group = shape->n_q_heads / shape->n_kv_heads;
     a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)shape->head_dim));
-    const DecodePlan plan = decode_plan(shape, n_req, (int64_t)max_blocks * pages->page_size);
-    if (plan.bound > MOST_UNITS) return tr_fail(TR_ERR_UNSUPPORTED, "%s: the table has room for more than 2^30 units of 32 (fp32: 16) keys", who);
+    const DecodePlan plan = decode_plan(shape, n_req, (int64_t)max_blocks * pages->page_size, form);
+    if (plan.bound > MOST_UNITS) return tr_fail(TR_ERR_UNSUPPORTED, "%s: the table has room for more than 2^30 units of %d keys", who, form.unit);
     if (plan.bytes) {
         if (!workspace || ((uintptr_t)workspace & 255)) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace missing or not 256-byte aligned", who);
         if (workspace_bytes < plan.bytes) return tr_fail(TR_ERR_WORKSPACE, "%s: workspace holds %zu bytes, %zu needed", who, workspace_bytes, plan.bytes);
@@ -359,12 +447,102 @@ extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const 
         a.ws_items = (int32_t*)((char*)workspace + plan.items_at);
     }
     a.ws_rows = plan.ws_rows;
-    const int64_t workers = std::min<int64_t>((plan.bound + TR_PAGED_MIN_UNITS - 1) / TR_PAGED_MIN_UNITS, TR_PAGED_WORKERS);
+    workers = (int)std::min<int64_t>((plan.bound + TR_PAGED_MIN_UNITS - 1) / TR_PAGED_MIN_UNITS, form.workers);
     // The join's workgroups, most of which find nothing to do, are what it costs: it looks at the rows of the result or at those
     // that each wave may have cut, whichever are fewer.  us of the whole call by row / by wave: 200 requests of 50 to 1200 rows, 32 / 8
     // heads (6400 rows or 4096) 102.7 / 101.1, 512 of 256 (16384 or 4096) 96.2 / 93.4, 4096 of 10 to 60, 16 / 4 heads of 64 (65536 or 4096)
     // 92.7 / 78.7.
     if (plan.bytes) a.cut = (int64_t)n_req * shape->n_q_heads <= workers * plan.ws_rows ? TR_PAGED_JOIN_BY_ROW : TR_PAGED_JOIN_BY_WAVE;
-    return tr_launch_paged_decode(a, shape->dtype, shape->head_dim, (int)workers, (hipStream_t)stream);
+    return TR_OK;
+}
+DecodeForm plain_form(const tr_shape* shape) { return {shape && shape->dtype == TR_BF16 ? tr_paged_unit_keys(TR_BF16) : tr_paged_unit_keys(TR_F32), TR_PAGED_WORKERS, 8}; }
+DecodeForm q8_form(const tr_shape*) { return {TR_Q8_UNIT, TR_PAGED_WORKERS, TR_Q8_ROWS}; }
+} // namespace
+
+extern "C" size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size)
+{
+    return tr_guard_size([&]() -> size_t {
+    tr_clear_error();
+    return decode_workspace(shape, n_req, max_blocks, page_size, plain_form(shape));
+    });
+}
+
+extern "C" int tr_paged_decode_attn(const tr_shape* shape, const void* q, const tr_pages* pages, const int32_t* block_table, int32_t max_blocks,
+                                    const int32_t* kv_lens, int32_t n_req, int32_t window, int32_t n_sink, void* out, void* workspace,
+                                    size_t workspace_bytes, void* stream)
+{
+    return tr_guard_int([&]() -> int {
+    tr_clear_error();
+    TrPagedDecodeArgs a;
+    int workers;
+    if (int rc = decode_args("tr_paged_decode_attn", shape, q, pages, block_table, max_blocks, kv_lens, n_req, window, n_sink, out, workspace, workspace_bytes,
+                             plain_form(shape), a, workers))
+        return rc;
+    if (a.n_req == 0) return TR_OK;
+    return tr_launch_paged_decode(a, shape->dtype, shape->head_dim, workers, (hipStream_t)stream);
+    });
+}
+
+extern "C" size_t tr_paged_decode_attn_q8_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size)
+{
+    return tr_guard_size([&]() -> size_t {
+    tr_clear_error();
+    return decode_workspace(shape, n_req, max_blocks, page_size, q8_form(shape));
+    });
+}
+
+extern "C" int tr_paged_decode_attn_q8(const tr_shape* shape, const void* q, const tr_pages_q8* pages, const int32_t* block_table, int32_t max_blocks,
+                                       const int32_t* kv_lens, int32_t n_req, int32_t window, int32_t n_sink, void* out, void* workspace,
+                                       size_t workspace_bytes, void* stream)
+{
+    return tr_guard_int([&]() -> int {
+    tr_clear_error();
+    TrPagedDecodeArgs a;
+    int workers;
+    if (int rc = decode_args("tr_paged_decode_attn_q8", shape, q, pages, block_table, max_blocks, kv_lens, n_req, window, n_sink, out, workspace, workspace_bytes,
+                             q8_form(shape), a, workers))
+        return rc;
+    if (a.n_req == 0) return TR_OK;
+    return tr_launch_paged_decode_q8(a, shape->dtype, shape->head_dim, workers, (hipStream_t)stream);
+    });
+}
+
+extern "C" int tr_paged_read_q8(const tr_shape* shape, const tr_pages_q8* pages, const int32_t* block_table, int32_t max_blocks, const int32_t* kv_lens,
+                                const int32_t* row_start, int32_t n_req, void* out_k, void* out_v, int32_t n_rows, void* stream)
+{
+    return tr_guard_int([&]() -> int {
+    tr_clear_error();
+    const char* const who = "tr_paged_read_q8";
+    if (int rc = tr_check_shape(shape)) return rc;
+    if (n_req < 0 || max_blocks < 0 || n_rows < 0) return tr_fail(TR_ERR_INVALID_ARG, "%s: a count is negative", who);
+    if (n_req > MOST_REQUESTS) return tr_fail(TR_ERR_UNSUPPORTED, "%s: %d requests, at most %d", who, n_req, MOST_REQUESTS);
+    if (!pages) return tr_fail(TR_ERR_INVALID_ARG, "%s: pages is NULL", who);
+    TrPagedReadArgs a;
+    memset(&a, 0, sizeof a);
+    if (int rc = pool_of(who, shape, pages, &a.pool)) return rc;
+    if (shape->n_kv_heads > MOST_HEADS) return tr_fail(TR_ERR_UNSUPPORTED, "%s: %d heads, at most 2^20", who, shape->n_kv_heads);
+    if ((int64_t)max_blocks * pages->page_size > MOST_KEYS) return tr_fail(TR_ERR_INVALID_ARG, "%s: max_blocks %d", who, max_blocks);
+    if (n_req == 0 || n_rows == 0 || max_blocks == 0) return TR_OK;
+    if (!block_table || !kv_lens || !row_start || !out_k || !out_v) return tr_fail(TR_ERR_INVALID_ARG, "%s: an array is NULL", who);
+    if (!aligned16(out_k) || !aligned16(out_v)) return tr_fail(TR_ERR_INVALID_ARG, "%s: the outputs must be 16-byte aligned", who);
+    const int64_t row = (int64_t)shape->n_kv_heads * shape->head_dim * tr_elem_bytes(shape);
+    const Span out[] = {rows(out_k, n_rows, row, row), rows(out_v, n_rows, row, row)};
+    if (overlap(out[0], out[1])) return tr_fail(TR_ERR_INVALID_ARG, "%s: the outputs overlap", who);
+    for (const Span& o : out) {
+        for (const Span& s : pool_spans(pages_of(pages)))
+            if (overlap(o, s)) return tr_fail(TR_ERR_INVALID_ARG, "%s: an output overlaps the pages", who);
+        for (const Span& s : {ints(block_table, (int64_t)n_req * max_blocks), ints(kv_lens, n_req), ints(row_start, (int64_t)n_req + 1)})
+            if (overlap(o, s)) return tr_fail(TR_ERR_INVALID_ARG, "%s: an output overlaps an index array", who);
+    }
+    a.table = block_table;
+    a.kv_lens = kv_lens;
+    a.row_start = row_start;
+    a.out_k = (char*)out_k;
+    a.out_v = (char*)out_v;
+    a.n_req = n_req;
+    a.max_blocks = max_blocks;
+    a.n_rows = n_rows;
+    a.n_kv_heads = shape->n_kv_heads;
+    return tr_launch_paged_read_q8(a, shape->dtype, shape->head_dim, (hipStream_t)stream);
     });
 }
