@@ -411,6 +411,7 @@ struct TrPool {
 };
 #define TR_Q8_ROWS 16 // that share a scale
 #define TR_Q8_UNIT 32 // keys that a wave of the decode over 8 bits takes at a time
+__host__ __device__ constexpr int tr_q8_workers(int dtype, int group) { return dtype == TR_F32 && group > 16 ? 1024 : 2048; } // waves; rings of 20 KB, or 40
 #define TR_PAGED_APPEND_TOKENS 8 // at most, of a workgroup
 struct TrPagedAppendArgs {
     const char* q;
