@@ -410,6 +410,7 @@ struct TrPool {
     uint8_t *k_scale, *v_scale; // of a pool in 8 bits
 };
 #define TR_Q8_ROWS 16 // that share a scale
+#define TR_Q8_FEW 4096 // tokens of an append that get a workgroup each, to look whether they begin a block
 #define TR_Q8_UNIT 32 // keys that a wave of the decode over 8 bits takes at a time
 __host__ __device__ constexpr int tr_q8_workers(int dtype, int group) { return dtype == TR_F32 && group > 16 ? 1024 : 2048; } // waves; rings of 20 KB, or 40
 #define TR_PAGED_APPEND_TOKENS 8 // at most, of a workgroup

@@ -312,11 +312,11 @@ int append_args(const char* who, const tr_shape* shape, const tr_rotary* rotary,
     a.eps = (float)eps;
     return TR_OK;
 }
-void append_tiles(TrPagedAppendArgs& a, const tr_shape* shape)
+void append_tiles(TrPagedAppendArgs& a, const tr_shape* shape, int64_t heads) // of a token, in the pass over heads
 {
     // A workgroup takes as many tokens as give its threads eight units each, if there are workgroups enough then.  us for 1 token /
     // this: 24000 rows of 4 KV heads of 128 44.6 / 23.6, 16000 tokens of 16 + 4 heads of 64 47.6 / 23.9, 16001 of 32 + 8 of 128 88.3 / 79.0.
-    const int64_t units = (int64_t)(a.n_q_heads + 2 * a.n_kv_heads) * shape->head_dim * tr_elem_bytes(shape) / 16; // of a token
+    const int64_t units = heads * shape->head_dim * tr_elem_bytes(shape) / 16; // of a token
     while ((2 << a.tile_shift) <= TR_PAGED_APPEND_TOKENS && (units << a.tile_shift) * 2 <= 2048 && a.n_tokens >= 2048ll << a.tile_shift) ++a.tile_shift;
     // Streamed stores make the call itself faster at any size, and what reads its results next slower where the caches still
     // hold them: us of the call and a pass over all it wrote, ordinary / streamed, by MB written: 12 MB 18.6 / 17.9, 25 MB 27.9 / 29.4, 49 MB
@@ -336,7 +336,7 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     if (int rc = append_args("tr_paged_append", shape, rotary, q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm, eps, pos, slots, n_tokens, q_out, pages, a, layout))
         return rc;
     if (a.n_tokens == 0) return TR_OK;
-    append_tiles(a, shape);
+    append_tiles(a, shape, a.n_q_heads + 2ll * a.n_kv_heads);
     return tr_launch_paged_append(a, shape->dtype, shape->head_dim, layout, (hipStream_t)stream);
     });
 }
@@ -352,15 +352,8 @@ extern "C" int tr_paged_append_q8(const tr_shape* shape, const tr_rotary* rotary
     if (int rc = append_args("tr_paged_append_q8", shape, rotary, q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm, eps, pos, slots, n_tokens, q_out, pages, a, layout))
         return rc;
     if (a.n_tokens == 0) return TR_OK;
-    if (a.q) {
-        TrPagedAppendArgs b = a;
-        b.k = b.v = nullptr;
-        b.slots = nullptr;
-        b.n_kv_heads = 0;
-        append_tiles(b, shape);
-        if (int rc = tr_launch_paged_append(b, shape->dtype, shape->head_dim, layout, (hipStream_t)stream)) return rc;
-    }
-    return a.k ? tr_launch_paged_append_q8(a, shape->dtype, shape->head_dim, layout, (hipStream_t)stream) : TR_OK;
+    append_tiles(a, shape, a.n_q_heads);
+    return tr_launch_paged_append_q8(a, shape->dtype, shape->head_dim, layout, (hipStream_t)stream);
     });
 }
 

@@ -19,133 +19,185 @@ template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t x)
     return x;
 }
 
-// A workgroup owns the tokens that the call writes to one block of 16 rows: those from its own index on whose slots lie in the block,
-// if the token in front does not.  Their heads need two steps, the largest value of the block's and then the codes; values wait for
-// that in registers.
+// Threads of a workgroup: 16 rows of a head at least.
+constexpr int append_q8_threads(int dtype, int d) { return std::max(256, TR_Q8_ROWS * d * (dtype == TR_F32 ? 4 : 2) / 16); }
+
+// A unit of N channels as codes.
+template <int N> __device__ __forceinline__ void put(char* to, const float (&x)[N])
+{
+    if constexpr (N == 8) *(uint2*)to = make_uint2(q8_encode(x[0], x[1], x[2], x[3]), q8_encode(x[4], x[5], x[6], x[7]));
+    else *(uint32_t*)to = q8_encode(x[0], x[1], x[2], x[3]);
+}
+
+// The rows of `which` of a block, a unit of N channels each, at another scale.
+template <int N> __device__ __forceinline__ void rescale(char* unit, uint32_t row_stride, uint32_t which, float by)
+{
+    constexpr int AT_ONCE = 8;
+#pragma unroll
+    for (int j0 = 0; j0 < TR_Q8_ROWS; j0 += AT_ONCE) {
+        uint32_t w[AT_ONCE][N / 4];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+            for (int c = 0; c < N / 4; ++c) w[j][c] = which & (1u << (j0 + j)) ? ((const uint32_t*)(unit + (int64_t)(j0 + j) * row_stride))[c] : 0u;
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            float y[N];
+#pragma unroll
+            for (int c = 0; c < N; c += 4) {
+                float z[4];
+                q8_decode(w[j][c / 4], z);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) y[c + b] = z[b] * by;
+            }
+            if (which & (1u << (j0 + j))) put<N>(unit + (int64_t)(j0 + j) * row_stride, y);
+        }
+    }
+}
+
+// Quantised heads.  A workgroup looks at `window` tokens and owns the blocks whose first tokens are among them, of keys or of values: the
+// tokens that the call writes to a block of 16 rows stand side by side, from one on whose slot lies in another block than that in front of it.
+// A block's heads need two steps, the largest value of all its rows and then the codes; values wait for that in registers, and the
+// next heads are on their way.
 constexpr int Q8_UNITS = 4;
-template <int DTYPE, int D, bool HALF>
-__global__ __launch_bounds__(TR_Q8_ROWS * D / Vec<DTYPE>::N) void append_q8_kernel(const TrPagedAppendArgs a, int64_t first)
+template <int DTYPE, int D, bool HALF, int THREADS>
+__device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2* turn, uint32_t (*tops)[Q8_UNITS * THREADS * Vec<DTYPE>::N / D], int64_t t0, int window,
+                                              bool keys)
 {
     using V = Vec<DTYPE>;
-    constexpr int N = V::N, LPH = D / N, UNITS = Q8_UNITS, HEAD = D * 16 / N, THREADS = TR_Q8_ROWS * LPH;
-    constexpr int TURNS = HALF ? N : N / 2;
-    __shared__ float2 turn[TR_Q8_ROWS * 64]; // cosine and sine of each token's pairs, times the amplitude
-    __shared__ uint32_t tops[3][UNITS * TR_Q8_ROWS];
-    const int tid = threadIdx.x, lane = tid & 63, piece = tid % LPH, g = tid / LPH;
-    const int64_t t0 = first + blockIdx.x;
+    constexpr int N = V::N, LPH = D / N, UNITS = Q8_UNITS, HEAD = D * 16 / N, ROWS = THREADS / LPH; // ROWS: heads of tokens at a time
+    constexpr int TURNS = HALF ? N : N / 2, TOPS = UNITS * ROWS;
+    static_assert(ROWS >= TR_Q8_ROWS, "");
+    const int tid = threadIdx.x, lane = tid & 63, piece = tid % LPH, g = tid / LPH, scale_shift = a.pool.page_shift - 4;
 
-    // lane i + 1: the slot of token t0 + i
-    const int64_t mine = t0 - 1 + lane;
-    const int slot = lane <= TR_Q8_ROWS && mine >= 0 && mine < a.n_tokens ? a.slots[mine] : -1;
+    const int64_t mine = t0 - 1 + lane; // lane i + 1: the slot of token t0 + i
+    const int slot = lane < window + TR_Q8_ROWS && mine >= 0 && mine < a.n_tokens ? a.slots[mine] : -1;
     const int block = slot >> 4;
-    const int own = __builtin_amdgcn_readlane(block, 1);
-    const int page = own >> (a.pool.page_shift - 4);
-    if (own < 0 || page >= a.pool.n_pages || __builtin_amdgcn_readlane(block, 0) == own) return;
-    const uint64_t member = __ballot(block == own) >> 1;
-    const int run = min(__builtin_ctzll(~member), TR_Q8_ROWS);
-    const bool in_run = lane >= 1 && lane <= run;
-    const bool anew = __ballot(in_run && (slot & 15) == 0) != 0;
-    const int in_page = own & ((1 << (a.pool.page_shift - 4)) - 1);
+    const int before = __shfl_up(block, 1);
+    uint64_t owners = __ballot(lane >= 1 && lane <= window && block >= 0 && block != before && block >> scale_shift < a.pool.n_pages);
+    if (!owners) return;
 
-    int wide = 0; // log2 of the tokens that are worked on at a time
-    while ((1 << wide) < run) ++wide;
-    const int step = TR_Q8_ROWS >> wide, tok = g / step, h0 = g % step; // heads at a time
-    const bool live = tok < run;
-    const int64_t t = t0 + (live ? tok : 0);
-    const int n_heads = 2 * a.n_kv_heads, pairs = a.rotary_dim / 2, half_units = pairs / N;
-    const bool turns = piece * N < a.rotary_dim, low = piece < half_units, full = a.rotary_dim == D;
+    const int n_heads = a.n_kv_heads, pairs = keys ? a.rotary_dim / 2 : 0, half_units = pairs / N;
+    const bool normed = keys && a.k_norm, turns = keys && piece * N < a.rotary_dim, low = piece < half_units, full = a.rotary_dim == D;
     const int partner = turns ? lane + (low ? half_units : -half_units) : lane;
     const int m0 = HALF ? (low ? piece : piece - half_units) * N : piece * (N / 2);
-    const char* const k = a.k + t * a.k_stride + piece * 16;
-    const char* const v = a.v + t * a.v_stride + piece * 16;
-    const int row = __shfl(slot, tok + 1) & 15;
-    const int64_t block_at = (int64_t)page * a.pool.page_stride + (int64_t)(in_page * TR_Q8_ROWS) * a.pool.row_stride + piece * N;
-    const int scale_shift = a.pool.page_shift - 4;
-
+    const char* const from = keys ? a.k : a.v;
+    const int64_t stride = keys ? a.k_stride : a.v_stride;
+    char* const to_pool = keys ? a.pool.k : a.pool.v;
+    uint8_t* const scales = keys ? a.pool.k_scale : a.pool.v_scale;
     u32x4 kw_raw = {};
-    if (a.k_norm) kw_raw = ((const u32x4*)a.k_norm)[piece];
+    if (normed) kw_raw = ((const u32x4*)a.k_norm)[piece];
     float kw[N];
     V::open(kw_raw, kw);
-    for (int i = tid; i < run * pairs; i += THREADS) {
-        const int at = i / pairs, m = i - at * pairs;
-        double sn, cn;
-        tr_sincos((double)a.pos[t0 + at] * a.freq[m], &sn, &cn);
-        turn[at * 64 + m] = make_float2((float)(cn * a.amplitude), (float)(sn * a.amplitude));
-    }
-    for (int i = tid; i < UNITS * TR_Q8_ROWS; i += THREADS) tops[0][i] = 0;
-    __syncthreads();
-    float2 e[TURNS];
+
+    while (owners) {
+        const int at0 = __builtin_ctzll(owners); // lane of the block's first token
+        owners &= owners - 1;
+        const int own = __builtin_amdgcn_readlane(block, at0), page = own >> scale_shift, in_page = own & ((1 << scale_shift) - 1);
+        const int run = min(__builtin_ctzll(~(__ballot(block == own) >> at0)), TR_Q8_ROWS);
+        const bool anew = __ballot(lane >= at0 && lane < at0 + run && (slot & 15) == 0) != 0;
+        int wide = 0; // log2 of the tokens that are worked on at a time
+        while ((1 << wide) < run) ++wide;
+        const int step = ROWS >> wide, tok = g / step, h0 = g % step; // heads at a time
+        const bool live = tok < run;
+        const int64_t t = t0 + at0 - 1 + (live ? tok : 0);
+        const int row = __shfl(slot, at0 + (live ? tok : 0)) & 15;
+        const char* const heads = from + t * stride + piece * 16;
+        char* const rows = to_pool + (int64_t)page * a.pool.page_stride + (int64_t)(in_page * TR_Q8_ROWS) * a.pool.row_stride + piece * N;
+        uint8_t* const scale = scales + (((int64_t)page * n_heads) << scale_shift) + in_page;
+
+        u32x4 raw[UNITS];
+        int held[UNITS];
+        auto load = [&](int c0) {
 #pragma unroll
-    for (int c = 0; c < TURNS; ++c) {
-        e[c] = turns && live ? turn[tok * 64 + m0 + c] : make_float2(1.0f, 0.0f);
-        if (HALF && low) e[c].y = -e[c].y;
-    }
-    int buf = 0;
-    for (int c0 = 0; c0 < n_heads; c0 += UNITS * step) {
-        float x[UNITS][N];
-        const int next = buf == 2 ? 0 : buf + 1;
-        for (int i = tid; i < UNITS * TR_Q8_ROWS; i += THREADS) tops[next][i] = 0; // nobody reads or adds to it until the barrier
-#pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            const int head = c0 + h0 + i * step, hv = head - a.n_kv_heads;
-            if (!live || head >= n_heads) continue;
-            V::open(*(const u32x4*)(hv < 0 ? k + (int64_t)head * HEAD : v + (int64_t)hv * HEAD), x[i]);
-            if (hv < 0) norm_and_turn<N, LPH, HALF>(x[i], a.k_norm != nullptr, kw, a.eps, e, turns, full, partner);
-            uint32_t top = 0;
-#pragma unroll
-            for (int c = 0; c < N; ++c) {
-                const uint32_t bits = __float_as_uint(x[i][c]) & 0x7fffffffu;
-                top = max(top, bits < 0x7f800000u ? bits : 0u);
+            for (int i = 0; i < UNITS; ++i) {
+                const int head = c0 + h0 + i * step;
+                raw[i] = u32x4{};
+                held[i] = 0;
+                if (!live || head >= n_heads) continue;
+                raw[i] = __builtin_nontemporal_load((const u32x4*)(heads + (int64_t)head * HEAD));
+                if (!anew) held[i] = scale[(int64_t)head << scale_shift];
             }
-            top = lanes_max<LPH>(top);
-            if (piece == 0) atomicMax(&tops[buf][h0 + i * step], top);
+        };
+        load(0);
+        __syncthreads(); // the last block's angles are read
+        for (int i = tid; i < run * pairs; i += THREADS) {
+            const int at = i / pairs, m = i - at * pairs;
+            double sn, cn;
+            tr_sincos((double)a.pos[t0 + at0 - 1 + at] * a.freq[m], &sn, &cn);
+            turn[at * 64 + m] = make_float2((float)(cn * a.amplitude), (float)(sn * a.amplitude));
         }
+        for (int i = tid; i < TOPS; i += THREADS) tops[0][i] = 0;
         __syncthreads();
+        float2 e[TURNS];
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            const int head = c0 + h0 + i * step, hv = head - a.n_kv_heads;
-            if (!live || head >= n_heads) continue;
-            const int hk = hv < 0 ? head : hv;
-            uint8_t* const scale = (hv < 0 ? a.pool.k_scale : a.pool.v_scale) + ((((int64_t)page * a.n_kv_heads + hk) << scale_shift) + in_page);
-            char* const rows = (hv < 0 ? a.pool.k : a.pool.v) + block_at + (int64_t)hk * a.pool.head_stride;
-            const int need = q8_exponent(tops[buf][h0 + i * step]), old = anew ? need : (int)*scale - 127, to = max(need, old);
-            const float by = q8_power(-to);
+        for (int c = 0; c < TURNS; ++c) {
+            e[c] = turns && live ? turn[tok * 64 + m0 + c] : make_float2(1.0f, 0.0f);
+            if (HALF && low) e[c].y = -e[c].y;
+        }
+        int buf = 0;
+        for (int c0 = 0; c0 < n_heads; c0 += UNITS * step) {
+            float x[UNITS][N];
+            int old[UNITS];
+            const int next = buf == 2 ? 0 : buf + 1;
+            for (int i = tid; i < TOPS; i += THREADS) tops[next][i] = 0; // nobody reads or adds to it until the barrier
 #pragma unroll
-            for (int c = 0; c < N; ++c) x[i][c] *= by;
-            if (to >= Q8_MOST) // the largest numbers would round to what fp32 has not
+            for (int i = 0; i < UNITS; ++i) {
+                const int head = c0 + h0 + i * step;
+                old[i] = held[i];
+                if (!live || head >= n_heads) continue;
+                V::open(raw[i], x[i]);
+                if (keys) norm_and_turn<N, LPH, HALF>(x[i], normed, kw, a.eps, e, turns, full, partner);
+                uint32_t top = 0;
 #pragma unroll
                 for (int c = 0; c < N; ++c) {
-                    const float most = 1.875f * q8_power(127 - to);
-                    if (fabsf(x[i][c]) > most && fabsf(x[i][c]) < 256.0f) x[i][c] = copysignf(most, x[i][c]);
+                    const uint32_t bits = __float_as_uint(x[i][c]) & 0x7fffffffu;
+                    top = max(top, bits < 0x7f800000u ? bits : 0u);
                 }
-            uint32_t w[N / 4];
-#pragma unroll
-            for (int c = 0; c < N; c += 4) w[c / 4] = q8_encode(x[i][c], x[i][c + 1], x[i][c + 2], x[i][c + 3]);
-            uint32_t* const at = (uint32_t*)(rows + (int64_t)row * a.pool.row_stride);
-#pragma unroll
-            for (int c = 0; c < N / 4; ++c) at[c] = w[c];
-            if (tok != 0 || to == old) { // a block that starts anew has old = need
-                if (tok == 0 && piece == 0 && anew) *scale = (uint8_t)(to + 127);
-                continue;
+                top = lanes_max<LPH>(top);
+                if (piece == 0) atomicMax(&tops[buf][h0 + i * step], top);
             }
-            // a larger scale: the block's other rows are written again
-            uint32_t written = 0;
-            for (int j = 0; j < run; ++j) written |= 1u << (__builtin_amdgcn_readlane(slot, j + 1) & 15);
-            const float factor = q8_power(old - to);
-            for (int j = 0; j < TR_Q8_ROWS; ++j) {
-                if (written & (1u << j)) continue;
-                uint32_t* const held = (uint32_t*)(rows + (int64_t)j * a.pool.row_stride);
+            if (c0 + UNITS * step < n_heads) load(c0 + UNITS * step);
+            __syncthreads();
 #pragma unroll
-                for (int c = 0; c < N / 4; ++c) {
-                    float y[4];
-                    q8_decode(held[c], y);
-                    held[c] = q8_encode(y[0] * factor, y[1] * factor, y[2] * factor, y[3] * factor);
+            for (int i = 0; i < UNITS; ++i) {
+                const int head = c0 + h0 + i * step;
+                if (!live || head >= n_heads) continue;
+                const int need = q8_exponent(tops[buf][h0 + i * step]), was = anew ? need : old[i] - 127, to = max(need, was);
+                const float by = q8_power(-to);
+#pragma unroll
+                for (int c = 0; c < N; ++c) x[i][c] *= by;
+                if (to >= Q8_MOST) // the largest numbers would round to what fp32 has not
+#pragma unroll
+                    for (int c = 0; c < N; ++c) {
+                        const float most = 1.875f * q8_power(127 - to);
+                        if (fabsf(x[i][c]) > most && fabsf(x[i][c]) < 256.0f) x[i][c] = copysignf(most, x[i][c]);
+                    }
+                char* const unit = rows + (int64_t)head * a.pool.head_stride;
+                put<N>(unit + (int64_t)row * a.pool.row_stride, x[i]);
+                if (tok != 0) continue;
+                if (piece == 0 && (anew || to != was)) scale[(int64_t)head << scale_shift] = (uint8_t)(to + 127);
+                if (to != was) { // a larger scale: the block's other rows are written again.  A block that starts anew has none
+                    uint32_t written = 0;
+                    for (int j = 0; j < run; ++j) written |= 1u << (__builtin_amdgcn_readlane(slot, at0 + j) & 15);
+                    rescale<N>(unit, a.pool.row_stride, ~written, q8_power(was - to));
                 }
             }
-            if (piece == 0) *scale = (uint8_t)(to + 127);
+            buf = next;
         }
-        buf = next;
     }
+}
+
+// Keys and values by separate workgroups, which have half as much to hold, and in front of the queries', as they take longer.
+template <int DTYPE, int D, bool HALF, bool STREAM>
+__global__ __launch_bounds__(append_q8_threads(DTYPE, D)) void append_q8_kernel(const TrPagedAppendArgs a, int64_t first, int window, int n_blocks)
+{
+    constexpr int THREADS = append_q8_threads(DTYPE, D);
+    __shared__ float2 turn[TR_Q8_ROWS * 64]; // cosine and sine of each token's pairs, times the amplitude
+    __shared__ uint32_t tops[3][Q8_UNITS * THREADS * Vec<DTYPE>::N / D];
+    const int block = blockIdx.x;
+    if (block < n_blocks) append_blocks<DTYPE, D, HALF, THREADS>(a, turn, tops, first + (int64_t)(block >> 1) * window, window, !(block & 1));
+    else append_heads<DTYPE, D, HALF, STREAM, THREADS, true>(a, turn, (first >> a.tile_shift) + block - n_blocks);
 }
 
 // Rows of the requests, 16 to a workgroup: a thread looks up where a row is, then each takes 16 codes at a time.
@@ -215,14 +267,21 @@ __global__ __launch_bounds__(256) void read_q8_kernel(const TrPagedReadArgs a, i
 
 } // namespace
 
+// A launch takes a part of the tokens, as it has fewer than 2^32 threads.
 template <int DTYPE, int D> static int launch_append(const TrPagedAppendArgs& a, int layout, hipStream_t s)
 {
-    constexpr int THREADS = TR_Q8_ROWS * D / Vec<DTYPE>::N;
-    const int64_t most = ((int64_t)1 << 31) / THREADS; // a launch has fewer than 2^32 threads
+    constexpr int THREADS = append_q8_threads(DTYPE, D);
+    const int window = a.n_tokens <= TR_Q8_FEW ? 1 : TR_Q8_ROWS, tile = 1 << a.tile_shift;
+    const int64_t most = TR_MAX_BLOCKS_256 / 4; // tokens, a multiple of the window and of the tile; at most that many workgroups of either side
     for (int64_t at = 0; at < a.n_tokens; at += most) {
-        const dim3 blocks((uint32_t)std::min<int64_t>(a.n_tokens - at, most));
-        if (layout == TR_ROPE_HALF) append_q8_kernel<DTYPE, D, true><<<blocks, dim3(THREADS), 0, s>>>(a, at);
-        else append_q8_kernel<DTYPE, D, false><<<blocks, dim3(THREADS), 0, s>>>(a, at);
+        const int64_t rest = std::min<int64_t>(a.n_tokens - at, most);
+        const int n_blocks = a.k ? 2 * (int)((rest + window - 1) / window) : 0, n_queries = a.q ? (int)((rest + tile - 1) / tile) : 0;
+        const dim3 grid(n_blocks + n_queries), block(THREADS);
+        const bool half = layout == TR_ROPE_HALF;
+        if (half && a.stream) append_q8_kernel<DTYPE, D, true, true><<<grid, block, 0, s>>>(a, at, window, n_blocks);
+        else if (half) append_q8_kernel<DTYPE, D, true, false><<<grid, block, 0, s>>>(a, at, window, n_blocks);
+        else if (a.stream) append_q8_kernel<DTYPE, D, false, true><<<grid, block, 0, s>>>(a, at, window, n_blocks);
+        else append_q8_kernel<DTYPE, D, false, false><<<grid, block, 0, s>>>(a, at, window, n_blocks);
         TR_HIP(hipGetLastError());
     }
     return TR_OK;
