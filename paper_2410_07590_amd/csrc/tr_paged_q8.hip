@@ -8,14 +8,14 @@
 namespace {
 
 // Largest of the lanes that share a head.
-template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t x)
+template <int LANES> __device__ __forceinline__ int lanes_max(int x)
 {
-    auto with = [&](int y) { x = max(x, (uint32_t)y); };
-    with(__builtin_amdgcn_update_dpp((int)x, (int)x, 0xB1, 0xf, 0xf, false));                    // quad_perm [1,0,3,2]
-    with(__builtin_amdgcn_update_dpp((int)x, (int)x, 0x4E, 0xf, 0xf, false));                    // quad_perm [2,3,0,1]
-    with(__builtin_amdgcn_update_dpp((int)x, (int)x, 0x141, 0xf, 0xf, false));                   // row_half_mirror
-    if (LANES >= 16) with(__builtin_amdgcn_update_dpp((int)x, (int)x, 0x140, 0xf, 0xf, false));  // row_mirror
-    if (LANES == 32) with(__shfl_xor((int)x, 16));
+    auto with = [&](int y) { x = max(x, y); };
+    with(__builtin_amdgcn_update_dpp(x, x, 0xB1, 0xf, 0xf, false));                    // quad_perm [1,0,3,2]
+    with(__builtin_amdgcn_update_dpp(x, x, 0x4E, 0xf, 0xf, false));                    // quad_perm [2,3,0,1]
+    with(__builtin_amdgcn_update_dpp(x, x, 0x141, 0xf, 0xf, false));                   // row_half_mirror
+    if (LANES >= 16) with(__builtin_amdgcn_update_dpp(x, x, 0x140, 0xf, 0xf, false));  // row_mirror
+    if (LANES == 32) with(__shfl_xor(x, 16));
     return x;
 }
 
@@ -29,43 +29,19 @@ template <int N> __device__ __forceinline__ void put(char* to, const float (&x)[
     else *(uint32_t*)to = q8_encode(x[0], x[1], x[2], x[3]);
 }
 
-// The rows of `which` of a block, a unit of N channels each, at another scale.
-template <int N> __device__ __forceinline__ void rescale(char* unit, uint32_t row_stride, uint32_t which, float by)
-{
-    constexpr int AT_ONCE = 8;
-#pragma unroll
-    for (int j0 = 0; j0 < TR_Q8_ROWS; j0 += AT_ONCE) {
-        uint32_t w[AT_ONCE][N / 4];
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j)
-#pragma unroll
-            for (int c = 0; c < N / 4; ++c) w[j][c] = which & (1u << (j0 + j)) ? ((const uint32_t*)(unit + (int64_t)(j0 + j) * row_stride))[c] : 0u;
-#pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-            float y[N];
-#pragma unroll
-            for (int c = 0; c < N; c += 4) {
-                float z[4];
-                q8_decode(w[j][c / 4], z);
-#pragma unroll
-                for (int b = 0; b < 4; ++b) y[c + b] = z[b] * by;
-            }
-            if (which & (1u << (j0 + j))) put<N>(unit + (int64_t)(j0 + j) * row_stride, y);
-        }
-    }
-}
-
 // Quantised heads.  A workgroup looks at `window` tokens and owns the blocks whose first tokens are among them, of keys or of values: the
 // tokens that the call writes to a block of 16 rows stand side by side, from one on whose slot lies in another block than that in front of it.
 // A block's heads need two steps, the largest value of all its rows and then the codes; values wait for that in registers, and the
 // next heads are on their way.
-constexpr int Q8_UNITS = 4;
+constexpr int append_q8_units(int dtype) { return dtype == TR_F32 ? 4 : 2; } // heads that a thread has part in at a time, 16 channels
+// The largest values of a step's heads, and the exponents that they had; what one step reads the next but one clears.
+template <int DTYPE, int D> using Tops = int[append_q8_units(DTYPE) * append_q8_threads(DTYPE, D) * Vec<DTYPE>::N / D];
 template <int DTYPE, int D, bool HALF, int THREADS>
-__device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2* turn, uint32_t (*tops)[Q8_UNITS * THREADS * Vec<DTYPE>::N / D], int64_t t0, int window,
+__device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2* turn, Tops<DTYPE, D>* tops, Tops<DTYPE, D>* olds, int64_t t0, int window,
                                               bool keys)
 {
     using V = Vec<DTYPE>;
-    constexpr int N = V::N, LPH = D / N, UNITS = Q8_UNITS, HEAD = D * 16 / N, ROWS = THREADS / LPH; // ROWS: heads of tokens at a time
+    constexpr int N = V::N, LPH = D / N, UNITS = append_q8_units(DTYPE), HEAD = D * 16 / N, ROWS = THREADS / LPH; // ROWS: heads of tokens at a time
     constexpr int TURNS = HALF ? N : N / 2, TOPS = UNITS * ROWS;
     static_assert(ROWS >= TR_Q8_ROWS, "");
     const int tid = threadIdx.x, lane = tid & 63, piece = tid % LPH, g = tid / LPH, scale_shift = a.pool.page_shift - 4;
@@ -95,7 +71,9 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
         owners &= owners - 1;
         const int own = __builtin_amdgcn_readlane(block, at0), page = own >> scale_shift, in_page = own & ((1 << scale_shift) - 1);
         const int run = min(__builtin_ctzll(~(__ballot(block == own) >> at0)), TR_Q8_ROWS);
-        const bool anew = __ballot(lane >= at0 && lane < at0 + run && (slot & 15) == 0) != 0;
+        uint32_t written = ROWS > TR_Q8_ROWS ? ~0xffffu : 0u; // rows of the block
+        for (int j = 0; j < run; ++j) written |= 1u << (__builtin_amdgcn_readlane(slot, at0 + j) & 15);
+        const bool anew = written & 1;
         int wide = 0; // log2 of the tokens that are worked on at a time
         while ((1 << wide) < run) ++wide;
         const int step = ROWS >> wide, tok = g / step, h0 = g % step; // heads at a time
@@ -148,14 +126,15 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
                 if (!live || head >= n_heads) continue;
                 V::open(raw[i], x[i]);
                 if (keys) norm_and_turn<N, LPH, HALF>(x[i], normed, kw, a.eps, e, turns, full, partner);
-                uint32_t top = 0;
+                int top = 0;
 #pragma unroll
                 for (int c = 0; c < N; ++c) {
-                    const uint32_t bits = __float_as_uint(x[i][c]) & 0x7fffffffu;
-                    top = max(top, bits < 0x7f800000u ? bits : 0u);
+                    const int bits = __float_as_int(x[i][c]) & 0x7fffffff;
+                    top = max(top, bits < 0x7f800000 ? bits : 0);
                 }
                 top = lanes_max<LPH>(top);
                 if (piece == 0) atomicMax(&tops[buf][h0 + i * step], top);
+                if (piece == 0 && tok == 0) olds[buf][h0 + i * step] = (int)old[i] - 127;
             }
             if (c0 + UNITS * step < n_heads) load(c0 + UNITS * step);
             __syncthreads();
@@ -173,14 +152,26 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
                         const float most = 1.875f * q8_power(127 - to);
                         if (fabsf(x[i][c]) > most && fabsf(x[i][c]) < 256.0f) x[i][c] = copysignf(most, x[i][c]);
                     }
-                char* const unit = rows + (int64_t)head * a.pool.head_stride;
-                put<N>(unit + (int64_t)row * a.pool.row_stride, x[i]);
-                if (tok != 0) continue;
-                if (piece == 0 && (anew || to != was)) scale[(int64_t)head << scale_shift] = (uint8_t)(to + 127);
-                if (to != was) { // a larger scale: the block's other rows are written again.  A block that starts anew has none
-                    uint32_t written = 0;
-                    for (int j = 0; j < run; ++j) written |= 1u << (__builtin_amdgcn_readlane(slot, at0 + j) & 15);
-                    rescale<N>(unit, a.pool.row_stride, ~written, q8_power(was - to));
+                put<N>(rows + (int64_t)head * a.pool.head_stride + (int64_t)row * a.pool.row_stride, x[i]);
+                if ((anew || to != was) && tok == 0 && piece == 0) scale[(int64_t)head << scale_shift] = (uint8_t)(to + 127);
+            }
+            if (!anew) { // where a scale has grown, the block's other rows are written again, a row to the lanes of a head
+                const int here = min(UNITS * step, n_heads - c0);
+                char* const other = rows + (int64_t)g * a.pool.row_stride;
+                for (int i = 0; i < here; ++i) {
+                    const int was = olds[buf][i], to = max(q8_exponent(tops[buf][i]), was);
+                    if (to == was || (written >> g) & 1) continue;
+                    uint32_t* const unit = (uint32_t*)(other + (int64_t)(c0 + i) * a.pool.head_stride);
+                    const float by = q8_power(was - to);
+                    float y[N];
+#pragma unroll
+                    for (int c = 0; c < N; c += 4) {
+                        float z[4];
+                        q8_decode(unit[c / 4], z);
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) y[c + b] = z[b] * by;
+                    }
+                    put<N>((char*)unit, y);
                 }
             }
             buf = next;
@@ -190,13 +181,13 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
 
 // Keys and values by separate workgroups, which have half as much to hold, and in front of the queries', as they take longer.
 template <int DTYPE, int D, bool HALF, bool STREAM>
-__global__ __launch_bounds__(append_q8_threads(DTYPE, D)) void append_q8_kernel(const TrPagedAppendArgs a, int64_t first, int window, int n_blocks)
+__global__ __launch_bounds__(append_q8_threads(DTYPE, D), DTYPE == TR_BF16 ? 4 : 2) void append_q8_kernel(const TrPagedAppendArgs a, int64_t first, int window, int n_blocks)
 {
     constexpr int THREADS = append_q8_threads(DTYPE, D);
     __shared__ float2 turn[TR_Q8_ROWS * 64]; // cosine and sine of each token's pairs, times the amplitude
-    __shared__ uint32_t tops[3][Q8_UNITS * THREADS * Vec<DTYPE>::N / D];
+    __shared__ Tops<DTYPE, D> tops[3], olds[3];
     const int block = blockIdx.x;
-    if (block < n_blocks) append_blocks<DTYPE, D, HALF, THREADS>(a, turn, tops, first + (int64_t)(block >> 1) * window, window, !(block & 1));
+    if (block < n_blocks) append_blocks<DTYPE, D, HALF, THREADS>(a, turn, tops, olds, first + (int64_t)(block >> 1) * window, window, !(block & 1));
     else append_heads<DTYPE, D, HALF, STREAM, THREADS, true>(a, turn, (first >> a.tile_shift) + block - n_blocks);
 }
 

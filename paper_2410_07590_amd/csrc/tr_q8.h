@@ -7,9 +7,9 @@ namespace {
 constexpr int Q8_LEAST = -117, Q8_MOST = 120; // exponents of scales: 2^-9 2^-117 is normal, 448 2^120 is beyond the largest fp32 number
 
 // The smallest e with top <= 448 * 2^e = 1.75 * 2^(e + 8), for the bits of a finite top >= 0.
-__device__ __forceinline__ int q8_exponent(uint32_t top)
+__device__ __forceinline__ int q8_exponent(int top)
 {
-    const int e = (int)(top >> 23) - (127 + 8) + ((top & 0x7fffffu) > 0x600000u);
+    const int e = (top >> 23) - (127 + 8) + ((top & 0x7fffff) > 0x600000);
     return min(max(e, Q8_LEAST), Q8_MOST);
 }
 __device__ __forceinline__ float q8_power(int e) { return __builtin_amdgcn_ldexpf(1.0f, e); }
