@@ -462,6 +462,7 @@ struct TrPagedReadArgs {
     char* out_k;
     char* out_v;
     int32_t n_req, max_blocks, n_rows, n_kv_heads;
+    int32_t rows; // of a wave
 };
 int tr_launch_page_map(const TrPageMapArgs& a, hipStream_t s);
 int tr_launch_paged_append(const TrPagedAppendArgs& a, int dtype, int head_dim, int layout, hipStream_t s);

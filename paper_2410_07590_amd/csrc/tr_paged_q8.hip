@@ -191,66 +191,140 @@ __global__ __launch_bounds__(append_q8_threads(DTYPE, D), DTYPE == TR_BF16 ? 4 :
     else append_heads<DTYPE, D, HALF, STREAM, THREADS, true>(a, turn, (first >> a.tile_shift) + block - n_blocks);
 }
 
-// Rows of the requests, 16 to a workgroup: a thread looks up where a row is, then each takes 16 codes at a time.
-constexpr int READ_ROWS = 16;
-template <int DTYPE, int D>
+// Largest i of 64 lanes with starts <= x, for ascending starts; -1 if there is none.
+__device__ __forceinline__ int lane_not_above(int starts, int x)
+{
+    int n = 0; // lanes below n are known to be
+#pragma unroll
+    for (int s = 32; s; s >>= 1)
+        if (__shfl(starts, n + s - 1) <= x) n += s;
+    if (n == 63 && __shfl(starts, 63) <= x) n = 64;
+    return n - 1;
+}
+
+__device__ __forceinline__ int64_t lane_of(int64_t x, int lane)
+{
+    return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
+}
+
+// Rows of the requests.  Bound by memory, and by a chain of trips to it before the first code is asked for: the requests' first rows, a
+// length and a page id, codes and scales.  A wave takes `rows` rows, a lane looks up one of them, and then each lane makes 16 bytes of
+// result at a time of READ_UNITS units of keys and as many of values.
+constexpr int READ_UNITS = 4;
+template <int DTYPE, int D, bool STREAM>
 __global__ __launch_bounds__(256) void read_q8_kernel(const TrPagedReadArgs a, int64_t first)
 {
-    __shared__ int64_t from[READ_ROWS], scale_from[READ_ROWS]; // bytes; -1: no page, -2: no such row
-    const int tid = threadIdx.x, shift = a.pool.page_shift;
-    const int64_t t0 = first + (int64_t)blockIdx.x * READ_ROWS;
-    if (tid < READ_ROWS) {
-        const int64_t t = t0 + tid;
-        int lo = 0, hi = a.n_req; // the last request that begins at or before t
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (a.row_start[mid] <= t) lo = mid; else hi = mid;
-        }
-        const int64_t j = t - a.row_start[lo];
-        int64_t f = -2, s = 0;
-        if (t < a.n_rows && j >= 0 && j < a.kv_lens[lo] && t < a.row_start[lo + 1] && j < (int64_t)a.max_blocks << shift) {
-            const int page = a.table[(int64_t)lo * a.max_blocks + (j >> shift)], row = (int)j & ((1 << shift) - 1);
-            f = -1;
-            if ((uint32_t)page < (uint32_t)a.pool.n_pages) {
-                f = (int64_t)page * a.pool.page_stride + (int64_t)row * a.pool.row_stride;
-                s = (((int64_t)page * a.n_kv_heads) << (shift - 4)) + (row >> 4);
-            }
-        }
-        from[tid] = f;
-        scale_from[tid] = s;
+    using V = Vec<DTYPE>;
+    constexpr int N = V::N, PER_HEAD = D / N;
+    const int lane = threadIdx.x & 63, shift = a.pool.page_shift, scale_shift = shift - 4;
+    const int64_t t0 = first + ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * a.rows;
+    if (t0 >= a.n_rows) return;
+
+    // lane i: the first row of request base + i, none of those in front of which begins behind t0
+    int base = 0, n = a.n_req + 1;
+    while (n > 64) {
+        const int step = (n + 63) >> 6, at = base + min(lane * step, n - 1);
+        const uint64_t below = __ballot(a.row_start[at] <= t0);
+        const int i = max(__builtin_popcountll(below) - 1, 0); // starts ascend
+        base += min(i * step, n - 1);
+        n = min(step, n - min(i * step, n - 1));
     }
-    __syncthreads();
-    const int per_row = a.n_kv_heads * (D / 16);
-    constexpr int OUT = DTYPE == TR_BF16 ? 2 : 4; // 16-byte units of 16 results
-    for (int64_t i = tid; i < (int64_t)READ_ROWS * per_row; i += 256) {
-        const int r = (int)(i / per_row), u = (int)(i - (int64_t)r * per_row), head = u / (D / 16), piece = u % (D / 16);
-        const int64_t f = from[r];
-        if (f == -2) continue;
-#pragma unroll
-        for (int side = 0; side < 2; ++side) {
-            u32x4 w = {0, 0, 0, 0};
-            int s = 127;
-            if (f >= 0) {
-                w = *(const u32x4*)((side ? a.pool.v : a.pool.k) + f + (int64_t)head * a.pool.head_stride + piece * 16);
-                s = (side ? a.pool.v_scale : a.pool.k_scale)[scale_from[r] + ((int64_t)head << (shift - 4))];
+    n = a.n_req + 1 - base; // the requests behind are of interest, too
+    const int start = lane < n ? a.row_start[base + lane] : INT32_MAX;
+    int64_t from = -2; // bytes; -1: no page, -2: no such row
+    int64_t scale = 0;
+    {
+        const int64_t t = t0 + lane;
+        const int last = (int)min(t0 + a.rows - 1, (int64_t)INT32_MAX - 1);
+        int i = __builtin_popcountll(__ballot(start <= (int)t0)) - 1, begin, end;
+        if (i == __builtin_popcountll(__ballot(start <= last)) - 1) { // all rows are of one request
+            begin = __builtin_amdgcn_readlane(start, max(i, 0));
+            end = __builtin_amdgcn_readlane(start, min(i + 1, 63));
+        } else {
+            i = lane_not_above(start, (int)min(t, (int64_t)last));
+            begin = __shfl(start, max(i, 0));
+            end = __shfl(start, min(i + 1, 63));
+        }
+        int r = base + max(i, 0);
+        if (i == 63 && lane < a.rows) { // more than 63 requests begin in these rows
+            int lo = r, hi = a.n_req;
+            while (hi - lo > 1) {
+                const int mid = lo + ((hi - lo) >> 1);
+                if (a.row_start[mid] <= t) lo = mid; else hi = mid;
             }
-            const float by = q8_power(s - 127);
-            u32x4* const to = (u32x4*)((side ? a.out_v : a.out_k) + ((t0 + r) * per_row + u) * (OUT * 16));
-            float x[16];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                float y[4];
-                q8_decode(w[c], y);
-#pragma unroll
-                for (int b = 0; b < 4; ++b) x[4 * c + b] = y[b] * by;
+            r = min(lo, a.n_req - 1);
+            begin = a.row_start[r];
+            end = a.row_start[r + 1];
+        }
+        const int64_t j = t - begin;
+        if (lane < a.rows && t < a.n_rows && i >= 0 && r < a.n_req && j >= 0 && t < end && j < (int64_t)a.max_blocks << shift) {
+            const int page = a.table[(int64_t)r * a.max_blocks + (j >> shift)], row = (int)j & ((1 << shift) - 1);
+            if (j < a.kv_lens[r]) {
+                from = -1;
+                if ((uint32_t)page < (uint32_t)a.pool.n_pages) {
+                    from = (int64_t)page * a.pool.page_stride + (int64_t)row * a.pool.row_stride;
+                    scale = (((int64_t)page * a.n_kv_heads) << scale_shift) + (row >> 4);
+                }
             }
-            constexpr int N = Vec<DTYPE>::N;
+        }
+    }
+    const int per_row = a.n_kv_heads * PER_HEAD, units = (int)min((int64_t)a.rows, a.n_rows - t0) * per_row; // below 2^31 as heads are at most 2^20
+    const uint64_t unit0 = (uint64_t)t0 * per_row;
+    const bool even = per_row % 64 == 0; // then a wave's units are of one row
+    int r = 0, in = 0;                    // that row and its first unit
+    for (int u0 = lane; u0 - lane < units; u0 += 64 * READ_UNITS) {
+        uint32_t w[2][READ_UNITS][N / 4];
+        int s[2][READ_UNITS];
+        bool mine[READ_UNITS];
 #pragma unroll
-            for (int c = 0; c < OUT; ++c) {
-                float y[N];
+        for (int i = 0; i < READ_UNITS; ++i) {
+            const int u = u0 + 64 * i;
+            int at_head;
+            int64_t at, sc;
+            if (even) {
+                at = lane_of(from, r), sc = lane_of(scale, r);
+                at_head = in + lane;
+                in += 64;
+                if (in == per_row) in = 0, ++r;
+            } else {
+                const int row = (uint32_t)u / (uint32_t)per_row;
+                at = __shfl(from, row & 63), sc = __shfl(scale, row & 63);
+                at_head = u - row * per_row;
+            }
+            const int head = at_head / PER_HEAD;
+            mine[i] = u < units && at != -2;
 #pragma unroll
-                for (int b = 0; b < N; ++b) y[b] = x[N * c + b];
-                to[c] = Vec<DTYPE>::close(y);
+            for (int side = 0; side < 2; ++side) {
+                s[side][i] = 127;
+#pragma unroll
+                for (int c = 0; c < N / 4; ++c) w[side][i][c] = 0;
+                if (u < units && at >= 0) {
+                    const char* const codes = (side ? a.pool.v : a.pool.k) + at + (int64_t)head * a.pool.head_stride + (at_head % PER_HEAD) * N;
+                    if constexpr (N == 8) {
+                        const uint64_t x = __builtin_nontemporal_load((const uint64_t*)codes);
+                        w[side][i][0] = (uint32_t)x, w[side][i][N / 4 - 1] = (uint32_t)(x >> 32);
+                    } else w[side][i][0] = __builtin_nontemporal_load((const uint32_t*)codes);
+                    s[side][i] = (side ? a.pool.v_scale : a.pool.k_scale)[sc + ((int64_t)head << scale_shift)];
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < READ_UNITS; ++i) {
+            if (!mine[i]) continue;
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+                const float by = q8_power(s[side][i] - 127);
+                float x[N];
+#pragma unroll
+                for (int c = 0; c < N; c += 4) {
+                    float y[4];
+                    q8_decode(w[side][i][c / 4], y);
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) x[c + b] = y[b] * by;
+                }
+                u32x4* const to = (u32x4*)((side ? a.out_v : a.out_k) + (unit0 + u0 + 64 * i) * 16);
+                if (STREAM) __builtin_nontemporal_store(V::close(x), to);
+                else *to = V::close(x);
             }
         }
     }
@@ -283,12 +357,16 @@ int tr_launch_paged_append_q8(const TrPagedAppendArgs& a, int dtype, int head_di
     return head_dim == 128 ? launch_append<TR_F32, 128>(a, layout, s) : launch_append<TR_F32, 64>(a, layout, s);
 }
 
-template <int DTYPE, int D> static int launch_read(const TrPagedReadArgs& a, hipStream_t s)
+template <int DTYPE, int D> static int launch_read(TrPagedReadArgs a, hipStream_t s)
 {
-    const int64_t most = (int64_t)TR_MAX_BLOCKS_256 * READ_ROWS;
+    const int per_row = a.n_kv_heads * (D / Vec<DTYPE>::N);
+    a.rows = std::min(std::max(64 * READ_UNITS / per_row, 1), 64);
+    const int64_t most = (int64_t)TR_MAX_BLOCKS_256 * 4 * a.rows;
+    const bool stream = 2 * 16ll * per_row * a.n_rows >= 150ll << 20;
     for (int64_t at = 0; at < a.n_rows; at += most) {
-        const dim3 blocks((uint32_t)((std::min<int64_t>(a.n_rows - at, most) + READ_ROWS - 1) / READ_ROWS));
-        read_q8_kernel<DTYPE, D><<<blocks, dim3(256), 0, s>>>(a, at);
+        const dim3 blocks((uint32_t)((std::min<int64_t>(a.n_rows - at, most) + 4 * a.rows - 1) / (4 * a.rows)));
+        if (stream) read_q8_kernel<DTYPE, D, true><<<blocks, dim3(256), 0, s>>>(a, at);
+        else read_q8_kernel<DTYPE, D, false><<<blocks, dim3(256), 0, s>>>(a, at);
         TR_HIP(hipGetLastError());
     }
     return TR_OK;
