@@ -411,8 +411,9 @@ struct TrPool {
 };
 #define TR_Q8_ROWS 16 // that share a scale
 #define TR_Q8_FEW 4096 // tokens of an append that get a workgroup each, to look whether they begin a block
-#define TR_Q8_UNIT 32 // keys that a wave of the decode over 8 bits takes at a time
-__host__ __device__ constexpr int tr_q8_workers(int dtype, int group) { return dtype == TR_F32 && group > 16 ? 1024 : 2048; } // waves; rings of 20 KB, or 40
+// Waves of a decode over codes.  A wave has a unit's keys and values on their way, half as many bytes where heads have 64 channels.
+__host__ __device__ constexpr int tr_q8_workers(int head_dim) { return head_dim == 64 ? 2048 : 1024; }
+#define TR_Q8_UNIT 64 // keys that a wave of the decode over 8 bits takes at a time
 #define TR_PAGED_APPEND_TOKENS 8 // at most, of a workgroup
 struct TrPagedAppendArgs {
     const char* q;

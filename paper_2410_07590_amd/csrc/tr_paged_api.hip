@@ -449,10 +449,7 @@ int decode_args(const char* who, const tr_shape* shape, const void* q, const POO
     return TR_OK;
 }
 DecodeForm plain_form(const tr_shape* shape) { return {shape && shape->dtype == TR_BF16 ? tr_paged_unit_keys(TR_BF16) : tr_paged_unit_keys(TR_F32), TR_PAGED_WORKERS, 8}; }
-DecodeForm q8_form(const tr_shape* shape) // a shape that is none has no query heads to a group yet
-{
-    return {TR_Q8_UNIT, shape && shape->n_kv_heads > 0 ? tr_q8_workers(shape->dtype, shape->n_q_heads / shape->n_kv_heads) : 0, TR_Q8_ROWS};
-}
+DecodeForm q8_form(const tr_shape* shape) { return {TR_Q8_UNIT, tr_q8_workers(shape ? shape->head_dim : 0), TR_Q8_ROWS}; }
 } // namespace
 
 extern "C" size_t tr_paged_decode_attn_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size)

@@ -47,16 +47,26 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 #define CONST_AS __attribute__((address_space(4)))
 
 constexpr float NOTHING = -__FLT_MAX__; // reference of a row that has seen no key
-constexpr int DMA_STREAM = 2;           // non-temporal: every key is read once
+// Non-temporal: every key is read once.  Where a row is half a line and the other half another head's, the waves of both heads want the
+// line, and it stays in the L2 for the second.  us, codes of 64 channels, 64 requests of 4000 rows of 16 / 4 heads, non-temporal / not: heads side by
+// side 52.7 / 38.6 (114 or 65 thousand KB are fetched), rows side by side 33.5 / 36.5; heads of 128 channels 98.0 / 110.0.
+constexpr int DMA_STREAM = 2;
 // What a pool holds: a tr_dtype, which is the type of queries and results too, or codes with scales, the latter's type being FMT & 1.
 enum { FMT_F32 = TR_F32, FMT_BF16 = TR_BF16, FMT_Q8_F32 = 2 | TR_F32, FMT_Q8_BF16 = 2 | TR_BF16 };
 // Loads of 1 KB that a wave has on their way.  us with 5 / 6 / 7 / 8: 64 x 4096 rows 95.5 / 92.6 / 91.7 / 96.2, one request of 131071 95.4 /
 // 92.2 / 91.3 / 94.3, windows over 32 requests 89.1 / 86.0 / 85.5 / 90.4, 200 requests of 50 to 1200 99.1 / 96.9 / 96.2 / 98.2.
 constexpr int FLIGHT = 7;
+// Codes: 64 requests of 8192 rows, 28 / 4 heads, with 7 / 8 / 9 / 10 / 12 / 16: 106.8 / 97.3 / 97.3 / 98.4 / 99.9 / 102.7; one of 131071 59.1 / 55.2 / 56.0 / 55.7 /
+// 59.3 / 56.9; windows over 32 requests 58.0 / 52.3 / 53.0 / 53.2 / 52.4 / 53.3.
+constexpr int FLIGHT_Q8 = 8;
 
-__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+// A bit for each key of a unit.
+template <int UNIT> using Mask = typename std::conditional<UNIT == 64, uint64_t, uint32_t>::type;
+template <class M> __device__ __forceinline__ M low_bits(int n) { return n >= 8 * (int)sizeof(M) ? ~(M)0 : n <= 0 ? (M)0 : ((M)1 << n) - 1; }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)uniform((int)x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) { return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x); }
 
 // Inclusive sums over the wave, on the vector unit's cross-lane path: within rows of 16 lanes, then across them.
 __device__ __forceinline__ int wave_scan(int x)
@@ -74,9 +84,10 @@ __device__ __forceinline__ int wave_scan(int x)
 template <int UNIT> struct Walk {
     int len, lo, sink, su, lu, units; // at least one unit, which writes the result
     __device__ __forceinline__ int unit(int i) const { return i < su ? i : i - su + lu; }
-    __device__ __forceinline__ uint32_t seen(int first_key) const // bit b: key first_key + b is visible
+    __device__ __forceinline__ Mask<UNIT> seen(int first_key) const // bit b: key first_key + b is visible
     {
-        return low_bits(UNIT) & low_bits(len - first_key) & (low_bits(sink - first_key) | ~low_bits(lo - first_key));
+        typedef Mask<UNIT> M;
+        return low_bits<M>(UNIT) & low_bits<M>(len - first_key) & (low_bits<M>(sink - first_key) | ~low_bits<M>(lo - first_key));
     }
 };
 template <int UNIT> __device__ __forceinline__ Walk<UNIT> walk_of(const TrPagedDecodeArgs& a, int kv_len)
@@ -103,11 +114,11 @@ template <bool MAX> __device__ __forceinline__ float column_reduce(float x) // o
 }
 
 // Two weights as three pairs of bf16 that add up to them, by cutting off 8 bits at a time.  Each rest gets 2^-30 of its weight besides, which no
-// sum in fp32 notices, so that no part is zero: infinite values times zero would be NaN.
+// sum in fp32 notices, so that no part is zero: infinite values times zero would be NaN.  Codes have no infinity.
 struct Split {
     uint32_t pair[3];
 };
-__device__ __forceinline__ Split split(float x, float y)
+template <bool INFINITE> __device__ __forceinline__ Split split(float x, float y)
 {
     auto upper = [](float f) { return __uint_as_float(__float_as_uint(f) & 0xffff0000u); };
     auto both = [](float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); };
@@ -116,15 +127,15 @@ __device__ __forceinline__ Split split(float x, float y)
     s.pair[0] = both(x, y);
 #pragma unroll
     for (int j = 1; j < 3; ++j) {
-        x = fmaf(wx, 0x1p-30f, x - upper(x));
-        y = fmaf(wy, 0x1p-30f, y - upper(y));
+        x = INFINITE ? fmaf(wx, 0x1p-30f, x - upper(x)) : x - upper(x);
+        y = INFINITE ? fmaf(wy, 0x1p-30f, y - upper(y)) : y - upper(y);
         s.pair[j] = both(x, y);
     }
     return s;
 }
 
 // A unit is 8 KB of K and 8 KB of V for heads of 128 channels (half of that for 64): 32 rows of bf16 or 16 of fp32; 32 rows of codes are
-// half as much.
+// half as much, and a unit of them 64.
 // Where a wave's loads of it go: load i fills rows RPI i .. of the unit, lane after lane.  K: 16-byte chunk c of row r sits at
 // c ^ ksw(r), so that the reads of operands spread over all banks; V: bf16 32-byte group g of row r at g ^ vsw(r), codes 16-byte group
 // likewise, for the same reason, fp32 as it comes.
@@ -135,7 +146,8 @@ template <int FMT, int D> struct Rows {
     static constexpr int IDS = Q8 ? 768 : 256;                                         // bytes of page ids, and scales
     static constexpr int QROW = D * (IO == TR_BF16 ? 2 : 4), QCPR = QROW / 16, QPI = 64 / QCPR; // a query row, its chunks, rows of a load
     static constexpr int KS = D * (BF16 ? 2 : 4) / 64, QPARTS = FMT == FMT_Q8_F32 ? 3 : 1;      // steps of a product, bf16 parts of a query
-    static constexpr int FLIGHT_ = FLIGHT < 2 * LPU ? FLIGHT : 2 * LPU;
+    static constexpr bool HALF_LINES = ROW < 128;
+    static constexpr int MOST = Q8 ? FLIGHT_Q8 : FLIGHT;
     __device__ static __forceinline__ int ksw(int r) { return CPR >= 16 ? r & 15 : (r / (16 / CPR)) & (CPR - 1); }
     __device__ static __forceinline__ int vsw(int r)
     {
@@ -169,10 +181,10 @@ __device__ __forceinline__ bf16x8 worth(uint32_t x, float x_by, uint32_t y, floa
 
 // One unit of a wave: where its KV head begins, its first key, which of its keys are seen, and where its page ids are among the
 // wave's.
-struct UnitRef {
+template <int UNIT> struct UnitRef {
     uint64_t head;
     int key0, at;
-    uint32_t seen;
+    Mask<UNIT> seen;
 };
 
 // A run of units of one item that one wave walks.
@@ -195,12 +207,15 @@ template <int FMT, int D> struct Stream {
     using R = Rows<FMT, D>;
     using P = Piece<R::UNIT>;
     typedef typename Operand<FMT>::T Op;
-    static constexpr int LPU = R::LPU, UNIT = R::UNIT, UNIT_SHIFT = UNIT == 32 ? 5 : 4;
+    static constexpr int LPU = R::LPU, UNIT = R::UNIT, UNIT_SHIFT = UNIT == 64 ? 6 : UNIT == 32 ? 5 : 4;
+    typedef UnitRef<UNIT> Ref;
+    typedef Mask<UNIT> M;
     static constexpr bool Q8 = R::Q8;
     uint32_t kring, vring, idring, qring, row_bytes, page_bytes;
     int lane, page_shift, sub_shift, per_unit_shift, n_pages; // sub_shift: rows of a unit that have an id (codes: and a scale) of their own
     int32_t max_blocks;
     uint32_t head_stride;
+    bool shared; // two heads' rows lie in one line
     uint32_t dk[LPU], dv[LPU]; // what a lane adds to the start of a unit's page for load i
 
     __device__ __forceinline__ Stream(const TrPagedDecodeArgs& a, uint32_t ring, int lane_) : lane(lane_)
@@ -212,6 +227,7 @@ template <int FMT, int D> struct Stream {
         row_bytes = a.pool.row_stride;
         page_bytes = a.pool.page_stride;
         head_stride = a.pool.head_stride;
+        shared = a.n_kv_heads > 1 && head_stride < 128;
         page_shift = a.pool.page_shift;
         n_pages = a.pool.n_pages;
         max_blocks = a.max_blocks;
@@ -315,33 +331,35 @@ template <int FMT, int D> struct Stream {
                 }
             }
     }
-    __device__ __forceinline__ UnitRef ref(const P& p, int j, int ids) const
+    __device__ __forceinline__ Ref ref(const P& p, int j, int ids) const
     {
-        UnitRef u;
+        Ref u;
         u.head = (uint64_t)(uint32_t)p.kvh * head_stride;
         u.key0 = uniform(p.w.unit(p.u0 + j) * UNIT);
         u.at = (j & (refill() - 1)) << per_unit_shift;
         u.seen = p.w.seen(u.key0);
-        uint32_t holes = (uint32_t)(__ballot(ids < 0) >> u.at) & low_bits(1 << per_unit_shift);
+        uint32_t holes = (uint32_t)(__ballot(ids < 0) >> u.at) & low_bits<uint32_t>(1 << per_unit_shift);
         while (holes) { // pages that are none
             const int s = __builtin_ctz(holes);
             holes &= holes - 1;
-            u.seen &= ~(low_bits(1 << sub_shift) << (s << sub_shift));
+            u.seen &= ~(low_bits<M>(1 << sub_shift) << (s << sub_shift));
         }
-        u.seen = (uint32_t)uniform((int)u.seen);
+        u.seen = uniform(u.seen);
         return u;
     }
-    // LATER: not the wave's first unit: no more than FLIGHT_ loads on their way.  The rows of a load lie in one page; where that is
+    // LATER: not the wave's first unit: no more than MOST loads on their way.  The rows of a load lie in one page; where that is
     // none, they are read from page 0, and rows behind the last key from wherever they would be: both exist, and neither is seen.
-    template <bool V, bool LATER> __device__ __forceinline__ void issue(const char* __restrict__ base, const UnitRef& u, int ids) const
+    template <bool V, bool LATER> __device__ __forceinline__ void issue(const char* __restrict__ base, const Ref& u, int ids) const
     {
         const char* const first_row = base + u.head + (uint64_t)(uint32_t)(u.key0 & ((1 << page_shift) - 1)) * row_bytes;
 #pragma unroll
         for (int i = 0; i < LPU; ++i) {
-            if (LATER && i + LPU >= R::FLIGHT_) wait_vm<R::FLIGHT_ - 1>();
+            if (LATER && i + LPU >= R::MOST) wait_vm<R::MOST - 1>();
             const uint32_t id = (uint32_t)max(__builtin_amdgcn_readlane(ids, u.at + ((i * R::RPI) >> sub_shift)), 0);
-            __builtin_amdgcn_global_load_lds((const GLB_AS void*)(first_row + (uint64_t)id * page_bytes + (V ? dv[i] : dk[i])),
-                                             (LDS_AS void*)(uintptr_t)((V ? vring : kring) + i * 1024), 16, 0, DMA_STREAM);
+            const GLB_AS void* const from = (const GLB_AS void*)(first_row + (uint64_t)id * page_bytes + (V ? dv[i] : dk[i]));
+            LDS_AS void* const to = (LDS_AS void*)(uintptr_t)((V ? vring : kring) + i * 1024);
+            if (R::HALF_LINES && shared) __builtin_amdgcn_global_load_lds(from, to, 16, 0, 0);
+            else __builtin_amdgcn_global_load_lds(from, to, 16, 0, DMA_STREAM);
         }
     }
 };
@@ -356,14 +374,14 @@ template <int FMT, int D, int NT>
 __device__ __forceinline__ void walk_units(const char* __restrict__ k, const char* __restrict__ v, const int32_t* __restrict__ table,
                                            const Stream<FMT, D>& st, const Piece<Rows<FMT, D>::UNIT>& p, const Piece<Rows<FMT, D>::UNIT>& then,
                                            const char* __restrict__ then_q, int then_rows,
-                                           const typename Operand<FMT>::T (&q)[NT][Rows<FMT, D>::KS][Rows<FMT, D>::QPARTS], const TrScales& sc, float scale, bool first, int& ids, UnitRef& cur, Acc<D, NT>& acc)
+                                           const typename Operand<FMT>::T (&q)[NT][Rows<FMT, D>::KS][Rows<FMT, D>::QPARTS], const TrScales& sc, float scale, bool first, int& ids, UnitRef<Rows<FMT, D>::UNIT>& cur, Acc<D, NT>& acc)
 {
     using R = Rows<FMT, D>;
     typedef typename Operand<FMT>::T Op;
     constexpr bool BF16 = R::BF16, Q8 = R::Q8;
     constexpr int LPU = R::LPU, KB = R::UNIT / 16, KS = R::ROW / 64; // blocks of 16 keys; 64-byte steps of a row
-    constexpr uint32_t ALL = BF16 ? 0xffffffffu : 0xffffu;
-    static_assert(R::FLIGHT_ <= 2 * LPU, "");
+    constexpr Mask<R::UNIT> ALL = R::UNIT == 16 ? 0xffffu : ~(Mask<R::UNIT>)0;
+    static_assert(R::MOST <= 2 * LPU, "");
     const int lane = st.lane, c16 = lane & 15, quad = lane >> 4;
     int koff[KS], voff[D / 16]; // V: fp32 four rows of two or one 256-byte groups, bf16 a group of 16 channels each
 #pragma unroll
@@ -377,7 +395,7 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
     int ks_of = 0, vs_of = 0; // scales of the blocks that ids are held for, a lane each
     auto request_ids = [&](int j0) { j0 < p.n ? st.request_ids(table, p, j0) : st.request_ids(table, then, 0); };
     for (int t = 0; t < p.n; ++t) {
-        UnitRef next;
+        UnitRef<R::UNIT> next;
         const bool last = t + 1 == p.n, more = !last || then.n > 0;
         // K(t).  Behind the keys of a piece that is not the first there are, besides its values, the results of the last one: at least
         // D / 16 stores of a lane, none of which touches another and could become one with it.
@@ -417,19 +435,20 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             else st.template issue<false, true>(k, next, ids);
         }
         if constexpr (Q8) {
+            float by[KB];
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                const float by = scale_of(ks_of, cur.at + kb);
+            for (int kb = 0; kb < KB; ++kb) by[kb] = scale_of(ks_of, cur.at + kb);
 #pragma unroll
-                for (int ks = 0; ks < 2 * KS; ++ks) {
-                    const bf16x8 a = worth(ka[kb][ks >> 1][2 * (ks & 1)], by, ka[kb][ks >> 1][2 * (ks & 1) + 1], by);
+            for (int ks = 0; ks < 2 * KS; ++ks)
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) { // as many chains as there are blocks
+                    const bf16x8 a = worth(ka[kb][ks >> 1][2 * (ks & 1)], by[kb], ka[kb][ks >> 1][2 * (ks & 1) + 1], by[kb]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int j = R::QPARTS - 1; j >= 0; --j)
                             s[n][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[n][ks][j], ks == 0 && j == R::QPARTS - 1 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : s[n][kb], 0, 0, 0);
                 }
-            }
         } else if constexpr (BF16) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
@@ -450,7 +469,7 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             }
         }
         // element e of block kb is key 16 kb + 4 quad + e of the unit
-        const uint32_t mine = cur.seen >> (4 * quad);
+        const Mask<R::UNIT> mine = cur.seen >> (4 * quad);
         if (cur.seen != ALL) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -458,12 +477,13 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
                 for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (!(mine & (1u << (16 * kb + e)))) s[n][kb][e] = -INFINITY;
+                        if (!((uint32_t)(mine >> (16 * kb)) & (1u << e))) s[n][kb][e] = -INFINITY;
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float top = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3]));
-            if (KB == 2) top = fmaxf(top, fmaxf(fmaxf(s[n][KB - 1][0], s[n][KB - 1][1]), fmaxf(s[n][KB - 1][2], s[n][KB - 1][3])));
+#pragma unroll
+            for (int kb = 1; kb < KB; ++kb) top = fmaxf(top, fmaxf(fmaxf(s[n][kb][0], s[n][kb][1]), fmaxf(s[n][kb][2], s[n][kb][3])));
             // A weight is 2^((s - m) scale), the difference first: it is exact or nearly so however large the scores are, where that of
             // two products with the scale would be off by their roundings.  No weight exceeds 1, so that values near the largest do not overflow.
             if (__any(top > acc.m[n])) {
@@ -487,71 +507,106 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
         if (more) wait_vm<LPU>(); // V(t)
         else wait_vm<0>();
         asm volatile("" ::: "memory");
-        Op va[D / 16];
-        i32x2 vraw[Q8 ? D / 16 : 1];
-#pragma unroll
-        for (int cb = 0; cb < D / 16; ++cb) {
-            if constexpr (Q8) {
-                vraw[cb] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_AS i32x2*)(lds + voff[cb])); // keys of the first block, of the second
-            } else if constexpr (BF16) {
-                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(lds + voff[cb]));
-                const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(lds + voff[cb] + 16 * R::ROW));
-                va[cb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-            } else {
-                va[cb] = *(LDS_AS const f32x4*)(lds + voff[cb]); // key 4 quad + cb % 4, channels 64 (cb / 4) + 4 c16 ..
-            }
-        }
-        wait_lds(); // the unit's values are read
-        if (!last) st.template issue<true, true>(v, next, ids);
         if constexpr (Q8) {
-            const float by[2] = {scale_of(vs_of, cur.at), scale_of(vs_of, cur.at + 1)};
+            i32x2 raw[KB / 2][D / 16]; // codes of four keys of a block, and of the block behind
 #pragma unroll
-            for (int cb = 0; cb < D / 16; ++cb) va[cb] = worth((uint32_t)vraw[cb][0], by[0], (uint32_t)vraw[cb][1], by[1]);
-        }
-        u32x4 parts[NT][3]; // of the weights, as bf16; fp32: they stay in s.  Not sooner: the next values are on their way meanwhile
-        if constexpr (BF16) {
+            for (int g = 0; g < KB / 2; ++g)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+                for (int cb = 0; cb < D / 16; ++cb) raw[g][cb] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((LDS_AS i32x2*)(lds + voff[cb] + g * 32 * R::ROW));
+            wait_lds(); // the unit's values are read
+            if (!last) st.template issue<true, true>(v, next, ids);
 #pragma unroll
-                for (int i = 0; i < 4 * KB; i += 2) {
-                    const auto w = split(s[n][i >> 2][i & 3], s[n][i >> 2][(i & 3) + 1]);
+            for (int g = 0; g < KB / 2; ++g) {
+                const float by[2] = {scale_of(vs_of, cur.at + 2 * g), scale_of(vs_of, cur.at + 2 * g + 1)};
+                Op va[D / 16];
 #pragma unroll
-                    for (int j = 0; j < 3; ++j) parts[n][j][i / 2] = w.pair[j];
+                for (int cb = 0; cb < D / 16; ++cb) va[cb] = worth((uint32_t)raw[g][cb][0], by[0], (uint32_t)raw[g][cb][1], by[1]);
+                if (cur.seen != ALL) { // what is not seen may be anything, and even a weight of zero would make NaN of NaN
+                    const uint32_t bits = (uint32_t)(mine >> (32 * g));
+                    u32x4 keep;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int bit = 16 * (i >> 1) + 2 * (i & 1);
+                        keep[i] = ((bits >> bit) & 1 ? 0xffffu : 0u) | ((bits >> bit) & 2 ? 0xffff0000u : 0u);
+                    }
+#pragma unroll
+                    for (int cb = 0; cb < D / 16; ++cb) va[cb] = __builtin_bit_cast(Op, __builtin_bit_cast(u32x4, va[cb]) & keep);
                 }
-        }
-        if (cur.seen != ALL) { // what is not seen may be anything, and even a weight of zero would make NaN of NaN
-            u32x4 keep; // bf16: element j of an operand is key 16 (j >> 2) + 4 quad + (j & 3)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int bit = BF16 ? 16 * (i >> 1) + 2 * (i & 1) : i;
-                keep[i] = BF16 ? ((mine >> bit) & 1 ? 0xffffu : 0u) | ((mine >> bit) & 2 ? 0xffff0000u : 0u) : (mine >> bit) & 1 ? 0xffffffffu : 0u;
+                for (int n = 0; n < NT; ++n) {
+                    u32x4 parts[3];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const auto w = split<false>(s[n][2 * g + (i >> 1)][2 * (i & 1)], s[n][2 * g + (i >> 1)][2 * (i & 1) + 1]);
+#pragma unroll
+                        for (int j = 0; j < 3; ++j) parts[j][i] = w.pair[j];
+                    }
+#pragma unroll
+                    for (int j = 0; j < 3; ++j)
+#pragma unroll
+                        for (int cb = 0; cb < D / 16; ++cb)
+                            acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], __builtin_bit_cast(bf16x8, parts[j]), acc.o[n][cb], 0, 0, 0);
+                }
             }
-#pragma unroll
-            for (int cb = 0; cb < D / 16; ++cb) {
-                const u32x4 mask = BF16 ? keep : u32x4{keep[cb & 3], keep[cb & 3], keep[cb & 3], keep[cb & 3]};
-                va[cb] = __builtin_bit_cast(Op, __builtin_bit_cast(u32x4, va[cb]) & mask);
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
+        } else {
+            Op va[D / 16];
 #pragma unroll
             for (int cb = 0; cb < D / 16; ++cb) {
                 if constexpr (BF16) {
-#pragma unroll
-                    for (int j = 0; j < 3; ++j)
-                        acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], __builtin_bit_cast(bf16x8, parts[n][j]), acc.o[n][cb], 0, 0, 0);
-                } else { // operand cb holds key cb % 4 of the four; its channel i goes to block 4 (cb / 4) + i
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        acc.o[n][(cb & ~3) | i] = __builtin_amdgcn_mfma_f32_16x16x4f32(va[cb][i], s[n][0][cb & 3], acc.o[n][(cb & ~3) | i], 0, 0, 0);
+                    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(lds + voff[cb]));
+                    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)(lds + voff[cb] + 16 * R::ROW));
+                    va[cb] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+                } else {
+                    va[cb] = *(LDS_AS const f32x4*)(lds + voff[cb]); // key 4 quad + cb % 4, channels 64 (cb / 4) + 4 c16 ..
                 }
             }
+            wait_lds(); // the unit's values are read
+            if (!last) st.template issue<true, true>(v, next, ids);
+            u32x4 parts[NT][3]; // of the weights, as bf16; fp32: they stay in s.  Not sooner: the next values are on their way meanwhile
+            if constexpr (BF16) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4 * KB; i += 2) {
+                        const auto w = split<true>(s[n][i >> 2][i & 3], s[n][i >> 2][(i & 3) + 1]);
+#pragma unroll
+                        for (int j = 0; j < 3; ++j) parts[n][j][i / 2] = w.pair[j];
+                    }
+            }
+            if (cur.seen != ALL) { // what is not seen may be anything, and even a weight of zero would make NaN of NaN
+                u32x4 keep; // bf16: element j of an operand is key 16 (j >> 2) + 4 quad + (j & 3)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int bit = BF16 ? 16 * (i >> 1) + 2 * (i & 1) : i;
+                    keep[i] = BF16 ? ((mine >> bit) & 1 ? 0xffffu : 0u) | ((mine >> bit) & 2 ? 0xffff0000u : 0u) : (mine >> bit) & 1 ? 0xffffffffu : 0u;
+                }
+#pragma unroll
+                for (int cb = 0; cb < D / 16; ++cb) {
+                    const u32x4 mask = BF16 ? keep : u32x4{keep[cb & 3], keep[cb & 3], keep[cb & 3], keep[cb & 3]};
+                    va[cb] = __builtin_bit_cast(Op, __builtin_bit_cast(u32x4, va[cb]) & mask);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int cb = 0; cb < D / 16; ++cb) {
+                    if constexpr (BF16) {
+#pragma unroll
+                        for (int j = 0; j < 3; ++j)
+                            acc.o[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[cb], __builtin_bit_cast(bf16x8, parts[n][j]), acc.o[n][cb], 0, 0, 0);
+                    } else { // operand cb holds key cb % 4 of the four; its channel i goes to block 4 (cb / 4) + i
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            acc.o[n][(cb & ~3) | i] = __builtin_amdgcn_mfma_f32_16x16x4f32(va[cb][i], s[n][0][cb & 3], acc.o[n][(cb & ~3) | i], 0, 0, 0);
+                    }
+                }
+        }
         cur = next;
     }
 }
 
 template <int FMT, int D, int NT, int WORKERS>
-__global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const TrPagedDecodeArgs a)
+__global__ __launch_bounds__(64, NT == 1 || WORKERS > 1024 ? 2 : 1) void paged_decode_kernel(const TrPagedDecodeArgs a)
 {
     using R = Rows<FMT, D>;
     using P = Piece<R::UNIT>;
@@ -648,7 +703,7 @@ __global__ __launch_bounds__(64, NT == 1 ? 2 : 1) void paged_decode_kernel(const
     wait_vm<16 * NT / R::QPI>(); // the ids
     asm volatile("" ::: "memory");
     int ids = st.take_ids(p, 0);
-    UnitRef cur = st.ref(p, 0, ids);
+    UnitRef<R::UNIT> cur = st.ref(p, 0, ids);
     const TrScales sc = {a.pool.k_scale, a.pool.v_scale, a.n_kv_heads};
     if constexpr (R::Q8) st.request_scales(sc, p, 0, ids);
     st.template issue<false, false>(a.pool.k, cur, ids);
