@@ -179,6 +179,69 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
     }
 }
 
+// Query heads: the pass of paged_append_kernel over one side.  A workgroup owns a few tokens, a thread the same unit of several heads of one of
+// them.
+template <int DTYPE, int D, bool HALF, bool STREAM, int THREADS>
+__device__ __forceinline__ void append_queries(const TrPagedAppendArgs& a, float2* turn, int64_t block)
+{
+    using V = Vec<DTYPE>;
+    constexpr int N = V::N, LPH = D / N, UNITS = 3, HEAD = D * 16 / N, TURNS = HALF ? N : N / 2;
+    const int tid = threadIdx.x, piece = tid % LPH;
+    const int pairs = a.rotary_dim / 2, half_units = pairs / N, n_heads = a.n_q_heads;
+    const bool turns = piece * N < a.rotary_dim, low = piece < half_units, normed = a.q_norm != nullptr;
+    const int partner = turns ? (tid & 63) + (low ? half_units : -half_units) : (tid & 63);
+    const int m0 = HALF ? (low ? piece : piece - half_units) * N : piece * (N / 2);
+    const int step = THREADS / LPH >> a.tile_shift; // heads of a token that are worked on at a time
+    const int64_t t0 = block << a.tile_shift;
+    const int tokens = (int)min((int64_t)1 << a.tile_shift, a.n_tokens - t0);
+    const int tok = tid / LPH / step;
+    const bool live = tok < tokens;
+    const int64_t t = t0 + (live ? tok : 0);
+    int h = tid / LPH % step;
+    const char* const q = a.q + t * a.q_stride + piece * 16;
+    char* const to = a.q_out + t * n_heads * HEAD + piece * 16;
+
+    u32x4 u[UNITS];
+    auto load = [&](int head) { return live && head < n_heads ? __builtin_nontemporal_load((const u32x4*)(q + (int64_t)head * HEAD)) : u32x4{}; };
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) u[i] = load(h + i * step);
+    u32x4 w_raw = {};
+    if (normed) w_raw = ((const u32x4*)a.q_norm)[piece];
+    for (int i = tid; i < tokens * pairs; i += THREADS) {
+        const int at = i / pairs, m = i - at * pairs;
+        double sn, cn;
+        tr_sincos((double)a.pos[t0 + at] * a.freq[m], &sn, &cn);
+        turn[at * 64 + m] = make_float2((float)(cn * a.amplitude), (float)(sn * a.amplitude));
+    }
+    __syncthreads();
+    float2 e[TURNS];
+#pragma unroll
+    for (int c = 0; c < TURNS; ++c) {
+        e[c] = turns && live ? turn[tok * 64 + m0 + c] : make_float2(1.0f, 0.0f);
+        if (HALF && low) e[c].y = -e[c].y;
+    }
+    float w[N];
+    V::open(w_raw, w);
+    for (;; h += UNITS * step) {
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int head = h + i * step;
+            if (!live || head >= n_heads) continue; // heads are dealt out whole, so the lanes of one are here together
+            if (pairs || normed) {
+                float x[N];
+                V::open(u[i], x);
+                norm_and_turn<N, LPH, HALF>(x, normed, w, a.eps, e, turns, a.rotary_dim == D, partner);
+                if (normed || turns) u[i] = V::close(x);
+            }
+            if (STREAM) __builtin_nontemporal_store(u[i], (u32x4*)(to + (int64_t)head * HEAD));
+            else *(u32x4*)(to + (int64_t)head * HEAD) = u[i];
+        }
+        if (h - tid / LPH % step + UNITS * step >= n_heads) break;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) u[i] = load(h + (UNITS + i) * step);
+    }
+}
+
 // Keys and values by separate workgroups, which have half as much to hold, and in front of the queries', as they take longer.
 template <int DTYPE, int D, bool HALF, bool STREAM>
 __global__ __launch_bounds__(append_q8_threads(DTYPE, D), DTYPE == TR_BF16 ? 4 : 2) void append_q8_kernel(const TrPagedAppendArgs a, int64_t first, int window, int n_blocks)
@@ -188,7 +251,7 @@ __global__ __launch_bounds__(append_q8_threads(DTYPE, D), DTYPE == TR_BF16 ? 4 :
     __shared__ Tops<DTYPE, D> tops[3], olds[3];
     const int block = blockIdx.x;
     if (block < n_blocks) append_blocks<DTYPE, D, HALF, THREADS>(a, turn, tops, olds, first + (int64_t)(block >> 1) * window, window, !(block & 1));
-    else append_heads<DTYPE, D, HALF, STREAM, THREADS, true>(a, turn, (first >> a.tile_shift) + block - n_blocks);
+    else append_queries<DTYPE, D, HALF, STREAM, THREADS>(a, turn, (first >> a.tile_shift) + block - n_blocks);
 }
 
 // Largest i of 64 lanes with starts <= x, for ascending starts; -1 if there is none.
