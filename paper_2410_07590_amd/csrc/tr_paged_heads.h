@@ -65,50 +65,4 @@ template <int LANES> __device__ __forceinline__ float other_half(float x)
     } else return __shfl_xor(x, LANES / 2);
 }
 
-// A lane's unit x of a head that LPH neighbouring lanes hold: normalised with the unit's weights w, turned by the cosines and sines e of
-// the pairs that it has part in (HALF: sines of the lower half negated).  turns: the unit's channels do; full: the whole head's; partner: the
-// lane with the other channels of its pairs.  paged_append_kernel has the same steps in its own loop: 16001 tokens of 32 / 8 heads take it 80.5 us
-// so, 82.2 with this function.
-template <int N, int LPH, bool HALF, int TURNS>
-__device__ __forceinline__ void norm_and_turn(float (&x)[N], bool normed, const float (&w)[N], float eps, const float2 (&e)[TURNS], bool turns, bool full, int partner)
-{
-    static_assert(TURNS == (HALF ? N : N / 2), "");
-    if (normed) {
-        auto mean_square = [&]() {
-            float ss = 0.0f;
-#pragma unroll
-            for (int c = 0; c < N; ++c) ss = fmaf(x[c], x[c], ss);
-            return lanes_sum<LPH>(ss) * (1.0f / (N * LPH));
-        };
-        float under = mean_square() + eps;
-        if (!(under <= __FLT_MAX__)) { // for all lanes of the head: the same of a head 2^70 times smaller
-#pragma unroll
-            for (int c = 0; c < N; ++c) x[c] *= 0x1p-70f;
-            under = mean_square() + eps * 0x1p-70f * 0x1p-70f;
-        }
-        const float r = rsqrtf(under);
-#pragma unroll
-        for (int c = 0; c < N; ++c) x[c] = x[c] * r * w[c]; // in this order: x r is of size 1
-    }
-    if (HALF) {
-        float y[N];
-        if (full) {
-#pragma unroll
-            for (int c = 0; c < N; ++c) y[c] = other_half<LPH>(x[c]);
-        } else {
-#pragma unroll
-            for (int c = 0; c < N; ++c) y[c] = __shfl(x[c], partner);
-        }
-#pragma unroll
-        for (int c = 0; c < N; ++c) x[c] = turns ? x[c] * e[c].x + y[c] * e[c].y : x[c];
-    } else {
-#pragma unroll
-        for (int c = 0; c < N / 2; ++c) {
-            const float one = x[2 * c], two = x[2 * c + 1];
-            x[2 * c] = turns ? one * e[c].x - two * e[c].y : one;
-            x[2 * c + 1] = turns ? two * e[c].x + one * e[c].y : two;
-        }
-    }
-}
-
 } // namespace

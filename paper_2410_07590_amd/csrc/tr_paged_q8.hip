@@ -7,16 +7,80 @@
 
 namespace {
 
-// Largest of the lanes that share a head.
-template <int LANES> __device__ __forceinline__ int lanes_max(int x)
+// The value of another lane of the row of 16, in a form that the instruction that takes it can contain.
+template <int CTRL> __device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true); }
+template <int CTRL> __device__ __forceinline__ float from_lane(float x) { return __int_as_float(from_lane<CTRL>(__float_as_int(x))); }
+constexpr int PAIRS = 0xB1, FOURS = 0x4E, EIGHTS = 0x141, ROW = 0x140, HALF_ROW = 0x128; // quad_perm [1,0,3,2], [2,3,0,1], mirrors, row_ror 8
+
+// Over the lanes that share a head: the largest, the sum.
+template <int LANES> __device__ __forceinline__ int most(int x)
 {
-    auto with = [&](int y) { x = max(x, y); };
-    with(__builtin_amdgcn_update_dpp(x, x, 0xB1, 0xf, 0xf, false));                    // quad_perm [1,0,3,2]
-    with(__builtin_amdgcn_update_dpp(x, x, 0x4E, 0xf, 0xf, false));                    // quad_perm [2,3,0,1]
-    with(__builtin_amdgcn_update_dpp(x, x, 0x141, 0xf, 0xf, false));                   // row_half_mirror
-    if (LANES >= 16) with(__builtin_amdgcn_update_dpp(x, x, 0x140, 0xf, 0xf, false));  // row_mirror
-    if (LANES == 32) with(__shfl_xor(x, 16));
+    x = max(x, from_lane<PAIRS>(x));
+    x = max(x, from_lane<FOURS>(x));
+    x = max(x, from_lane<EIGHTS>(x));
+    if (LANES >= 16) x = max(x, from_lane<ROW>(x));
+    if (LANES == 32) x = max(x, __shfl_xor(x, 16));
     return x;
+}
+template <int LANES> __device__ __forceinline__ float sum(float x)
+{
+    x += from_lane<PAIRS>(x);
+    x += from_lane<FOURS>(x);
+    x += from_lane<EIGHTS>(x);
+    if (LANES >= 16) x += from_lane<ROW>(x);
+    if (LANES == 32) x += __shfl_xor(x, 16);
+    return x;
+}
+
+// A lane's unit x of a head that LPH neighbouring lanes hold: normalised with the unit's weights w, turned by the cosines and sines e of
+// the pairs that it has part in (HALF: sines of the lower half negated).  turns: the unit's channels do; full: the whole head's; partner: the
+// lane with the other channels of its pairs.  The steps of paged_append_kernel, which has them in its own loop: 16001 tokens of 32 / 8 heads take it
+// 80.5 us so, 82.2 with a function like this one.
+template <int N, int LPH, bool HALF, int TURNS>
+__device__ __forceinline__ void norm_and_turn(float (&x)[N], bool normed, const float (&w)[N], float eps, const float2 (&e)[TURNS], bool turns, bool full, int partner)
+{
+    static_assert(TURNS == (HALF ? N : N / 2), "");
+    if (normed) {
+        auto mean_square = [&]() {
+            float ss = 0.0f;
+#pragma unroll
+            for (int c = 0; c < N; ++c) ss = fmaf(x[c], x[c], ss);
+            return sum<LPH>(ss) * (1.0f / (N * LPH));
+        };
+        float under = mean_square() + eps;
+        if (!(under <= __FLT_MAX__)) { // for all lanes of the head: the same of a head 2^70 times smaller
+#pragma unroll
+            for (int c = 0; c < N; ++c) x[c] *= 0x1p-70f;
+            under = mean_square() + eps * 0x1p-70f * 0x1p-70f;
+        }
+        const float r = rsqrtf(under);
+#pragma unroll
+        for (int c = 0; c < N; ++c) x[c] = x[c] * r * w[c]; // in this order: x r is of size 1
+    }
+    if (HALF && full) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) x[c] = x[c] * e[c].x + (LPH == 16 ? from_lane<HALF_ROW>(x[c]) : other_half<LPH>(x[c])) * e[c].y;
+    } else if (HALF) {
+        float y[N];
+#pragma unroll
+        for (int c = 0; c < N; ++c) y[c] = __shfl(x[c], partner);
+#pragma unroll
+        for (int c = 0; c < N; ++c) x[c] = turns ? x[c] * e[c].x + y[c] * e[c].y : x[c];
+    } else if (full) {
+#pragma unroll
+        for (int c = 0; c < N / 2; ++c) {
+            const float one = x[2 * c], two = x[2 * c + 1];
+            x[2 * c] = one * e[c].x - two * e[c].y;
+            x[2 * c + 1] = two * e[c].x + one * e[c].y;
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < N / 2; ++c) {
+            const float one = x[2 * c], two = x[2 * c + 1];
+            x[2 * c] = turns ? one * e[c].x - two * e[c].y : one;
+            x[2 * c + 1] = turns ? two * e[c].x + one * e[c].y : two;
+        }
+    }
 }
 
 // Threads of a workgroup: 16 rows of a head at least.
@@ -33,15 +97,16 @@ template <int N> __device__ __forceinline__ void put(char* to, const float (&x)[
 // tokens that the call writes to a block of 16 rows stand side by side, from one on whose slot lies in another block than that in front of it.
 // A block's heads need two steps, the largest value of all its rows and then the codes; values wait for that in registers, and the
 // next heads are on their way.
-constexpr int append_q8_units(int dtype) { return dtype == TR_F32 ? 4 : 2; } // heads that a thread has part in at a time, 16 channels
+constexpr int VU = 2;
+// Heads that a thread has part in at a time: 16 channels of keys, which it holds in fp32, 32 of values, which it holds as they come.
+constexpr int append_q8_units(int dtype, bool keys) { return (dtype == TR_F32 ? 4 : 2) * (keys ? 1 : VU); }
 // The largest values of a step's heads, and the exponents that they had; what one step reads the next but one clears.
-template <int DTYPE, int D> using Tops = int[append_q8_units(DTYPE) * append_q8_threads(DTYPE, D) * Vec<DTYPE>::N / D];
-template <int DTYPE, int D, bool HALF, int THREADS>
-__device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2* turn, Tops<DTYPE, D>* tops, Tops<DTYPE, D>* olds, int64_t t0, int window,
-                                              bool keys)
+template <int DTYPE, int D> using Tops = int[append_q8_units(DTYPE, false) * append_q8_threads(DTYPE, D) * Vec<DTYPE>::N / D];
+template <int DTYPE, int D, bool HALF, int THREADS, bool KEYS>
+__device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2* turn, Tops<DTYPE, D>* tops, Tops<DTYPE, D>* olds, int64_t t0, int window)
 {
     using V = Vec<DTYPE>;
-    constexpr int N = V::N, LPH = D / N, UNITS = append_q8_units(DTYPE), HEAD = D * 16 / N, ROWS = THREADS / LPH; // ROWS: heads of tokens at a time
+    constexpr int N = V::N, LPH = D / N, UNITS = append_q8_units(DTYPE, KEYS), HEAD = D * 16 / N, ROWS = THREADS / LPH; // ROWS: heads of tokens at a time
     constexpr int TURNS = HALF ? N : N / 2, TOPS = UNITS * ROWS;
     static_assert(ROWS >= TR_Q8_ROWS, "");
     const int tid = threadIdx.x, lane = tid & 63, piece = tid % LPH, g = tid / LPH, scale_shift = a.pool.page_shift - 4;
@@ -53,14 +118,15 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
     uint64_t owners = __ballot(lane >= 1 && lane <= window && block >= 0 && block != before && block >> scale_shift < a.pool.n_pages);
     if (!owners) return;
 
-    const int n_heads = a.n_kv_heads, pairs = keys ? a.rotary_dim / 2 : 0, half_units = pairs / N;
-    const bool normed = keys && a.k_norm, turns = keys && piece * N < a.rotary_dim, low = piece < half_units, full = a.rotary_dim == D;
+    const int n_heads = a.n_kv_heads, pairs = KEYS ? a.rotary_dim / 2 : 0, half_units = pairs / N;
+    const bool normed = KEYS && a.k_norm, turns = KEYS && piece * N < a.rotary_dim, low = piece < half_units, full = a.rotary_dim == D;
     const int partner = turns ? lane + (low ? half_units : -half_units) : lane;
     const int m0 = HALF ? (low ? piece : piece - half_units) * N : piece * (N / 2);
-    const char* const from = keys ? a.k : a.v;
-    const int64_t stride = keys ? a.k_stride : a.v_stride;
-    char* const to_pool = keys ? a.pool.k : a.pool.v;
-    uint8_t* const scales = keys ? a.pool.k_scale : a.pool.v_scale;
+    const char* const from = KEYS ? a.k : a.v;
+    const int64_t stride = KEYS ? a.k_stride : a.v_stride;
+    char* const to_pool = KEYS ? a.pool.k : a.pool.v;
+    uint8_t* const scales = KEYS ? a.pool.k_scale : a.pool.v_scale;
+    const double freq = lane < pairs ? a.freq[lane] : 0.0;
     u32x4 kw_raw = {};
     if (normed) kw_raw = ((const u32x4*)a.k_norm)[piece];
     float kw[N];
@@ -99,11 +165,19 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
         };
         load(0);
         __syncthreads(); // the last block's angles are read
-        for (int i = tid; i < run * pairs; i += THREADS) {
-            const int at = i / pairs, m = i - at * pairs;
-            double sn, cn;
-            tr_sincos((double)a.pos[t0 + at0 - 1 + at] * a.freq[m], &sn, &cn);
-            turn[at * 64 + m] = make_float2((float)(cn * a.amplitude), (float)(sn * a.amplitude));
+        if (KEYS) { // a lane has the same pair of every token that its wave takes
+            constexpr int WAVES = THREADS / 64, EACH = TR_Q8_ROWS / WAVES;
+            const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+            int pos[EACH];
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) pos[j] = wave + j * WAVES < run && pairs ? a.pos[t0 + at0 - 1 + wave + j * WAVES] : 0;
+#pragma unroll
+            for (int j = 0; j < EACH; ++j) {
+                if (wave + j * WAVES >= run || lane >= pairs) continue;
+                double sn, cn;
+                tr_sincos((double)pos[j] * freq, &sn, &cn);
+                turn[(wave + j * WAVES) * 64 + lane] = make_float2((float)(cn * a.amplitude), (float)(sn * a.amplitude));
+            }
         }
         for (int i = tid; i < TOPS; i += THREADS) tops[0][i] = 0;
         __syncthreads();
@@ -115,7 +189,8 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
         }
         int buf = 0;
         for (int c0 = 0; c0 < n_heads; c0 += UNITS * step) {
-            float x[UNITS][N];
+            float x[KEYS ? UNITS : 1][N];
+            u32x4 now[UNITS];
             int old[UNITS];
             const int next = buf == 2 ? 0 : buf + 1;
             for (int i = tid; i < TOPS; i += THREADS) tops[next][i] = 0; // nobody reads or adds to it until the barrier
@@ -124,15 +199,22 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
                 const int head = c0 + h0 + i * step;
                 old[i] = held[i];
                 if (!live || head >= n_heads) continue;
-                V::open(raw[i], x[i]);
-                if (keys) norm_and_turn<N, LPH, HALF>(x[i], normed, kw, a.eps, e, turns, full, partner);
+                float (&y)[N] = x[KEYS ? i : 0];
+                now[i] = raw[i];
+                V::open(raw[i], y);
+                if (KEYS) norm_and_turn<N, LPH, HALF>(y, normed, kw, a.eps, e, turns, full, partner);
                 int top = 0;
 #pragma unroll
-                for (int c = 0; c < N; ++c) {
-                    const int bits = __float_as_int(x[i][c]) & 0x7fffffff;
-                    top = max(top, bits < 0x7f800000 ? bits : 0);
+                for (int c = 0; c < N; ++c) top = max(top, __float_as_int(y[c]) & 0x7fffffff);
+                if (top >= 0x7f800000) { // infinite and NaN channels have no part in it
+                    top = 0;
+#pragma unroll
+                    for (int c = 0; c < N; ++c) {
+                        const int bits = __float_as_int(y[c]) & 0x7fffffff;
+                        top = max(top, bits < 0x7f800000 ? bits : 0);
+                    }
                 }
-                top = lanes_max<LPH>(top);
+                top = most<LPH>(top);
                 if (piece == 0) atomicMax(&tops[buf][h0 + i * step], top);
                 if (piece == 0 && tok == 0) olds[buf][h0 + i * step] = (int)old[i] - 127;
             }
@@ -144,15 +226,17 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
                 if (!live || head >= n_heads) continue;
                 const int need = q8_exponent(tops[buf][h0 + i * step]), was = anew ? need : old[i] - 127, to = max(need, was);
                 const float by = q8_power(-to);
+                float (&y)[N] = x[KEYS ? i : 0];
+                if (!KEYS) V::open(now[i], y);
 #pragma unroll
-                for (int c = 0; c < N; ++c) x[i][c] *= by;
+                for (int c = 0; c < N; ++c) y[c] *= by;
                 if (to >= Q8_MOST) // the largest numbers would round to what fp32 has not
 #pragma unroll
                     for (int c = 0; c < N; ++c) {
                         const float most = 1.875f * q8_power(127 - to);
-                        if (fabsf(x[i][c]) > most && fabsf(x[i][c]) < 256.0f) x[i][c] = copysignf(most, x[i][c]);
+                        if (fabsf(y[c]) > most && fabsf(y[c]) < 256.0f) y[c] = copysignf(most, y[c]);
                     }
-                put<N>(rows + (int64_t)head * a.pool.head_stride + (int64_t)row * a.pool.row_stride, x[i]);
+                put<N>(rows + (int64_t)head * a.pool.head_stride + (int64_t)row * a.pool.row_stride, y);
                 if ((anew || to != was) && tok == 0 && piece == 0) scale[(int64_t)head << scale_shift] = (uint8_t)(to + 127);
             }
             if (!anew) { // where a scale has grown, the block's other rows are written again, a row to the lanes of a head
@@ -250,7 +334,9 @@ __global__ __launch_bounds__(append_q8_threads(DTYPE, D), DTYPE == TR_BF16 ? 4 :
     __shared__ float2 turn[TR_Q8_ROWS * 64]; // cosine and sine of each token's pairs, times the amplitude
     __shared__ Tops<DTYPE, D> tops[3], olds[3];
     const int block = blockIdx.x;
-    if (block < n_blocks) append_blocks<DTYPE, D, HALF, THREADS>(a, turn, tops, olds, first + (int64_t)(block >> 1) * window, window, !(block & 1));
+    const int64_t t0 = first + (int64_t)(block >> 1) * window;
+    if (block < n_blocks && !(block & 1)) append_blocks<DTYPE, D, HALF, THREADS, true>(a, turn, tops, olds, t0, window);
+    else if (block < n_blocks) append_blocks<DTYPE, D, HALF, THREADS, false>(a, turn, tops, olds, t0, window);
     else append_queries<DTYPE, D, HALF, STREAM, THREADS>(a, turn, (first >> a.tile_shift) + block - n_blocks);
 }
 
