@@ -410,7 +410,6 @@ struct TrPool {
     uint8_t *k_scale, *v_scale; // of a pool in 8 bits
 };
 #define TR_Q8_ROWS 16 // that share a scale
-#define TR_Q8_FEW 4096 // tokens of an append that get a workgroup each, to look whether they begin a block
 // Waves of a decode over codes.  A wave has a unit's keys and values on their way, half as many bytes where heads have 64 channels.
 __host__ __device__ constexpr int tr_q8_workers(int head_dim) { return head_dim == 64 ? 2048 : 1024; }
 #define TR_Q8_UNIT 64 // keys that a wave of the decode over 8 bits takes at a time

@@ -93,62 +93,97 @@ template <int N> __device__ __forceinline__ void put(char* to, const float (&x)[
     else *(uint32_t*)to = q8_encode(x[0], x[1], x[2], x[3]);
 }
 
-// Quantised heads.  A workgroup looks at `window` tokens and owns the blocks whose first tokens are among them, of keys or of values: the
-// tokens that the call writes to a block of 16 rows stand side by side, from one on whose slot lies in another block than that in front of it.
-// A block's heads need two steps, the largest value of all its rows and then the codes; values wait for that in registers, and the
-// next heads are on their way.
-constexpr int VU = 2;
+// The rows `which` of a block, a unit of N channels each, at another scale.
+template <int N> __device__ __forceinline__ void rescale(char* unit, uint32_t row_stride, uint32_t which, float by)
+{
+    constexpr int AT_ONCE = 32 / N; // as many as fill eight registers
+#pragma unroll 1
+    for (int j0 = 0; j0 < TR_Q8_ROWS; j0 += AT_ONCE) {
+        uint32_t w[AT_ONCE][N / 4] = {};
+        char* const at = unit + (int64_t)j0 * row_stride;
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+            for (int c = 0; c < N / 4; ++c)
+                if (which >> (j0 + j) & 1) w[j][c] = ((const uint32_t*)(at + (int64_t)j * row_stride))[c];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            float y[N];
+#pragma unroll
+            for (int c = 0; c < N; c += 4) {
+                float z[4];
+                q8_decode(w[j][c / 4], z);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) y[c + b] = z[b] * by;
+            }
+            if (which >> (j0 + j) & 1) put<N>(at + (int64_t)j * row_stride, y);
+        }
+    }
+}
+
+// Quantised heads.  The tokens that the call writes to a block of 16 rows stand side by side, as a run, from one on whose slot lies in another
+// block than that in front of it.  A workgroup looks at `window` tokens, at most 16, and owns the runs that begin with one of them, for some of the heads of keys
+// or of values.  It works on as many runs at a time as have 16 tokens together, a row of lanes to a token.  A block's heads need two steps, the
+// largest value of all its rows and then the codes; values wait for that in registers, and the next heads are on their way.
 // Heads that a thread has part in at a time: 16 channels of keys, which it holds in fp32, 32 of values, which it holds as they come.
-constexpr int append_q8_units(int dtype, bool keys) { return (dtype == TR_F32 ? 4 : 2) * (keys ? 1 : VU); }
-// The largest values of a step's heads, and the exponents that they had; what one step reads the next but one clears.
+constexpr int append_q8_units(int dtype, bool keys) { return (dtype == TR_F32 ? 4 : 2) * (keys ? 1 : 2); }
+// The largest values of a step's runs and heads; what one step reads the next but one clears.
 template <int DTYPE, int D> using Tops = int[append_q8_units(DTYPE, false) * append_q8_threads(DTYPE, D) * Vec<DTYPE>::N / D];
 template <int DTYPE, int D, bool HALF, int THREADS, bool KEYS>
-__device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2* turn, Tops<DTYPE, D>* tops, Tops<DTYPE, D>* olds, int64_t t0, int window)
+__device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2* turn, Tops<DTYPE, D>* tops, int* slots, int64_t t0, int window, int first_head, int end_head)
 {
     using V = Vec<DTYPE>;
     constexpr int N = V::N, LPH = D / N, UNITS = append_q8_units(DTYPE, KEYS), HEAD = D * 16 / N, ROWS = THREADS / LPH; // ROWS: heads of tokens at a time
-    constexpr int TURNS = HALF ? N : N / 2, TOPS = UNITS * ROWS;
+    constexpr int TURNS = HALF ? N : N / 2, TOPS = UNITS * ROWS, LOOK = 2 * TR_Q8_ROWS;                                 // lanes that hold a token's slot
     static_assert(ROWS >= TR_Q8_ROWS, "");
     const int tid = threadIdx.x, lane = tid & 63, piece = tid % LPH, g = tid / LPH, scale_shift = a.pool.page_shift - 4;
 
     const int64_t mine = t0 - 1 + lane; // lane i + 1: the slot of token t0 + i
-    const int slot = lane < window + TR_Q8_ROWS && mine >= 0 && mine < a.n_tokens ? a.slots[mine] : -1;
+    const int slot = lane < LOOK && mine >= 0 && mine < a.n_tokens ? a.slots[mine] : -1;
     const int block = slot >> 4;
     const int before = __shfl_up(block, 1);
-    uint64_t owners = __ballot(lane >= 1 && lane <= window && block >= 0 && block != before && block >> scale_shift < a.pool.n_pages);
-    if (!owners) return;
+    const uint64_t valid = __ballot(block >= 0 && block >> scale_shift < a.pool.n_pages), changes = __ballot(lane == 0 || block != before);
+    uint64_t owned = changes & valid & (((1ull << window) - 1) << 1); // lanes of the first tokens of runs
+    if (!owned) return;
+    const uint64_t firsts = __ballot(slot >= 0 && (slot & 15) == 0);
+    auto end_of = [&](int at) { return min(at + 1 + __builtin_ctzll(changes >> (at + 1) | 1ull << 62), at + TR_Q8_ROWS); }; // of the run that begins there
+    if (tid < LOOK) slots[tid] = slot;
 
-    const int n_heads = a.n_kv_heads, pairs = KEYS ? a.rotary_dim / 2 : 0, half_units = pairs / N;
+    const int pairs = KEYS ? a.rotary_dim / 2 : 0, half_units = pairs / N;
     const bool normed = KEYS && a.k_norm, turns = KEYS && piece * N < a.rotary_dim, low = piece < half_units, full = a.rotary_dim == D;
     const int partner = turns ? lane + (low ? half_units : -half_units) : lane;
     const int m0 = HALF ? (low ? piece : piece - half_units) * N : piece * (N / 2);
     const char* const from = KEYS ? a.k : a.v;
     const int64_t stride = KEYS ? a.k_stride : a.v_stride;
-    char* const to_pool = KEYS ? a.pool.k : a.pool.v;
-    uint8_t* const scales = KEYS ? a.pool.k_scale : a.pool.v_scale;
     const double freq = lane < pairs ? a.freq[lane] : 0.0;
     u32x4 kw_raw = {};
     if (normed) kw_raw = ((const u32x4*)a.k_norm)[piece];
     float kw[N];
     V::open(kw_raw, kw);
 
-    while (owners) {
-        const int at0 = __builtin_ctzll(owners); // lane of the block's first token
-        owners &= owners - 1;
-        const int own = __builtin_amdgcn_readlane(block, at0), page = own >> scale_shift, in_page = own & ((1 << scale_shift) - 1);
-        const int run = min(__builtin_ctzll(~(__ballot(block == own) >> at0)), TR_Q8_ROWS);
-        uint32_t written = ROWS > TR_Q8_ROWS ? ~0xffffu : 0u; // rows of the block
-        for (int j = 0; j < run; ++j) written |= 1u << (__builtin_amdgcn_readlane(slot, at0 + j) & 15);
-        const bool anew = written & 1;
+    while (owned) {
+        const int at0 = __builtin_ctzll(owned);
+        int end = end_of(at0);
+        owned &= owned - 1;
+        while (owned && end_of(__builtin_ctzll(owned)) - at0 <= TR_Q8_ROWS) {
+            end = end_of(__builtin_ctzll(owned));
+            owned &= owned - 1;
+        }
+        const int tokens = end - at0;
         int wide = 0; // log2 of the tokens that are worked on at a time
-        while ((1 << wide) < run) ++wide;
+        while ((1 << wide) < tokens) ++wide;
         const int step = ROWS >> wide, tok = g / step, h0 = g % step; // heads at a time
-        const bool live = tok < run;
-        const int64_t t = t0 + at0 - 1 + (live ? tok : 0);
-        const int row = __shfl(slot, at0 + (live ? tok : 0)) & 15;
-        const char* const heads = from + t * stride + piece * 16;
-        char* const rows = to_pool + (int64_t)page * a.pool.page_stride + (int64_t)(in_page * TR_Q8_ROWS) * a.pool.row_stride + piece * N;
-        uint8_t* const scale = scales + (((int64_t)page * n_heads) << scale_shift) + in_page;
+        const int at = min(at0 + tok, end - 1);                       // the token's lane
+        const bool live = tok < tokens && (valid >> at & 1);
+        const int begin = 63 - __builtin_clzll(changes & ((2ull << at) - 1)); // lane of its run's first token
+        const bool anew = (firsts >> begin & ((1ull << (end_of(begin) - begin)) - 1)) != 0, leads = at == begin;
+        __syncthreads(); // the slots are there, and the last runs' angles are read
+        const int own = slots[at];
+        const int64_t page = own >> a.pool.page_shift;
+        const int row = own & 15, in_page = (own >> 4) & ((1 << scale_shift) - 1);
+        const char* const heads = from + (t0 + at - 1) * stride + piece * 16;
+        char* const rows = (KEYS ? a.pool.k : a.pool.v) + page * a.pool.page_stride + (int64_t)(in_page * TR_Q8_ROWS) * a.pool.row_stride + piece * N;
+        uint8_t* const scale = (KEYS ? a.pool.k_scale : a.pool.v_scale) + ((page * a.n_kv_heads) << scale_shift) + in_page;
 
         u32x4 raw[UNITS];
         int held[UNITS];
@@ -158,22 +193,21 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
                 const int head = c0 + h0 + i * step;
                 raw[i] = u32x4{};
                 held[i] = 0;
-                if (!live || head >= n_heads) continue;
+                if (!live || head >= end_head) continue;
                 raw[i] = __builtin_nontemporal_load((const u32x4*)(heads + (int64_t)head * HEAD));
                 if (!anew) held[i] = scale[(int64_t)head << scale_shift];
             }
         };
-        load(0);
-        __syncthreads(); // the last block's angles are read
+        load(first_head);
         if (KEYS) { // a lane has the same pair of every token that its wave takes
             constexpr int WAVES = THREADS / 64, EACH = TR_Q8_ROWS / WAVES;
             const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
             int pos[EACH];
 #pragma unroll
-            for (int j = 0; j < EACH; ++j) pos[j] = wave + j * WAVES < run && pairs ? a.pos[t0 + at0 - 1 + wave + j * WAVES] : 0;
+            for (int j = 0; j < EACH; ++j) pos[j] = wave + j * WAVES < tokens && pairs ? a.pos[t0 + at0 - 1 + wave + j * WAVES] : 0;
 #pragma unroll
             for (int j = 0; j < EACH; ++j) {
-                if (wave + j * WAVES >= run || lane >= pairs) continue;
+                if (wave + j * WAVES >= tokens || lane >= pairs) continue;
                 double sn, cn;
                 tr_sincos((double)pos[j] * freq, &sn, &cn);
                 turn[(wave + j * WAVES) * 64 + lane] = make_float2((float)(cn * a.amplitude), (float)(sn * a.amplitude));
@@ -188,17 +222,18 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
             if (HALF && low) e[c].y = -e[c].y;
         }
         int buf = 0;
-        for (int c0 = 0; c0 < n_heads; c0 += UNITS * step) {
+        for (int c0 = first_head; c0 < end_head; c0 += UNITS * step) {
             float x[KEYS ? UNITS : 1][N];
             u32x4 now[UNITS];
             int old[UNITS];
             const int next = buf == 2 ? 0 : buf + 1;
             for (int i = tid; i < TOPS; i += THREADS) tops[next][i] = 0; // nobody reads or adds to it until the barrier
+            auto top_of = [&](int i) -> int& { return tops[buf][((h0 + i * step) << wide) + begin - at0]; };
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) {
                 const int head = c0 + h0 + i * step;
                 old[i] = held[i];
-                if (!live || head >= n_heads) continue;
+                if (!live || head >= end_head) continue;
                 float (&y)[N] = x[KEYS ? i : 0];
                 now[i] = raw[i];
                 V::open(raw[i], y);
@@ -215,16 +250,15 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
                     }
                 }
                 top = most<LPH>(top);
-                if (piece == 0) atomicMax(&tops[buf][h0 + i * step], top);
-                if (piece == 0 && tok == 0) olds[buf][h0 + i * step] = (int)old[i] - 127;
+                if (piece == 0) atomicMax(&top_of(i), top);
             }
-            if (c0 + UNITS * step < n_heads) load(c0 + UNITS * step);
+            if (c0 + UNITS * step < end_head) load(c0 + UNITS * step);
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) {
                 const int head = c0 + h0 + i * step;
-                if (!live || head >= n_heads) continue;
-                const int need = q8_exponent(tops[buf][h0 + i * step]), was = anew ? need : old[i] - 127, to = max(need, was);
+                if (!live || head >= end_head) continue;
+                const int need = q8_exponent(top_of(i)), was = anew ? need : old[i] - 127, to = max(need, was);
                 const float by = q8_power(-to);
                 float (&y)[N] = x[KEYS ? i : 0];
                 if (!KEYS) V::open(now[i], y);
@@ -236,26 +270,14 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
                         const float most = 1.875f * q8_power(127 - to);
                         if (fabsf(y[c]) > most && fabsf(y[c]) < 256.0f) y[c] = copysignf(most, y[c]);
                     }
-                put<N>(rows + (int64_t)head * a.pool.head_stride + (int64_t)row * a.pool.row_stride, y);
-                if ((anew || to != was) && tok == 0 && piece == 0) scale[(int64_t)head << scale_shift] = (uint8_t)(to + 127);
-            }
-            if (!anew) { // where a scale has grown, the block's other rows are written again, a row to the lanes of a head
-                const int here = min(UNITS * step, n_heads - c0);
-                char* const other = rows + (int64_t)g * a.pool.row_stride;
-                for (int i = 0; i < here; ++i) {
-                    const int was = olds[buf][i], to = max(q8_exponent(tops[buf][i]), was);
-                    if (to == was || (written >> g) & 1) continue;
-                    uint32_t* const unit = (uint32_t*)(other + (int64_t)(c0 + i) * a.pool.head_stride);
-                    const float by = q8_power(was - to);
-                    float y[N];
-#pragma unroll
-                    for (int c = 0; c < N; c += 4) {
-                        float z[4];
-                        q8_decode(unit[c / 4], z);
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) y[c + b] = z[b] * by;
-                    }
-                    put<N>((char*)unit, y);
+                char* const block_rows = rows + (int64_t)head * a.pool.head_stride;
+                put<N>(block_rows + (int64_t)row * a.pool.row_stride, y);
+                if (!leads || !(anew || to != was)) continue;
+                if (piece == 0) scale[(int64_t)head << scale_shift] = (uint8_t)(to + 127);
+                if (to != was) { // a larger scale: the block's other rows are written again.  A block that starts anew has none
+                    uint32_t others = 0xffffu;
+                    for (int j = begin; j < end_of(begin); ++j) others &= ~(1u << (slots[j] & 15));
+                    rescale<N>(block_rows, a.pool.row_stride, others, q8_power(was - to));
                 }
             }
             buf = next;
@@ -328,16 +350,20 @@ __device__ __forceinline__ void append_queries(const TrPagedAppendArgs& a, float
 
 // Keys and values by separate workgroups, which have half as much to hold, and in front of the queries', as they take longer.
 template <int DTYPE, int D, bool HALF, bool STREAM>
-__global__ __launch_bounds__(append_q8_threads(DTYPE, D), DTYPE == TR_BF16 ? 4 : 2) void append_q8_kernel(const TrPagedAppendArgs a, int64_t first, int window, int n_blocks)
+__global__ __launch_bounds__(append_q8_threads(DTYPE, D), DTYPE == TR_BF16 ? 3 : 2) void append_q8_kernel(const TrPagedAppendArgs a, int64_t first, int window, int n_windows, int n_parts)
 {
     constexpr int THREADS = append_q8_threads(DTYPE, D);
     __shared__ float2 turn[TR_Q8_ROWS * 64]; // cosine and sine of each token's pairs, times the amplitude
-    __shared__ Tops<DTYPE, D> tops[3], olds[3];
-    const int block = blockIdx.x;
-    const int64_t t0 = first + (int64_t)(block >> 1) * window;
-    if (block < n_blocks && !(block & 1)) append_blocks<DTYPE, D, HALF, THREADS, true>(a, turn, tops, olds, t0, window);
-    else if (block < n_blocks) append_blocks<DTYPE, D, HALF, THREADS, false>(a, turn, tops, olds, t0, window);
-    else append_queries<DTYPE, D, HALF, STREAM, THREADS>(a, turn, (first >> a.tile_shift) + block - n_blocks);
+    __shared__ Tops<DTYPE, D> tops[3];
+    __shared__ int slots[2 * TR_Q8_ROWS];
+    const int block = blockIdx.x, part = block / n_windows; // parts of the heads of keys, then of values
+    if (part < 2 * n_parts) {
+        const int p = part >> 1, per = (a.n_kv_heads + n_parts - 1) / n_parts;
+        const int first_head = p * per, end_head = min(first_head + per, a.n_kv_heads);
+        const int64_t t0 = first + (int64_t)(block - part * n_windows) * window;
+        if (part & 1) append_blocks<DTYPE, D, HALF, THREADS, false>(a, turn, tops, slots, t0, window, first_head, end_head);
+        else append_blocks<DTYPE, D, HALF, THREADS, true>(a, turn, tops, slots, t0, window, first_head, end_head);
+    } else append_queries<DTYPE, D, HALF, STREAM, THREADS>(a, turn, (first >> a.tile_shift) + block - 2 * n_parts * n_windows);
 }
 
 // Largest i of 64 lanes with starts <= x, for ascending starts; -1 if there is none.
@@ -481,21 +507,25 @@ __global__ __launch_bounds__(256) void read_q8_kernel(const TrPagedReadArgs a, i
 
 } // namespace
 
+static constexpr int PARTS_WGS = 512;
 // A launch takes a part of the tokens, as it has fewer than 2^32 threads.
 template <int DTYPE, int D> static int launch_append(const TrPagedAppendArgs& a, int layout, hipStream_t s)
 {
-    constexpr int THREADS = append_q8_threads(DTYPE, D);
-    const int window = a.n_tokens <= TR_Q8_FEW ? 1 : TR_Q8_ROWS, tile = 1 << a.tile_shift;
-    const int64_t most = TR_MAX_BLOCKS_256 / 4; // tokens, a multiple of the window and of the tile; at most that many workgroups of either side
+    constexpr int THREADS = append_q8_threads(DTYPE, D), UNITS = append_q8_units(DTYPE, true);
+    const int tile = 1 << a.tile_shift;
+    const int64_t most = TR_MAX_BLOCKS_256 / 4; // tokens, a multiple of a window and of the tile
     for (int64_t at = 0; at < a.n_tokens; at += most) {
         const int64_t rest = std::min<int64_t>(a.n_tokens - at, most);
-        const int n_blocks = a.k ? 2 * (int)((rest + window - 1) / window) : 0, n_queries = a.q ? (int)((rest + tile - 1) / tile) : 0;
-        const dim3 grid(n_blocks + n_queries), block(THREADS);
+        const int all_parts = a.k ? (a.n_kv_heads + UNITS - 1) / UNITS : 0, n_queries = a.q ? (int)((rest + tile - 1) / tile) : 0;
+        int window = 1;
+        while (window < TR_Q8_ROWS && 2 * all_parts * ((rest + window - 1) / window) > PARTS_WGS) window *= 2;
+        const int n_windows = (int)((rest + window - 1) / window), n_parts = std::min(all_parts, std::max(PARTS_WGS / (2 * n_windows), 1));
+        const dim3 grid(2 * n_parts * n_windows + n_queries), block(THREADS);
         const bool half = layout == TR_ROPE_HALF;
-        if (half && a.stream) append_q8_kernel<DTYPE, D, true, true><<<grid, block, 0, s>>>(a, at, window, n_blocks);
-        else if (half) append_q8_kernel<DTYPE, D, true, false><<<grid, block, 0, s>>>(a, at, window, n_blocks);
-        else if (a.stream) append_q8_kernel<DTYPE, D, false, true><<<grid, block, 0, s>>>(a, at, window, n_blocks);
-        else append_q8_kernel<DTYPE, D, false, false><<<grid, block, 0, s>>>(a, at, window, n_blocks);
+        if (half && a.stream) append_q8_kernel<DTYPE, D, true, true><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts);
+        else if (half) append_q8_kernel<DTYPE, D, true, false><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts);
+        else if (a.stream) append_q8_kernel<DTYPE, D, false, true><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts);
+        else append_q8_kernel<DTYPE, D, false, false><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts);
         TR_HIP(hipGetLastError());
     }
     return TR_OK;
