@@ -513,7 +513,7 @@ template <int DTYPE, int D> static int launch_append(const TrPagedAppendArgs& a,
 {
     constexpr int THREADS = append_q8_threads(DTYPE, D), UNITS = append_q8_units(DTYPE, true);
     const int tile = 1 << a.tile_shift;
-    const int64_t most = TR_MAX_BLOCKS_256 / 4; // tokens, a multiple of a window and of the tile
+    const int64_t most = 1 << 22; // tokens, a multiple of a window and of the tile
     for (int64_t at = 0; at < a.n_tokens; at += most) {
         const int64_t rest = std::min<int64_t>(a.n_tokens - at, most);
         const int all_parts = a.k ? (a.n_kv_heads + UNITS - 1) / UNITS : 0, n_queries = a.q ? (int)((rest + tile - 1) / tile) : 0;
