@@ -30,6 +30,15 @@
 // first kernel alone 83, 6.5 TB/s); one of 131071, 32 / 8 heads, pages of 16: 90.9; 32 of up to 32000 rows through a window of 4000 and
 // 4 first tokens: 85.4 (489 MB); five of 300 to 3000 rows: 13.6; one of 700: 8.5, which is two launches and, in the first, four
 // dependent trips to memory (lengths, page ids, keys, results).
+//
+// Codes (e4m3, a power of two to a block of 16 rows and a head) take the same way.  They go to LDS as they are and become bf16 on the way to
+// the matrix unit, times their scale and exactly, by one instruction for two of them, so that products, softmax and sums are those of a
+// bf16 pool that holds what the codes are worth: the error against 64 bits is the same.  V goes through the transposing read of 8 bits; an fp32 query
+// is three bf16 parts.  Scales are asked for with the page ids that name them, a lane each, and come before the keys.  A unit is 64 keys
+// (32 and twice the waves: as fast where it is long, 71.3 / 69.8 for 200 requests of 50 to 1200 rows, 12.5 / 10.7 for five of 300 to 3000, 8.5 / 9.2 for one of 700), for
+// heads of 64 channels by twice the waves.  64 requests of 8192 rows, 28 / 4 heads: 97.3 (538 MB, 5.5 TB/s; the first kernel alone 85.7, 6.3 TB/s; only
+// the stream of it, without products, 96); one of 131071, 32 / 8 heads: 54.7 (270 MB); windows of 4000 over 32 requests: 51.7 (246 MB).  Pools that keep the
+// rows of a head together are read 3 % faster.
 #pragma once
 #include "tr_device.h"
 #include "tr_internal.h"

@@ -1,4 +1,5 @@
-// Kernels of the paged cache in 8 bits: append with head norms, rotation and quantisation; rows read back.
+// Kernels of the paged cache in 8 bits: append with head norms, rotation and quantisation; rows read back.  Times: us of a call over three
+// sets of buffers in turn, on a stream.
 #include "tr_internal.h"
 #include "tr_paged_heads.h"
 #include "tr_q8.h"
@@ -121,10 +122,21 @@ template <int N> __device__ __forceinline__ void rescale(char* unit, uint32_t ro
     }
 }
 
-// Quantised heads.  The tokens that the call writes to a block of 16 rows stand side by side, as a run, from one on whose slot lies in another
-// block than that in front of it.  A workgroup looks at `window` tokens, at most 16, and owns the runs that begin with one of them, for some of the heads of keys
-// or of values.  It works on as many runs at a time as have 16 tokens together, a row of lanes to a token.  A block's heads need two steps, the
-// largest value of all its rows and then the codes; values wait for that in registers, and the next heads are on their way.
+// Quantised heads.  The scale of a block is 2^e with the smallest e that holds its largest value, so a head takes two steps: the largest
+// value of all rows of the block, then the codes.  A power of two costs no precision, as codes are floating-point numbers, and lets rows
+// that a block holds already go over to a larger scale without a second rounding unless they are small.
+//
+// Work.  The tokens that the call writes to a block stand side by side, as a run, from one on whose slot lies in another block than that in
+// front of it.  A workgroup looks at `window` tokens, at most 16, and owns the runs that begin with one of them, for some of the heads of keys or
+// of values.  It works on as many runs at a time as have 16 tokens together, a row of lanes to a token, so that a prompt's blocks and
+// single tokens of many requests fill it alike: nobody has to know which they are.  (Runs one after another: 1024 requests of a
+// token, 8 heads of 128, 41 us, 10.4 so; a workgroup for each token: 13.8, and 58 for four prompts of 1024, 22.9 so.)
+//
+// Bound by memory where tokens are many: 16000 of 32 / 8 heads (384 of padding), 367 MB, 74.9, 4.9 TB/s, a copy of as many bytes 73; queries alone 51, keys and
+// values alone 31, which is half vector instructions and half the chain of slots, heads, barrier, codes, hidden only by other workgroups.  So
+// registers count: values wait as they come and keys in fp32, two heads at a time (154 registers, three workgroups to a compute unit; four
+// heads at a time took 104.5), and no head is on its way for longer than the one in front of it.  64 tokens of 28 / 4 heads 4.5, one token 4.5, of
+// which a launch is 3.3.
 // Heads that a thread has part in at a time: 16 channels of keys, which it holds in fp32, 32 of values, which it holds as they come.
 constexpr int append_q8_units(int dtype, bool keys) { return (dtype == TR_F32 ? 4 : 2) * (keys ? 1 : 2); }
 // The largest values of a step's runs and heads; what one step reads the next but one clears.
@@ -348,22 +360,27 @@ __device__ __forceinline__ void append_queries(const TrPagedAppendArgs& a, float
     }
 }
 
-// Keys and values by separate workgroups, which have half as much to hold, and in front of the queries', as they take longer.
+// Keys and values by separate workgroups, which have half as much to hold.  They come first, as they take longer than the queries', or, where a
+// launch has many rounds of workgroups, evenly among them, so that the ones' chains overlap with the others' stream.  First / among: a prompt of
+// 512 7.2 / 9.4, 1024 requests of a token 10.4 / 13.1, four prompts of 1024 22.9 / 22.6, eight 39.8 / 38.3, 16000 tokens 77.2 / 74.9.
 template <int DTYPE, int D, bool HALF, bool STREAM>
-__global__ __launch_bounds__(append_q8_threads(DTYPE, D), DTYPE == TR_BF16 ? 3 : 2) void append_q8_kernel(const TrPagedAppendArgs a, int64_t first, int window, int n_windows, int n_parts)
+__global__ __launch_bounds__(append_q8_threads(DTYPE, D), DTYPE == TR_BF16 ? 3 : 2) void append_q8_kernel(const TrPagedAppendArgs a, int64_t first, int window, int n_windows, int n_parts, int spread)
 {
     constexpr int THREADS = append_q8_threads(DTYPE, D);
     __shared__ float2 turn[TR_Q8_ROWS * 64]; // cosine and sine of each token's pairs, times the amplitude
     __shared__ Tops<DTYPE, D> tops[3];
     __shared__ int slots[2 * TR_Q8_ROWS];
-    const int block = blockIdx.x, part = block / n_windows; // parts of the heads of keys, then of values
-    if (part < 2 * n_parts) {
+    const int n_blocks = 2 * n_parts * n_windows, at = blockIdx.x;
+    auto among = [&](int n) { return spread ? (int)((uint64_t)n * n_blocks / gridDim.x) : min(n, n_blocks); }; // the first n workgroups
+    const int block = among(at);
+    if (among(at + 1) > block) {
+        const int part = block / n_windows; // parts of the heads, of keys and of values in turn
         const int p = part >> 1, per = (a.n_kv_heads + n_parts - 1) / n_parts;
         const int first_head = p * per, end_head = min(first_head + per, a.n_kv_heads);
         const int64_t t0 = first + (int64_t)(block - part * n_windows) * window;
         if (part & 1) append_blocks<DTYPE, D, HALF, THREADS, false>(a, turn, tops, slots, t0, window, first_head, end_head);
         else append_blocks<DTYPE, D, HALF, THREADS, true>(a, turn, tops, slots, t0, window, first_head, end_head);
-    } else append_queries<DTYPE, D, HALF, STREAM, THREADS>(a, turn, (first >> a.tile_shift) + block - 2 * n_parts * n_windows);
+    } else append_queries<DTYPE, D, HALF, STREAM, THREADS>(a, turn, (first >> a.tile_shift) + at - block);
 }
 
 // Largest i of 64 lanes with starts <= x, for ascending starts; -1 if there is none.
@@ -382,10 +399,11 @@ __device__ __forceinline__ int64_t lane_of(int64_t x, int lane)
     return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
 }
 
-// Rows of the requests.  Bound by memory, and by a chain of trips to it before the first code is asked for: the requests' first rows, a
-// length and a page id, codes and scales.  A wave takes `rows` rows, a lane looks up one of them, and then each lane makes 16 bytes of
-// result at a time of READ_UNITS units of keys and as many of values.
-constexpr int READ_UNITS = 4;
+// Rows of the requests.  Bound by memory, two bytes written for each that is read (bf16), and by a chain of trips to it before the first code is
+// asked for: the requests' first rows, a length and a page id, codes and scales.  A wave takes `rows` rows, as many as its lanes have units of, a
+// lane looks up one of them, and then each lane makes 16 bytes of keys and of values at a time, so that stores are whole lines.  Many waves with
+// little each: with one / two / four such units to a lane at a time 16 requests of 300 to 9000 rows, 8 heads of 128 channels, 478 MB, take 84.0 (5.7 TB/s) /
+// 92.9 / 95.8, nine fp32 ones of up to 2500 5.6 / 6.1 / 6.4, one of 700 rows 4.8 / 5.0 / 5.3 (16 codes to a lane and a search by each workgroup: 110.5, 7.6, 4.0).
 template <int DTYPE, int D, bool STREAM>
 __global__ __launch_bounds__(256) void read_q8_kernel(const TrPagedReadArgs a, int64_t first)
 {
@@ -447,66 +465,56 @@ __global__ __launch_bounds__(256) void read_q8_kernel(const TrPagedReadArgs a, i
     const uint64_t unit0 = (uint64_t)t0 * per_row;
     const bool even = per_row % 64 == 0; // then a wave's units are of one row
     int r = 0, in = 0;                    // that row and its first unit
-    for (int u0 = lane; u0 - lane < units; u0 += 64 * READ_UNITS) {
-        uint32_t w[2][READ_UNITS][N / 4];
-        int s[2][READ_UNITS];
-        bool mine[READ_UNITS];
+    for (int u = lane; u - lane < units; u += 64) {
+        int64_t at, sc;
+        int unit; // of the row
+        if (even) {
+            at = lane_of(from, r), sc = lane_of(scale, r);
+            unit = in + lane;
+            in += 64;
+            if (in == per_row) in = 0, ++r;
+        } else {
+            const int row = (uint32_t)u / (uint32_t)per_row;
+            at = __shfl(from, row & 63), sc = __shfl(scale, row & 63);
+            unit = u - row * per_row;
+        }
+        if (u >= units || at == -2) continue;
+        const int head = unit / PER_HEAD;
+        uint32_t w[2][N / 4] = {};
+        int s[2] = {127, 127};
 #pragma unroll
-        for (int i = 0; i < READ_UNITS; ++i) {
-            const int u = u0 + 64 * i;
-            int at_head;
-            int64_t at, sc;
-            if (even) {
-                at = lane_of(from, r), sc = lane_of(scale, r);
-                at_head = in + lane;
-                in += 64;
-                if (in == per_row) in = 0, ++r;
-            } else {
-                const int row = (uint32_t)u / (uint32_t)per_row;
-                at = __shfl(from, row & 63), sc = __shfl(scale, row & 63);
-                at_head = u - row * per_row;
-            }
-            const int head = at_head / PER_HEAD;
-            mine[i] = u < units && at != -2;
-#pragma unroll
-            for (int side = 0; side < 2; ++side) {
-                s[side][i] = 127;
-#pragma unroll
-                for (int c = 0; c < N / 4; ++c) w[side][i][c] = 0;
-                if (u < units && at >= 0) {
-                    const char* const codes = (side ? a.pool.v : a.pool.k) + at + (int64_t)head * a.pool.head_stride + (at_head % PER_HEAD) * N;
-                    if constexpr (N == 8) {
-                        const uint64_t x = __builtin_nontemporal_load((const uint64_t*)codes);
-                        w[side][i][0] = (uint32_t)x, w[side][i][N / 4 - 1] = (uint32_t)(x >> 32);
-                    } else w[side][i][0] = __builtin_nontemporal_load((const uint32_t*)codes);
-                    s[side][i] = (side ? a.pool.v_scale : a.pool.k_scale)[sc + ((int64_t)head << scale_shift)];
-                }
-            }
+        for (int side = 0; side < 2; ++side) {
+            if (at < 0) continue;
+            const char* const codes = (side ? a.pool.v : a.pool.k) + at + (int64_t)head * a.pool.head_stride + (unit % PER_HEAD) * N;
+            if constexpr (N == 8) {
+                const uint64_t x = STREAM ? __builtin_nontemporal_load((const uint64_t*)codes) : *(const uint64_t*)codes;
+                w[side][0] = (uint32_t)x, w[side][N / 4 - 1] = (uint32_t)(x >> 32);
+            } else w[side][0] = STREAM ? __builtin_nontemporal_load((const uint32_t*)codes) : *(const uint32_t*)codes;
+            s[side] = (side ? a.pool.v_scale : a.pool.k_scale)[sc + ((int64_t)head << scale_shift)];
         }
 #pragma unroll
-        for (int i = 0; i < READ_UNITS; ++i) {
-            if (!mine[i]) continue;
+        for (int side = 0; side < 2; ++side) {
+            const float by = q8_power(s[side] - 127);
+            float x[N];
 #pragma unroll
-            for (int side = 0; side < 2; ++side) {
-                const float by = q8_power(s[side][i] - 127);
-                float x[N];
+            for (int c = 0; c < N; c += 4) {
+                float y[4];
+                q8_decode(w[side][c / 4], y);
 #pragma unroll
-                for (int c = 0; c < N; c += 4) {
-                    float y[4];
-                    q8_decode(w[side][i][c / 4], y);
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) x[c + b] = y[b] * by;
-                }
-                u32x4* const to = (u32x4*)((side ? a.out_v : a.out_k) + (unit0 + u0 + 64 * i) * 16);
-                if (STREAM) __builtin_nontemporal_store(V::close(x), to);
-                else *to = V::close(x);
+                for (int b = 0; b < 4; ++b) x[c + b] = y[b] * by;
             }
+            u32x4* const to = (u32x4*)((side ? a.out_v : a.out_k) + (unit0 + u) * 16);
+            if (STREAM) __builtin_nontemporal_store(V::close(x), to);
+            else *to = V::close(x);
         }
     }
 }
 
 } // namespace
 
+// Workgroups of quantised heads that a launch is cut into where tokens are few: first windows of fewer than 16 tokens, then parts of the heads.
+// us with windows of 16 always / this: 64 tokens 6.3 / 5.4, a prompt of 512 8.7 / 7.2, six short fp32 prompts 10.1 / 6.3; with 512 / 1024 of them: two
+// prompts of 1024 15.5 / 18.4, four 22.9 / 24.6, 4096 requests of a token 22.8 / 25.8, 1024 10.4 / 10.4.
 static constexpr int PARTS_WGS = 512;
 // A launch takes a part of the tokens, as it has fewer than 2^32 threads.
 template <int DTYPE, int D> static int launch_append(const TrPagedAppendArgs& a, int layout, hipStream_t s)
@@ -522,10 +530,10 @@ template <int DTYPE, int D> static int launch_append(const TrPagedAppendArgs& a,
         const int n_windows = (int)((rest + window - 1) / window), n_parts = std::min(all_parts, std::max(PARTS_WGS / (2 * n_windows), 1));
         const dim3 grid(2 * n_parts * n_windows + n_queries), block(THREADS);
         const bool half = layout == TR_ROPE_HALF;
-        if (half && a.stream) append_q8_kernel<DTYPE, D, true, true><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts);
-        else if (half) append_q8_kernel<DTYPE, D, true, false><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts);
-        else if (a.stream) append_q8_kernel<DTYPE, D, false, true><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts);
-        else append_q8_kernel<DTYPE, D, false, false><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts);
+        if (half && a.stream) append_q8_kernel<DTYPE, D, true, true><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, rest > 4096);
+        else if (half) append_q8_kernel<DTYPE, D, true, false><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, rest > 4096);
+        else if (a.stream) append_q8_kernel<DTYPE, D, false, true><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, rest > 4096);
+        else append_q8_kernel<DTYPE, D, false, false><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, rest > 4096);
         TR_HIP(hipGetLastError());
     }
     return TR_OK;
@@ -539,9 +547,11 @@ int tr_launch_paged_append_q8(const TrPagedAppendArgs& a, int dtype, int head_di
 template <int DTYPE, int D> static int launch_read(TrPagedReadArgs a, hipStream_t s)
 {
     const int per_row = a.n_kv_heads * (D / Vec<DTYPE>::N);
-    a.rows = std::min(std::max(64 * READ_UNITS / per_row, 1), 64);
+    a.rows = std::min(std::max(64 / per_row, 1), 64);
     const int64_t most = (int64_t)TR_MAX_BLOCKS_256 * 4 * a.rows;
-    const bool stream = 2 * 16ll * per_row * a.n_rows >= 150ll << 20;
+    // Streamed loads and stores make the call itself faster, and what reads its results, or the pages, next slower where the caches still hold them.  us of
+    // the call and a pass over all it wrote, ordinary / streamed, by MB written: 46 MB 47.2 / 50.7, 93 MB 68.4 / 79.2, 187 MB 120.5 / 128.4, 375 MB 234.0 / 230.7.
+    const bool stream = 2 * 16ll * per_row * a.n_rows >= 256ll << 20;
     for (int64_t at = 0; at < a.n_rows; at += most) {
         const dim3 blocks((uint32_t)((std::min<int64_t>(a.n_rows - at, most) + 4 * a.rows - 1) / (4 * a.rows)));
         if (stream) read_q8_kernel<DTYPE, D, true><<<blocks, dim3(256), 0, s>>>(a, at);
