@@ -92,9 +92,9 @@ int main(int, char** argv)
     auto read = [&](int32_t n_req, int32_t rows) {
         return CALL(tr_paged_read_q8)(&s, &p, idx, 100, (const int32_t*)at(31), (const int32_t*)at(32), n_req, at(34), at(36), rows, nullptr);
     };
-    check("read, one row", read(1, 1), 1, 1); // a head of 128 channels: 16 units, 16 rows to a wave
-    check("read, 65536 requests", read(65536, 65), 2, 1);
-    check("read, 2^31 - 1 rows", read(3, INT32_MAX), 1 << 25, 3);
+    check("read, one row", read(1, 1), 1, 1); // a head of 128 channels: 16 units, 4 rows to a wave
+    check("read, 65536 requests", read(65536, 65), 5, 1);
+    check("read, 2^31 - 1 rows", read(3, INT32_MAX), 1 << 27, 9);
     s.n_q_heads = s.n_kv_heads = p.n_kv_heads = 32;
     check("read, rows of 512 units", read(3, 1000), 250, 1);
     s.n_q_heads = s.n_kv_heads = p.n_kv_heads = 1;
