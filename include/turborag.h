@@ -448,7 +448,7 @@ int tr_paged_read_q8(const tr_shape* shape, const tr_pages_q8* pages, const int3
                      const int32_t* kv_lens /*device*/, const int32_t* row_start /*device*/, int32_t n_req, void* out_k, void* out_v,
                      int32_t n_rows, void* stream);
 
-/* tr_paged_decode_attn over such a pool: the same arguments, masks, guarantees and limits (units of 32 keys for both types).  Keys
+/* tr_paged_decode_attn over such a pool: the same arguments, masks, guarantees and limits (units of 64 keys for both types).  Keys
  * and values enter the products as they are worth, exactly; queries, weights, scores and sums are fp32 or what the type holds.  A visible
  * NaN makes its head's (key) or its channel's (value) results NaN. */
 size_t tr_paged_decode_attn_q8_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size);
