@@ -135,8 +135,7 @@ template <int N> __device__ __forceinline__ void rescale(char* unit, uint32_t ro
 // Bound by memory where tokens are many: 16000 of 32 / 8 heads (384 of padding), 367 MB, 74.9, 4.9 TB/s, a copy of as many bytes 73; queries alone 51, keys and
 // values alone 31, which is half vector instructions and half the chain of slots, heads, barrier, codes, hidden only by other workgroups.  So
 // registers count: values wait as they come and keys in fp32, two heads at a time (154 registers, three workgroups to a compute unit; four
-// heads at a time took 104.5), and no head is on its way for longer than the one in front of it.  64 tokens of 28 / 4 heads 4.5, one token 4.5, of
-// which a launch is 3.3.
+// heads at a time took 104.5), and only the next two are on their way.  64 tokens of 28 / 4 heads 4.5, one token 4.5, of which a launch is 3.3.
 // Heads that a thread has part in at a time: 16 channels of keys, which it holds in fp32, 32 of values, which it holds as they come.
 constexpr int append_q8_units(int dtype, bool keys) { return (dtype == TR_F32 ? 4 : 2) * (keys ? 1 : 2); }
 // The largest values of a step's runs and heads; what one step reads the next but one clears.
@@ -279,8 +278,8 @@ __device__ __forceinline__ void append_blocks(const TrPagedAppendArgs& a, float2
                 if (to >= Q8_MOST) // the largest numbers would round to what fp32 has not
 #pragma unroll
                     for (int c = 0; c < N; ++c) {
-                        const float most = 1.875f * q8_power(127 - to);
-                        if (fabsf(y[c]) > most && fabsf(y[c]) < 256.0f) y[c] = copysignf(most, y[c]);
+                        const float limit = 1.875f * q8_power(127 - to);
+                        if (fabsf(y[c]) > limit && fabsf(y[c]) < 256.0f) y[c] = copysignf(limit, y[c]);
                     }
                 char* const block_rows = rows + (int64_t)head * a.pool.head_stride;
                 put<N>(block_rows + (int64_t)row * a.pool.row_stride, y);
