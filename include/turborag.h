@@ -450,7 +450,8 @@ int tr_paged_read_q8(const tr_shape* shape, const tr_pages_q8* pages, const int3
 
 /* tr_paged_decode_attn over such a pool: the same arguments, masks, guarantees and limits (units of 64 keys for both types).  Keys
  * and values enter the products as they are worth, exactly; queries, weights, scores and sums are fp32 or what the type holds.  A visible
- * NaN makes its head's (key) or its channel's (value) results NaN. */
+ * NaN makes its head's (key) or its channel's (value) results NaN.  How a batch is shared out, and with it the last bits, also depends on
+ * whether heads of 64 channels lie beside each other in a line of 128 bytes. */
 size_t tr_paged_decode_attn_q8_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size);
 int tr_paged_decode_attn_q8(const tr_shape* shape, const void* q, const tr_pages_q8* pages, const int32_t* block_table /*device*/,
                             int32_t max_blocks, const int32_t* kv_lens /*device*/, int32_t n_req, int32_t window, int32_t n_sink,

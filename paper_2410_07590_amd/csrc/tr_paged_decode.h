@@ -623,7 +623,27 @@ __global__ __launch_bounds__(64, NT == 1 || WORKERS > 1024 ? 2 : 1) void paged_d
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int lane = threadIdx.x, c16 = lane & 15, quad = lane >> 4;
     const int tiles = (a.group + ROWS - 1) / ROWS, per_req = a.n_kv_heads * tiles; // items of a request
-    const int worker = blockIdx.x;
+    // A wave takes the share `turn` of the batch's items.  Where two heads lie in one line they make one item for the shares, and two waves of
+    // one die take the same share, a head each, so that the line is fetched once: a wave and the one eight workgroups on.  Waves are counted
+    // so that those which have pieces of one head stand side by side.  us with heads shared out by themselves / so, 16 / 4 heads of 64 channels: 91 requests of 3700
+    // to 11300 rows 120.4 / 83.8, three of 41000 to 90000 38.7 / 26.4, 64 of 500 to 4000 33.2 / 23.8, 64 of 4000 (where the two were eight apart anyway) 38.9 / 38.9.
+    int worker = blockIdx.x, turn = worker, member = 0;
+    bool paired = false;
+    if constexpr (R::HALF_LINES) {
+        paired = a.pool.head_stride < 128 && a.n_kv_heads % 2 == 0 && tiles == 1 && gridDim.x % 2 == 0;
+        if (paired) {
+            const int half = gridDim.x / 2, full = half & ~7;
+            if (worker < 2 * full) {
+                turn = (worker >> 4) * 8 + (worker & 7);
+                member = (worker >> 3) & 1;
+            } else {
+                turn = full + ((worker - 2 * full) >> 1);
+                member = worker & 1;
+            }
+            worker = member * half + turn;
+        }
+    }
+    const int share_items = paired ? per_req / 2 : per_req, turns = paired ? WORKERS / 2 : WORKERS;
 
     // the batch's units, and the request that this wave's share begins in: a lane sums up `per` neighbouring requests
     auto len_of = [&](int r) { return r < a.n_req ? a.kv_lens[r] : 0; };
@@ -638,9 +658,9 @@ __global__ __launch_bounds__(64, NT == 1 || WORKERS > 1024 ? 2 : 1) void paged_d
         for (int j = 0; j < 8; ++j) own += i + j < per ? units_of(lane * per + i + j, l[j]) : 0;
     }
     int sums = wave_scan(own);
-    const int total = __builtin_amdgcn_readlane(sums, 63) * per_req;
-    const int share = max((total + WORKERS - 1) / WORKERS, TR_PAGED_MIN_UNITS);
-    const int begin = share * worker;
+    const int total = __builtin_amdgcn_readlane(sums, 63) * share_items;
+    const int share = max((total + turns - 1) / turns, TR_PAGED_MIN_UNITS);
+    const int begin = share * turn;
     // who has pieces of the cut items, by the item or by the wave that begins it (a share begins at most one)
     auto record = [&](int64_t at, int x, int pieces) {
         if (lane == 0) *(int2*)(a.ws_items + 2 * at) = make_int2(x, pieces);
@@ -651,7 +671,7 @@ __global__ __launch_bounds__(64, NT == 1 || WORKERS > 1024 ? 2 : 1) void paged_d
     }
     const int end = min(begin + share, total);
     int left = end - begin; // behind the pieces described so far
-    const int unit = begin / per_req; // in units of all heads together
+    const int unit = begin / share_items; // in units of all heads together
     int at = __builtin_ctzll(__ballot(sums > unit)), r0 = 0;
     int before = __builtin_amdgcn_readlane(sums, at) - __builtin_amdgcn_readlane(own, at);
     if (per > 1) { // one of that lane's
@@ -671,12 +691,12 @@ __global__ __launch_bounds__(64, NT == 1 || WORKERS > 1024 ? 2 : 1) void paged_d
     P p;
     p.r = min(r0 + at, a.n_req - 1);
     p.w = walk_of<R::UNIT>(a, __builtin_amdgcn_readlane(lens, at));
-    const int local = begin - before * per_req;
+    const int local = begin - before * share_items;
     p.item = uniform(local / p.w.units);
     p.u0 = local - p.item * p.w.units;
     auto place = [&](P& x) {
-        x.kvh = tiles == 1 ? x.item : uniform(x.item / tiles);
-        x.tile = x.item - x.kvh * tiles;
+        x.kvh = paired ? 2 * x.item + member : tiles == 1 ? x.item : uniform(x.item / tiles);
+        x.tile = paired ? 0 : x.item - x.kvh * tiles;
     };
     place(p);
     p.n = min(p.w.units - p.u0, left);
@@ -685,7 +705,7 @@ __global__ __launch_bounds__(64, NT == 1 || WORKERS > 1024 ? 2 : 1) void paged_d
         P x = from;
         x.u0 = x.n = 0;
         if (left == 0) return x;
-        if (++x.item == per_req) {
+        if (++x.item == share_items) {
             if (x.r + 1 == a.n_req) { // not reached unless the lengths are written meanwhile
                 x.item = left = 0;
                 return x;
@@ -761,11 +781,12 @@ __global__ __launch_bounds__(64, NT == 1 || WORKERS > 1024 ? 2 : 1) void paged_d
             }
             if (!whole && quad == 0) *(float2*)(a.ws_ml + slot * 2) = make_float2(acc.m[t], l);
         }
-        const int pieces = p.whole() || p.u0 ? 1 : (end - left - then.n - p.n + p.w.units - 1) / share - worker + 1; // of the item that begins here
+        const int item = paired ? 2 * p.item + member : p.item; // of the request's
+        const int pieces = p.whole() || p.u0 ? 1 : (end - left - then.n - p.n + p.w.units - 1) / share - turn + 1; // of the item that begins here
         if (a.cut == TR_PAGED_JOIN_BY_WAVE) {
-            if (then.n == 0) record(worker, p.r * per_req + p.item, pieces);
+            if (then.n == 0) record(worker, p.r * per_req + item, pieces);
         } else if (a.cut && p.u0 == 0) {
-            record((int64_t)p.r * per_req + p.item, worker, pieces);
+            record((int64_t)p.r * per_req + item, worker, pieces);
         }
         if (then.n == 0) break;
         p = then;

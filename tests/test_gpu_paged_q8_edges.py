@@ -8,6 +8,7 @@ from tests import paged_q8_reference as Q
 from tests import paged_reference as R
 from tests.test_gpu_paged import DT, ints, randn, tables
 from tests.test_gpu_paged_q8 import EPS, Pool, check_append, check_read
+from tests.test_gpu_paged_q8_decode import check as check_decode
 from tests.test_gpu_paged_q8_decode import run
 
 pytestmark = pytest.mark.gpu
@@ -151,3 +152,27 @@ def test_queries_are_those_of_the_append_in_the_shapes_type(B, dt, d, rot, layou
         B.tr_paged_append_q8(gs, rotary, q, None, None, norm, None, EPS, pos, None, b, None)
         torch.cuda.synchronize()
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hk", [(2, 2), (3, 3), (8, 4), (6, 6), (20, 10), (36, 2), (80, 2)])
+@pytest.mark.parametrize("order", ["rows", "wide", "heads"])
+def test_decode_heads_that_share_lines(B, dt, hq, hk, order):
+    """64 channels: pairs of heads are shared out together where they lie in one line.  Few units and many, shares that cut items and that do not."""
+    rng = np.random.default_rng(hq)
+    for lens in ([1], [64], [65], [130, 0, 1], [700], list(rng.integers(0, 300, 9)), list(rng.integers(0, 200, 150)), [9000, 3], [64 * 40] * 13):
+        check_decode(B, dt, hq, hk, 64, [int(x) for x in lens], page=32, order=order, seed=len(lens), hide=len(lens) < 20)
+    check_decode(B, dt, hq, hk, 64, [5000, 70, 900], page=16, order=order, window=700, sinks=70, seed=5)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_decode_bits_do_not_depend_on_the_tables_width(B, dt, d):
+    lens = [5000, 1, 777, 2000]
+    table, n_pages = tables(np.random.default_rng(1), lens, 16)
+    (k, ks), (v, vs) = (Q.random_pool(n_pages, 16, 2, d, i) for i in (1, 2))
+    q = randn(4, 8, d, seed=5, dtype=DT[dt]).cuda()
+    gs, pool = B.make_shape(8, 2, d, dt, 1e4), (k.cuda(), v.cuda(), ks.cuda(), vs.cuda())
+    want = run(B, gs, q, *pool, ints(table), ints(lens))
+    for more in (1, 7, 300):   # columns that no length reaches
+        assert torch.equal(want, run(B, gs, q, *pool, ints(np.concatenate([table, np.full((4, more), 7)], 1)), ints(lens)))
