@@ -449,7 +449,8 @@ int tr_paged_read_q8(const tr_shape* shape, const tr_pages_q8* pages, const int3
                      int32_t n_rows, void* stream);
 
 /* tr_paged_decode_attn over such a pool: the same arguments, masks, guarantees and limits (units of 64 keys for both types).  Keys
- * and values enter the products as they are worth, exactly; queries, weights, scores and sums are fp32 or what the type holds.  A visible
+ * and values enter the products as they are worth, exactly; queries, weights, scores and sums are fp32 or what the type holds (of an
+ * fp32 query head with a channel of 2^-32 or more, channels are taken to multiples of 2^-133, towards zero).  A visible
  * NaN makes its head's (key) or its channel's (value) results NaN.  How a batch is shared out, and with it the last bits, also depends on
  * whether heads of 64 channels lie beside each other in a line of 128 bytes. */
 size_t tr_paged_decode_attn_q8_workspace_size(const tr_shape* shape, int32_t n_req, int32_t max_blocks, int32_t page_size);

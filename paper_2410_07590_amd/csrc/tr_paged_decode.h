@@ -303,11 +303,26 @@ template <int FMT, int D> struct Stream {
                                              (LDS_AS void*)(uintptr_t)(qring + i * 1024), 16, 0, 0);
     }
     // Codes: step 2 j + h of a product is channels 64 j + 16 quad + 8 h + 0 .. 7, a lane's share of which is half of a 16-byte unit.  An fp32
-    // query is three bf16 parts there, which together are it, so that its products are exact like those of a bf16 one.
-    template <int NT> __device__ __forceinline__ void take_q(Op (&q)[NT][R::KS][R::QPARTS]) const
+    // query is three bf16 parts there, which together are it, so that its products are exact like those of a bf16 one.  bf16 ends at 2^-133, fp32
+    // at 2^-149: a query head whose channels are all below 2^-32 is taken 2^24 times as large, which `by`, a factor on its scores, takes
+    // back (scores stay below 2^-8 2^128 d).
+    template <int NT> __device__ __forceinline__ void take_q(Op (&q)[NT][R::KS][R::QPARTS], float (&by)[NT]) const
     {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t) {
+            [[maybe_unused]] float lift = 1.0f;
+            if constexpr (FMT == FMT_Q8_F32) {
+                const uint32_t row = qring + (uint32_t)((16 * t + (lane & 15)) * R::QROW + (lane >> 4) * 16);
+                float top = 0.0f; // every channel is in one of the column's four lanes
+#pragma unroll
+                for (int c = 0; c < R::QCPR / 4; ++c) {
+                    const f32x4 x = *(LDS_AS const f32x4*)(uintptr_t)(row + 64 * c);
+                    top = fmaxf(fmaxf(top, fmaxf(fabsf(x[0]), fabsf(x[1]))), fmaxf(fabsf(x[2]), fabsf(x[3])));
+                }
+                const bool small = column_reduce<true>(top) < 0x1p-32f;
+                lift = small ? 0x1p24f : 1.0f;
+                by[t] = small ? 0x1p-24f : 1.0f;
+            } else by[t] = 1.0f;
 #pragma unroll
             for (int ks = 0; ks < R::KS; ++ks) {
                 const uint32_t row = qring + (uint32_t)((16 * t + (lane & 15)) * R::QROW);
@@ -319,7 +334,7 @@ template <int FMT, int D> struct Stream {
                     u32x4 part[3];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float a = x[2 * i], b = x[2 * i + 1];
+                        float a = x[2 * i] * lift, b = x[2 * i + 1] * lift;
 #pragma unroll
                         for (int j = 0; j < 3; ++j) {
                             const uint32_t ua = __float_as_uint(a) & 0xffff0000u, ub = __float_as_uint(b) & 0xffff0000u;
@@ -339,6 +354,7 @@ template <int FMT, int D> struct Stream {
                     asm volatile("" : "+v"(q[t][ks][0]) : : "memory");
                 }
             }
+        }
     }
     __device__ __forceinline__ Ref ref(const P& p, int j, int ids) const
     {
@@ -383,7 +399,7 @@ template <int FMT, int D, int NT>
 __device__ __forceinline__ void walk_units(const char* __restrict__ k, const char* __restrict__ v, const int32_t* __restrict__ table,
                                            const Stream<FMT, D>& st, const Piece<Rows<FMT, D>::UNIT>& p, const Piece<Rows<FMT, D>::UNIT>& then,
                                            const char* __restrict__ then_q, int then_rows,
-                                           const typename Operand<FMT>::T (&q)[NT][Rows<FMT, D>::KS][Rows<FMT, D>::QPARTS], const TrScales& sc, float scale, bool first, int& ids, UnitRef<Rows<FMT, D>::UNIT>& cur, Acc<D, NT>& acc)
+                                           const typename Operand<FMT>::T (&q)[NT][Rows<FMT, D>::KS][Rows<FMT, D>::QPARTS], const TrScales& sc, const float (&scale)[NT], bool first, int& ids, UnitRef<Rows<FMT, D>::UNIT>& cur, Acc<D, NT>& acc)
 {
     using R = Rows<FMT, D>;
     typedef typename Operand<FMT>::T Op;
@@ -496,7 +512,7 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             // A weight is 2^((s - m) scale), the difference first: it is exact or nearly so however large the scores are, where that of
             // two products with the scale would be off by their roundings.  No weight exceeds 1, so that values near the largest do not overflow.
             if (__any(top > acc.m[n])) {
-                const float to = fmaxf(acc.m[n], column_reduce<true>(top)), alpha = __builtin_amdgcn_exp2f((acc.m[n] - to) * scale);
+                const float to = fmaxf(acc.m[n], column_reduce<true>(top)), alpha = __builtin_amdgcn_exp2f((acc.m[n] - to) * scale[n]);
                 acc.m[n] = to;
                 acc.l[n] *= alpha;
 #pragma unroll
@@ -507,7 +523,7 @@ __device__ __forceinline__ void walk_units(const char* __restrict__ k, const cha
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < 4 * KB; ++i) {
-                const float w = __builtin_amdgcn_exp2f((s[n][i >> 2][i & 3] - acc.m[n]) * scale);
+                const float w = __builtin_amdgcn_exp2f((s[n][i >> 2][i & 3] - acc.m[n]) * scale[n]);
                 sum += w;
                 s[n][i >> 2][i & 3] = w;
             }
@@ -742,7 +758,10 @@ __global__ __launch_bounds__(64, NT == 1 || WORKERS > 1024 ? 2 : 1) void paged_d
         const P then = following(p);
         typename Operand<FMT>::T q[NT][R::KS][R::QPARTS];
         asm volatile("" ::: "memory");
-        st.template take_q<NT>(q);
+        float by[NT], scale[NT];
+        st.template take_q<NT>(q, by);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) scale[t] = by[t] * a.scale_log2e;
         Acc<D, NT> acc;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -751,7 +770,7 @@ __global__ __launch_bounds__(64, NT == 1 || WORKERS > 1024 ? 2 : 1) void paged_d
 #pragma unroll
             for (int cb = 0; cb < D / 16; ++cb) acc.o[t][cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        walk_units<FMT, D, NT>(a.pool.k, a.pool.v, a.table, st, p, then, first_q(then), rows_of(then), q, sc, a.scale_log2e, first, ids, cur, acc);
+        walk_units<FMT, D, NT>(a.pool.k, a.pool.v, a.table, st, p, then, first_q(then), rows_of(then), q, sc, scale, first, ids, cur, acc);
         if (then.n) st.template issue<true, false>(a.pool.v, cur, ids);
         asm volatile("" ::: "memory");
 
@@ -779,7 +798,7 @@ __global__ __launch_bounds__(64, NT == 1 || WORKERS > 1024 ? 2 : 1) void paged_d
                     *(f32x4*)(to + 16 * b + 16 * quad + 4 * e) = f32x4{o[b][e], o[b + 1][e], o[b + 2][e], o[b + 3][e]} * f;
                 }
             }
-            if (!whole && quad == 0) *(float2*)(a.ws_ml + slot * 2) = make_float2(acc.m[t], l);
+            if (!whole && quad == 0) *(float2*)(a.ws_ml + slot * 2) = make_float2(acc.m[t] == NOTHING ? NOTHING : acc.m[t] * by[t], l);
         }
         const int item = paired ? 2 * p.item + member : p.item; // of the request's
         const int pieces = p.whole() || p.u0 ? 1 : (end - left - then.n - p.n + p.w.units - 1) / share - turn + 1; // of the item that begins here
