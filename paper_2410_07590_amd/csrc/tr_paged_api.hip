@@ -312,17 +312,23 @@ int append_args(const char* who, const tr_shape* shape, const tr_rotary* rotary,
     a.eps = (float)eps;
     return TR_OK;
 }
-void append_tiles(TrPagedAppendArgs& a, const tr_shape* shape, int64_t heads) // of a token, in the pass over heads
+// heads: of a token, in the pass over heads; streamed: bytes of them from which on stores are streamed
+void append_tiles(TrPagedAppendArgs& a, const tr_shape* shape, int64_t heads, int64_t streamed)
 {
     // A workgroup takes as many tokens as give its threads eight units each, if there are workgroups enough then.  us for 1 token /
     // this: 24000 rows of 4 KV heads of 128 44.6 / 23.6, 16000 tokens of 16 + 4 heads of 64 47.6 / 23.9, 16001 of 32 + 8 of 128 88.3 / 79.0.
+    // Over 8 bits, where the pass is that over the queries: 16000 tokens of 32 / 8 heads of 128 89.7 / 73.6, of 16 / 4 heads of 64 60.0 / 30.6.
     const int64_t units = heads * shape->head_dim * tr_elem_bytes(shape) / 16; // of a token
     while ((2 << a.tile_shift) <= TR_PAGED_APPEND_TOKENS && (units << a.tile_shift) * 2 <= 2048 && a.n_tokens >= 2048ll << a.tile_shift) ++a.tile_shift;
-    // Streamed stores make the call itself faster at any size, and what reads its results next slower where the caches still
-    // hold them: us of the call and a pass over all it wrote, ordinary / streamed, by MB written: 12 MB 18.6 / 17.9, 25 MB 27.9 / 29.4, 49 MB
-    // 45.4 / 46.8, 98 MB 78.4 / 84.1, 197 MB 151.5 / 148.0.
-    a.stream = 16 * units * a.n_tokens >= 150ll << 20;
+    a.stream = 16 * units * a.n_tokens >= streamed;
 }
+// Streamed stores make an append itself faster at any size, and what reads its results next slower where the caches still hold them.  us of the
+// call and a pass over all it wrote, ordinary / streamed, by MB written: 12 MB 18.6 / 17.9, 25 MB 27.9 / 29.4, 49 MB 45.4 / 46.8, 98 MB 78.4 / 84.1,
+// 197 MB 151.5 / 148.0.
+const int64_t STREAMED = 150ll << 20;
+// Over 8 bits, of the call and a pass over the queries, 32 / 8 heads of 128, by MiB of queries: 25 38.8 / 42.3, 100 103.3 / 121.4, 150 161.0 / 172.3, 220
+// 231.9 / 247.0, 240 267.4 / 267.4, 256 292.0 / 284.0, 320 366.9 / 350.1; 28 / 4 cross at 250, fp32 and bf16 heads of 64 at 230.
+const int64_t STREAMED_Q8 = 240ll << 20;
 } // namespace
 
 extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
@@ -336,7 +342,7 @@ extern "C" int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, c
     if (int rc = append_args("tr_paged_append", shape, rotary, q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm, eps, pos, slots, n_tokens, q_out, pages, a, layout))
         return rc;
     if (a.n_tokens == 0) return TR_OK;
-    append_tiles(a, shape, a.n_q_heads + 2ll * a.n_kv_heads);
+    append_tiles(a, shape, a.n_q_heads + 2ll * a.n_kv_heads, STREAMED);
     return tr_launch_paged_append(a, shape->dtype, shape->head_dim, layout, (hipStream_t)stream);
     });
 }
@@ -352,7 +358,7 @@ extern "C" int tr_paged_append_q8(const tr_shape* shape, const tr_rotary* rotary
     if (int rc = append_args("tr_paged_append_q8", shape, rotary, q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm, eps, pos, slots, n_tokens, q_out, pages, a, layout))
         return rc;
     if (a.n_tokens == 0) return TR_OK;
-    append_tiles(a, shape, a.n_q_heads);
+    append_tiles(a, shape, a.n_q_heads, STREAMED_Q8);
     return tr_launch_paged_append_q8(a, shape->dtype, shape->head_dim, layout, (hipStream_t)stream);
     });
 }
