@@ -360,8 +360,7 @@ __device__ __forceinline__ void append_queries(const TrPagedAppendArgs& a, float
 }
 
 // Keys and values by separate workgroups, which have half as much to hold.  They come first, as they take longer than the queries', or, where a
-// launch has many rounds of workgroups, evenly among them, so that the ones' chains overlap with the others' stream.  First / among: a prompt of
-// 512 7.2 / 9.4, 1024 requests of a token 10.4 / 13.1, four prompts of 1024 22.9 / 22.6, eight 39.8 / 38.3, 16000 tokens 77.2 / 74.9.
+// launch has many rounds of workgroups and most of them are queries', evenly among them, so that the ones' chains overlap with the others' stream.
 template <int DTYPE, int D, bool HALF, bool STREAM>
 __global__ __launch_bounds__(append_q8_threads(DTYPE, D), DTYPE == TR_BF16 ? 3 : 2) void append_q8_kernel(const TrPagedAppendArgs a, int64_t first, int window, int n_windows, int n_parts, int spread)
 {
@@ -515,6 +514,11 @@ __global__ __launch_bounds__(256) void read_q8_kernel(const TrPagedReadArgs a, i
 // us with windows of 16 always / this: 64 tokens 6.3 / 5.4, a prompt of 512 8.7 / 7.2, six short fp32 prompts 10.1 / 6.3; with 512 / 1024 of them: two
 // prompts of 1024 15.5 / 18.4, four 22.9 / 24.6, 4096 requests of a token 22.8 / 25.8, 1024 10.4 / 10.4.
 static constexpr int PARTS_WGS = 512;
+// Whether they are mixed with the queries'.  us first / mixed, 32 / 8 heads of 128: 4096 single tokens 22.2 / 23.6, 5000 25.8 / 26.4, 8192 39.7 / 39.3,
+// 16384 84.2 / 78.6; 1024 requests of 5 25.5 / 28.2; prompts of 1024, four 21.2 / 22.0, eight 38.5 / 37.8, sixteen 77.4 / 75.3.  16384 single tokens of
+// other heads of 128: 8 / 8 45.0 / 56.0, 16 / 2 41.3 / 45.0, 20 / 4 50.6 / 50.5, 24 / 4 58.9 / 54.9, 32 / 32 149.0 / 147.1; of 64: 16 / 4 31.6 / 34.8, 32 / 8 45.5 / 46.6,
+// 48 / 8 59.6 / 56.8; fp32 of 64: 4 / 4 28.1 / 38.8, 16 / 4 42.5 / 41.5, 32 / 8 81.1 / 73.4; fp32 of 128, in workgroups of 512: 16 / 4 111.9 / 112.8, 32 / 8 185.0 / 189.3.
+static constexpr int MIX_TOKENS = 8192, MIX_BYTES = 6144; // MIX_BYTES: of a token's queries
 // A launch takes a part of the tokens, as it has fewer than 2^32 threads.
 template <int DTYPE, int D> static int launch_append(const TrPagedAppendArgs& a, int layout, hipStream_t s)
 {
@@ -528,11 +532,12 @@ template <int DTYPE, int D> static int launch_append(const TrPagedAppendArgs& a,
         while (window < TR_Q8_ROWS && 2 * all_parts * ((rest + window - 1) / window) > PARTS_WGS) window *= 2;
         const int n_windows = (int)((rest + window - 1) / window), n_parts = std::min(all_parts, std::max(PARTS_WGS / (2 * n_windows), 1));
         const dim3 grid(2 * n_parts * n_windows + n_queries), block(THREADS);
+        const bool mixed = THREADS == 256 && rest >= MIX_TOKENS && (int64_t)a.n_q_heads * D * (DTYPE == TR_F32 ? 4 : 2) >= MIX_BYTES;
         const bool half = layout == TR_ROPE_HALF;
-        if (half && a.stream) append_q8_kernel<DTYPE, D, true, true><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, rest > 4096);
-        else if (half) append_q8_kernel<DTYPE, D, true, false><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, rest > 4096);
-        else if (a.stream) append_q8_kernel<DTYPE, D, false, true><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, rest > 4096);
-        else append_q8_kernel<DTYPE, D, false, false><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, rest > 4096);
+        if (half && a.stream) append_q8_kernel<DTYPE, D, true, true><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, mixed);
+        else if (half) append_q8_kernel<DTYPE, D, true, false><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, mixed);
+        else if (a.stream) append_q8_kernel<DTYPE, D, false, true><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, mixed);
+        else append_q8_kernel<DTYPE, D, false, false><<<grid, block, 0, s>>>(a, at, window, n_windows, n_parts, mixed);
         TR_HIP(hipGetLastError());
     }
     return TR_OK;
