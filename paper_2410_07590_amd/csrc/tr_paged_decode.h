@@ -310,31 +310,34 @@ template <int FMT, int D> struct Stream {
     {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            [[maybe_unused]] float lift = 1.0f;
+            const uint32_t row = qring + (uint32_t)((16 * t + (lane & 15)) * R::QROW);
+            by[t] = 1.0f;
             if constexpr (FMT == FMT_Q8_F32) {
-                const uint32_t row = qring + (uint32_t)((16 * t + (lane & 15)) * R::QROW + (lane >> 4) * 16);
-                float top = 0.0f; // every channel is in one of the column's four lanes
+                float x[R::KS][8], top = 0.0f;
 #pragma unroll
-                for (int c = 0; c < R::QCPR / 4; ++c) {
-                    const f32x4 x = *(LDS_AS const f32x4*)(uintptr_t)(row + 64 * c);
-                    top = fmaxf(fmaxf(top, fmaxf(fabsf(x[0]), fabsf(x[1]))), fmaxf(fabsf(x[2]), fabsf(x[3])));
-                }
-                const bool small = column_reduce<true>(top) < 0x1p-32f;
-                lift = small ? 0x1p24f : 1.0f;
-                by[t] = small ? 0x1p-24f : 1.0f;
-            } else by[t] = 1.0f;
-#pragma unroll
-            for (int ks = 0; ks < R::KS; ++ks) {
-                const uint32_t row = qring + (uint32_t)((16 * t + (lane & 15)) * R::QROW);
-                if constexpr (FMT == FMT_Q8_F32) {
+                for (int ks = 0; ks < R::KS; ++ks) {
                     const uint32_t at = row + (64 * (ks >> 1) + 16 * (lane >> 4) + 8 * (ks & 1)) * 4;
-                    float x[8];
-                    *(f32x4*)x = *(LDS_AS const f32x4*)(uintptr_t)at;
-                    *(f32x4*)(x + 4) = *(LDS_AS const f32x4*)(uintptr_t)(at + 16);
+                    *(f32x4*)x[ks] = *(LDS_AS const f32x4*)(uintptr_t)at;
+                    *(f32x4*)(x[ks] + 4) = *(LDS_AS const f32x4*)(uintptr_t)(at + 16);
+                }
+#pragma unroll
+                for (int ks = 0; ks < R::KS; ++ks)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[ks][i]));
+                if (__any(top < 0x1p-32f)) { // a lane has a quarter of a head's channels
+                    const bool small = column_reduce<true>(top) < 0x1p-32f;
+                    by[t] = small ? 0x1p-24f : 1.0f;
+#pragma unroll
+                    for (int ks = 0; ks < R::KS; ++ks)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[ks][i] *= small ? 0x1p24f : 1.0f;
+                }
+#pragma unroll
+                for (int ks = 0; ks < R::KS; ++ks) {
                     u32x4 part[3];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float a = x[2 * i] * lift, b = x[2 * i + 1] * lift;
+                        float a = x[ks][2 * i], b = x[ks][2 * i + 1];
 #pragma unroll
                         for (int j = 0; j < 3; ++j) {
                             const uint32_t ua = __float_as_uint(a) & 0xffff0000u, ub = __float_as_uint(b) & 0xffff0000u;
@@ -348,7 +351,10 @@ template <int FMT, int D> struct Stream {
                         q[t][ks][j] = __builtin_bit_cast(bf16x8, part[j]);
                         asm volatile("" : "+v"(q[t][ks][j]) : : "memory");
                     }
-                } else {
+                }
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < R::KS; ++ks) {
                     const uint32_t at = Q8 ? row + (64 * (ks >> 1) + 16 * (lane >> 4) + 8 * (ks & 1)) * 2 : row + (4 * ks + (lane >> 4)) * 16;
                     q[t][ks][0] = *(LDS_AS const Op*)(uintptr_t)at;
                     asm volatile("" : "+v"(q[t][ks][0]) : : "memory");
