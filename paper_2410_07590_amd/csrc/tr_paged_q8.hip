@@ -461,17 +461,12 @@ __global__ __launch_bounds__(256) void read_q8_kernel(const TrPagedReadArgs a, i
     }
     const int per_row = a.n_kv_heads * PER_HEAD, units = (int)min((int64_t)a.rows, a.n_rows - t0) * per_row; // below 2^31 as heads are at most 2^20
     const uint64_t unit0 = (uint64_t)t0 * per_row;
-    const bool even = per_row % 64 == 0; // then a wave's units are of one row
-    int r = 0, in = 0;                    // that row and its first unit
+    const bool even = per_row % 64 == 0; // then a wave has one row
+    const int64_t at0 = lane_of(from, 0), sc0 = lane_of(scale, 0);
     for (int u = lane; u - lane < units; u += 64) {
-        int64_t at, sc;
-        int unit; // of the row
-        if (even) {
-            at = lane_of(from, r), sc = lane_of(scale, r);
-            unit = in + lane;
-            in += 64;
-            if (in == per_row) in = 0, ++r;
-        } else {
+        int64_t at = at0, sc = sc0;
+        int unit = u; // of the row
+        if (!even) {
             const int row = (uint32_t)u / (uint32_t)per_row;
             at = __shfl(from, row & 63), sc = __shfl(scale, row & 63);
             unit = u - row * per_row;
