@@ -375,6 +375,7 @@ __global__ __launch_bounds__(append_q8_threads(DTYPE, D), DTYPE == TR_BF16 ? 3 :
         const int part = block / n_windows; // parts of the heads, of keys and of values in turn
         const int p = part >> 1, per = (a.n_kv_heads + n_parts - 1) / n_parts;
         const int first_head = p * per, end_head = min(first_head + per, a.n_kv_heads);
+        if (first_head >= end_head) return; // the heads of a part are rounded up, so the last ones may have none
         const int64_t t0 = first + (int64_t)(block - part * n_windows) * window;
         if (part & 1) append_blocks<DTYPE, D, HALF, THREADS, false>(a, turn, tops, slots, t0, window, first_head, end_head);
         else append_blocks<DTYPE, D, HALF, THREADS, true>(a, turn, tops, slots, t0, window, first_head, end_head);
