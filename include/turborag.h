@@ -380,7 +380,8 @@ int tr_paged_append(const tr_shape* shape, const tr_rotary* rotary, const void* 
  * visible); scores are scaled by 1/sqrt(head_dim).
  * out [n_req, n_q_heads, head_dim], which may be q itself.  A request that sees no row (length 0, or no page behind any visible row) gets zeros.  Rows
  * that are not visible are not read as values: what they hold (NaN included) does not matter.
- * Scores, softmax and the weighted sum are fp32, whatever the type; scores may be of any size that fp32 has.  A visible value that
+ * Scores, softmax and the weighted sum are fp32, whatever the type; scores may be of any size that fp32 has.  The sum of values times weights of at
+ * most 1 comes before its division by the weights' sum, so that several values near the largest fp32 number may overflow.  A visible value that
  * is infinite makes its channel so (NaN where the channel holds both signs; it may where the weight is less than 2^-96 of the
  * largest).  The bits of a result depend on the batch's lengths, window and sinks, which decide how it is shared out, not on the
  * table's width or the order of pages.
@@ -403,8 +404,8 @@ int tr_paged_decode_attn(const tr_shape* shape, const void* q, const tr_pages* p
  * tr_pages_q8: row i of page p of KV head h begins at byte p * page_stride + i * row_stride + h * head_stride of k (and of v) and
  * is head_dim codes: e4m3 (1 sign, 4 exponent bits of bias 7, 3 mantissa bits; largest 448; 0x7f and 0xff NaN; no infinity).  Each block
  * of 16 rows of a page has for each head a scale for its keys and one for its values: k_scale, v_scale
- * [n_pages, n_kv_heads, page_size / 16], bytes s of the meaning 2^(s - 127).  A row is worth code * 2^(s - 127).  The calls write 10 <= s <= 247, with
- * which every value but NaN is a normal number or zero of fp32 and of bf16; other bytes from 1 to 254 are read for what they mean, as far
+ * [n_pages, n_kv_heads, page_size / 16], bytes s of the meaning 2^(s - 127).  A row is worth code * 2^(s - 127).  The calls write 10 <= s <= 247 and
+ * codes with which every value but NaN is a normal number or zero of fp32 and of bf16; other bytes from 1 to 254 are read for what they mean, as far
  * as the values are normal numbers or zero, 0 and 255 make the values of the block's rows undefined.
  * Strides, alignment and limits are those of tr_pages for elements of one byte, except that page_size is 16 .. 1024; the shape's dtype
  * is that of queries, new keys and values and results.  The scales have no alignment. */

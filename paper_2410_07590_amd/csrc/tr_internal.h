@@ -433,7 +433,7 @@ struct TrPagedAppendArgs {
     float eps, amplitude;
     double freq[64];
 };
-// Decode: each of TR_PAGED_WORKERS waves takes an equal share of the batch's units, of at least TR_PAGED_MIN_UNITS.
+// Decode: each of TR_PAGED_WORKERS waves (over codes: tr_q8_workers()) takes an equal share of the batch's units, of at least TR_PAGED_MIN_UNITS.
 __host__ __device__ constexpr int tr_paged_unit_keys(int dtype) { return dtype == TR_BF16 ? 32 : 16; }
 #define TR_PAGED_WORKERS 1024
 #define TR_PAGED_MIN_UNITS 1

@@ -2,14 +2,15 @@
 // on the GPU only.
 //
 // Bound by the stream of keys and values (4 g flops per 4 bytes of bf16 for g query heads to a KV head), so the design is about
-// keeping requests for memory on their way on every compute unit, whatever the lengths are:
+// keeping requests for memory on their way on every compute unit, whatever the lengths are.  (The cache is read once for each block of
+// at most 32 query heads to a KV head.)
 //
 // Work.  An item is a (request, KV head, block of at most 16 NT query heads).  Its visible keys are walked in units (32 of bf16,
-// 16 of fp32) by single waves that share nothing.  The host does not know the lengths, so the launch is a fixed number of waves,
-// four per compute unit, each of which takes ceil(sum / 1024) of the batch's units, in order of items: it works out the sum from
-// kv_lens and finds its own range in it.  So no share is longer than that, whatever the mix of lengths; the waves at the end have less
-// or nothing (1744 units are 872 shares of two), which matters where shares are few units long.  At most the first and the last item
-// of a share are cut.  Pieces of cut items go to the workspace and a second, small launch joins them.  (Workgroups of four waves that
+// 16 of fp32, 64 of codes) by single waves that share nothing.  The host does not know the lengths, so the launch is a fixed number of
+// waves, WORKERS: 1024, four per compute unit, twice as many for codes of 64 channels.  Each takes ceil(sum / WORKERS) of the batch's units, in
+// order of items (two waves a share, where two heads lie in one line: see the kernel): it works out the sum from kv_lens and finds its
+// own range in it.  So no share is longer than that, whatever the mix of lengths; the waves at the end have less or nothing (1744 units
+// are 872 shares of two for 1024 waves), which matters where shares are few units long.  At most the first and the last item of a share are cut.  Pieces of cut items go to the workspace and a second, small launch joins them.  (Workgroups of four waves that
 // walked an item's keys together and joined them in LDS took 94.3 us for 64 x 4096 rows where single waves took 90.3, 97.5 for one request
 // of 131071 rows (90.2), 104 for 200 requests of 50 to 1200 rows (95.1): their waves wait for one another at the end of each item.)
 //
@@ -56,8 +57,8 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 #define CONST_AS __attribute__((address_space(4)))
 
 constexpr float NOTHING = -__FLT_MAX__; // reference of a row that has seen no key
-// Non-temporal: every key is read once.  Where a row is half a line and the other half another head's, the waves of both heads want the
-// line, and it stays in the L2 for the second.  us, codes of 64 channels, 64 requests of 4000 rows of 16 / 4 heads, non-temporal / not: heads side by
+// Non-temporal: a key is read once, or once for each block of query heads.  Where a row is half a line and the other half another head's, the
+// waves of both heads want the line, and it stays in the L2 for the second.  us, codes of 64 channels, 64 requests of 4000 rows of 16 / 4 heads, non-temporal / not: heads side by
 // side 52.7 / 38.6 (114 or 65 thousand KB are fetched), rows side by side 33.5 / 36.5; heads of 128 channels 98.0 / 110.0.
 constexpr int DMA_STREAM = 2;
 // What a pool holds: a tr_dtype, which is the type of queries and results too, or codes with scales, the latter's type being FMT & 1.
